@@ -1,0 +1,656 @@
+"""The language-model operators on the GPU against the 64-bit oracle: sizes around every unit of
+work, types, row strides and alignments, masked rows and tokens, refusals, streams and graphs.
+
+Tolerances follow from the formulas.  With u = 2^-24 the unit roundoff of the 32-bit sums, d the
+distance of a logit to its row's maximum and D the mean of d under the softmax:
+  - a term exp(-d) carries 3 u d from its argument (difference, product, constant) and 4 u of its
+    own; a sum of n positive terms whose longest chain of additions is n_c carries n_c u more, with
+    n_c <= 64 + n / 64 for any split over at least a wave's lanes, or 64 values per lane;
+  - ln of the sum carries the sum's relative error, 4 u |ln S| from its evaluation and storage;
+  - p = exp(-d - ln S) carries 3 u d + 4 u ln S + 8 u besides the sum's;
+  - a result is rounded once to its type, whose unit roundoff is `U`, or to a multiple of the
+    type's smallest number `TINY`.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_20739_amd as P
+from paper_2607_20739_amd import ops
+from oracle import ops as O
+
+pytestmark = pytest.mark.gpu
+
+u = 2.0 ** -24
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+U = {"f32": 2.0 ** -24, "bf16": 2.0 ** -8, "f16": 2.0 ** -11}
+TINY = {"f32": 2.0 ** -126, "bf16": 2.0 ** -126, "f16": 2.0 ** -24}
+INF = float("inf")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    assert torch.cuda.is_available(), "GPU tests need an MI355X"
+    ops.lib()
+
+
+def _say(*what):
+    print("\n[gpu case]", *what, flush=True)
+
+
+def _place(x, pad=0, shift=0, fill=0.0):
+    """x on the GPU with `pad` columns more between its rows, starting `shift` values into its memory."""
+    rows, cols = x.shape
+    buf = torch.full((shift + rows * (cols + pad) + 32,), fill, dtype=x.dtype, device="cuda")
+    view = buf[shift:shift + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+    view.copy_(x)
+    return buf, view
+
+
+def _np(t):
+    return t.detach().double().cpu().numpy()
+
+
+def _close(got, want, tol, what):
+    got, want, tol = _np(got) if torch.is_tensor(got) else got, np.asarray(want), np.broadcast_to(tol, np.shape(want))
+    assert got.shape == want.shape
+    nan = np.isnan(want)
+    assert (np.isnan(got) == nan).all(), (what, "NaN places")
+    inf = np.isinf(want)
+    assert (got[inf] == want[inf]).all(), (what, "infinities")
+    rest = ~(nan | inf)
+    off = np.abs(got[rest] - want[rest])
+    bad = ~(off <= tol[rest])
+    assert not bad.any(), (what, int(bad.sum()), float((off - tol[rest]).max()), float(off.max()))
+
+
+# ---- dropout ------------------------------------------------------------------------------
+
+DROPOUT_SHAPES = [(1, 1), (3, 2), (2, 5), (5, 7), (4, 8), (3, 9), (2, 31), (7, 64), (33, 100), (1, 1001), (9, 1024),
+                  (3, 2049), (2, 8191)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", DROPOUT_SHAPES)
+def test_dropout_matches_the_oracle(dtype, rows, cols):
+    rng = np.random.default_rng(rows * 10007 + cols)
+    for case, (p, residual, ids, pad, shift) in enumerate([(0.1, False, False, 0, 0), (0.5, True, True, 0, 0),
+                                                           (0.25, True, False, 3, 1), (0.9, False, True, 5, 3)]):
+        _say("dropout", dtype, rows, cols, case)
+        seed = int(rng.integers(0, 1 << 63)) * 2 + 1
+        first = int(rng.integers(-100, 1 << 40))
+        row_ids = rng.integers(-5, 1 << 50, rows) if ids else first + np.arange(rows)
+        x = torch.from_numpy(rng.normal(size=(rows, cols))).to(DTYPES[dtype])
+        r = torch.from_numpy(rng.normal(size=(rows, cols))).to(DTYPES[dtype])
+        _, xg = _place(x, pad, shift)
+        _, rg = _place(r, pad + 1, shift)
+        buf, out = _place(torch.zeros_like(x), pad, shift, fill=77.0)
+        args = dict(row_ids=torch.from_numpy(row_ids).cuda() if ids else None, first_row=first)
+        got = ops.dropout(xg, p, seed, residual=rg if residual else None, out=out, **args)
+        assert got is out
+        want = O.dropout(x.double().numpy(), p, seed, row_ids, r.double().numpy() if residual else None)
+        # x s: factor and product; then the sum; then the type.
+        scaled = np.abs(want - (r.double().numpy() if residual else 0.0))
+        tol = 3 * u * scaled + u * np.abs(want) + U[dtype] * np.abs(want) * (1 + 4 * u) + TINY[dtype]
+        _close(got, want, tol, "out")
+        if not residual:
+            assert ((_np(got) == 0) == (want == 0)).all()
+        out.fill_(77.0)
+        assert (buf == 77.0).all(), "values outside of the output were written"
+        back = ops.dropout_backward(xg, p, seed, **args)
+        want = O.dropout(x.double().numpy(), p, seed, row_ids)
+        _close(back, want, 3 * u * np.abs(want) + U[dtype] * np.abs(want) * (1 + 4 * u) + TINY[dtype], "dx")
+
+
+def test_dropout_bounds_of_p_and_values_in_dropped_places():
+    _say("dropout p = 0, 1, NaN in dropped places")
+    x = torch.randn(5, 333, device="cuda")
+    r = torch.randn(5, 333, device="cuda")
+    assert torch.equal(ops.dropout(x, 0.0, 3), x)
+    assert torch.equal(ops.dropout(x, 1.0, 3), torch.zeros_like(x))
+    assert torch.equal(ops.dropout(x, 1.0, 3, residual=r), r)
+    assert torch.equal(ops.dropout(x, 2.0 ** -18, 3), x)           # rounds to no dropout
+    keep = torch.from_numpy(O.keep_mask(0.5, 3, range(5), 333)).cuda()
+    for v in (float("nan"), INF, -INF):
+        y = ops.dropout(torch.where(keep, x, v), 0.5, 3, residual=r)
+        assert torch.equal(y, torch.where(keep, 2 * x, 0.0) + r)
+        y = ops.dropout(torch.where(keep, v, x), 0.5, 3)
+        assert (y[~keep] == 0).all() and not y[keep].isfinite().any()
+
+
+def test_dropout_in_place_and_gathered_rows():
+    _say("dropout in place, gathered rows")
+    for dtype in DTYPES.values():
+        x = torch.randn(37, 515, device="cuda").to(dtype)
+        r = torch.randn(37, 515, device="cuda").to(dtype)
+        want = ops.dropout(x, 0.3, 11, residual=r, first_row=100)
+        order = torch.randperm(37, device="cuda")
+        got = ops.dropout(x[order], 0.3, 11, residual=r[order], row_ids=order + 100)
+        assert torch.equal(got, want[order])            # the mask goes with the row's number
+        a, b = x.clone(), r.clone()
+        assert torch.equal(ops.dropout(a, 0.3, 11, residual=r, first_row=100, out=a), want)
+        assert torch.equal(ops.dropout(x, 0.3, 11, residual=b, first_row=100, out=b), want)
+
+
+# ---- logits -------------------------------------------------------------------------------
+
+COLS = [1, 2, 3, 5, 7, 8, 9, 10, 15, 16, 17, 31, 33, 63, 64, 65, 100, 127, 129, 255, 256, 257, 500, 513, 1000, 1024,
+        1025, 2047, 2048, 2049, 4095, 4097, 8191, 8193, 12289, 16384, 16391, 32767, 40001, 50021, 65536, 65537, 100003,
+        131071, 131072, 131073, 262147]
+
+
+def _rows_for(cols):
+    return 37 if cols <= 64 else 11 if cols <= 4096 else 5
+
+
+def _case(dtype, rows, cols, seed, spread=2.0, banned=None):
+    """Logits on the CPU in their type, targets with some rows without a token."""
+    rng = np.random.default_rng(seed)
+    z = torch.from_numpy((rng.normal(size=(rows, cols)) * spread).astype(np.float32)).to(DTYPES[dtype])
+    y = torch.from_numpy(rng.integers(0, cols, rows).astype(np.int32))
+    z[torch.arange(rows), y.long()] += float(np.log(cols))
+    if banned is not None and cols > 3:
+        off = torch.from_numpy(rng.random(cols) < 0.2)
+        z[:, off] = banned
+        z[torch.arange(rows), y.long()] = 1.0
+    if rows > 2:
+        y[rng.integers(0, rows)] = -1
+        y[rng.integers(0, rows)] = cols
+    return z, y
+
+
+class _Expected:
+    """The oracle's values of a case, and the errors that 32-bit evaluation allows."""
+
+    def __init__(self, z, y):
+        self.z, self.y = z.double().numpy(), y.numpy()
+        rows, cols = self.z.shape
+        self.on = O.has_token(self.y, cols)
+        self.top, self.log_sum = O.row_stats(self.z)
+        with np.errstate(invalid="ignore"):
+            self.d = np.where(np.isfinite(self.z), self.top[:, None] - self.z, 0.0)
+            self.p = np.exp(self.z - self.top[:, None] - self.log_sum[:, None])
+        mean_d = np.nansum(np.where(self.p > 0, self.p * self.d, 0.0), 1)
+        self.sum_rel = u * (64 + cols / 64 + 4 + 3 * mean_d)
+        self.lp = O.token_logprobs(self.z, self.y)
+        self.lp[np.abs(self.lp) > float(np.finfo(np.float32).max)] *= INF   # past what 32 bits hold
+        dy = np.array([self.d[t, k] if o else 0.0 for t, (k, o) in enumerate(zip(self.y, self.on))])
+        self.lp_tol = self.sum_rel + u * (8 + 2 * dy + 4 * np.abs(self.log_sum))
+
+    def gradient(self, g, dtype, g_tol=0.0):
+        """(gradient, tolerance) for the factor g per row, itself known to g_tol."""
+        want = O.token_logprobs_backward(self.z, self.y, g)
+        g, g_tol = np.abs(g)[:, None], np.broadcast_to(g_tol, np.shape(g))[:, None]
+        rel = self.sum_rel[:, None] + u * (3 * self.d + 4 * np.abs(self.log_sum)[:, None] + 8)
+        p = np.nan_to_num(self.p)
+        tol = g * p * rel + 2 * u * np.abs(want) + g_tol * p
+        for t in np.flatnonzero(self.on):
+            tol[t, self.y[t]] += 2 * u * g[t, 0] + g_tol[t, 0]
+        tol[~self.on] = 0.0
+        return want, tol * (1 + U[dtype]) + U[dtype] * np.abs(want) + TINY[dtype]
+
+
+def _check_logprobs(z, y, dtype, pad, shift, seed):
+    e = _Expected(z, y)
+    _, zg = _place(z, pad, shift, fill=100.0)
+    yg = y.cuda()
+    lp, stats = ops.token_logprobs(zg, yg)
+    _close(lp, e.lp, e.lp_tol, "logprobs")
+    fine = e.on & ~np.isnan(e.log_sum)
+    _close(stats[:, 0].cpu().numpy()[fine], e.top[fine], 0.0, "maxima")
+    _close(stats[:, 1].cpu().double().numpy()[fine], e.log_sum[fine], (e.sum_rel + 4 * u * np.abs(e.log_sum))[fine], "log sums")
+    assert not stats[torch.from_numpy(~e.on).cuda()].any()
+    g = np.random.default_rng(seed).normal(size=len(z)).astype(np.float32)
+    g[0] = 0.0
+    buf, out = _place(torch.zeros_like(z), pad, shift, fill=77.0)
+    dz = ops.token_logprobs_backward(zg, yg, stats, torch.from_numpy(g).cuda(), out=out)
+    _close(dz, *e.gradient(g, dtype), "gradient")
+    out.fill_(77.0)
+    assert (buf == 77.0).all(), "values outside of the output were written"
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", COLS)
+def test_token_logprobs_match_the_oracle(dtype, cols):
+    for case, (pad, shift, banned) in enumerate([(0, 0, None), (3, 1, -INF), (0, 3, "lowest")]):
+        _say("logprobs", dtype, cols, case)
+        low = torch.finfo(DTYPES[dtype]).min if banned == "lowest" else banned
+        rows = _rows_for(cols) if case == 0 else 3
+        z, y = _case(dtype, rows, cols, cols * 31 + case, banned=low)
+        _check_logprobs(z, y, dtype, pad, shift, case)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [10, 1000, 40001])
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 8, 15, 16, 17, 31, 64, 65, 127, 255, 257, 1023])
+def test_token_logprobs_for_any_number_of_rows(dtype, cols, rows):
+    if rows * cols > 4_000_000:
+        rows = 4_000_000 // cols          # the largest on fewer rows
+    _say("logprobs rows", dtype, cols, rows)
+    z, y = _case(dtype, rows, cols, rows)
+    _check_logprobs(z, y, dtype, 0, 0, rows)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [10, 64, 1000, 9001, 131071])
+def test_logits_of_large_magnitude(dtype, cols):
+    """Maxima far from 0 cancel exactly: errors stay those of the differences."""
+    _say("logprobs magnitude", dtype, cols)
+    z, y = _case(dtype, 4, cols, cols, spread=30.0)
+    z = (z.float() + torch.tensor([[0.0], [3000.0], [-3000.0], [100.0]])).to(DTYPES[dtype])
+    _check_logprobs(z, y, dtype, 0, 0, 1)
+
+
+def _special_rows(dtype, cols):
+    """Rows whose mask leaves nothing or one value, extreme and broken rows, and what is to come."""
+    low, high = torch.finfo(DTYPES[dtype]).min, torch.finfo(DTYPES[dtype]).max
+    base = torch.linspace(-1, 1, cols)
+    last = cols - 1
+    rows = [base, torch.full((cols,), -INF), torch.full((cols,), low), torch.full((cols,), high), base.clone(),
+            base.clone(), base.clone(), torch.full((cols,), -INF), base.clone(), torch.full((cols,), -INF), base]
+    rows[4][last] = float("nan")
+    rows[5][0] = INF
+    rows[6][last] = -INF          # the target itself cannot occur
+    rows[7][last] = -2.0          # only the target can
+    rows[8][0], rows[8][last] = high, low
+    rows[9][0] = float("nan")
+    y = torch.full((len(rows),), last, dtype=torch.int32)
+    return torch.stack(rows).to(DTYPES[dtype]), y
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [2, 10, 65, 513, 1001, 4097, 20000, 70001, 131072, 200001])
+def test_special_rows(dtype, cols):
+    _say("special rows", dtype, cols)
+    z, y = _special_rows(dtype, cols)
+    e = _Expected(z, y)
+    zg, yg = z.cuda(), y.cuda()
+    lp, stats = ops.token_logprobs(zg, yg)
+    _close(lp, e.lp, np.nan_to_num(e.lp_tol, nan=0.0, posinf=0.0), "logprobs")
+    g = np.ones(len(z), np.float32)
+    want, tol = e.gradient(g, dtype)
+    dz = ops.token_logprobs_backward(zg, yg, stats, torch.from_numpy(g).cuda())
+    _close(dz, want, np.nan_to_num(tol), "gradient")
+    # The same rows through the policy loss (ratio 1 where the log-probability is finite).
+    old = torch.where(lp.isfinite(), lp, 0.0)
+    loss, lp2, dz2 = ops.policy_loss(zg, yg, old, torch.ones_like(lp), clip_low=1.0, clip_high=1e30)
+    broken = np.isnan(e.lp)
+    assert np.isnan(_np(loss)[broken]).all() and np.isnan(_np(dz2)[broken]).all()
+    assert np.isfinite(_np(loss)[~broken]).all() and np.isfinite(_np(dz2)[~broken]).all()
+    _close(lp2, e.lp, np.nan_to_num(e.lp_tol, nan=0.0, posinf=0.0), "policy logprobs")
+    # Skipped rows are not read: no token, no gradient, no weight.
+    none = torch.full_like(yg, -1)
+    lp, stats = ops.token_logprobs(zg, none)
+    assert not lp.any() and not stats.any()
+    for t, gr in [(none, torch.ones(len(z), device="cuda")), (yg, torch.zeros(len(z), device="cuda"))]:
+        assert not ops.token_logprobs_backward(zg, t, stats, gr).any()
+    for t, w in [(none, None), (yg, torch.zeros(len(z), device="cuda"))]:
+        for out in ops.policy_loss(zg, t, old, torch.ones_like(lp), token_weights=w):
+            assert not out.any()
+
+
+# ---- preference loss ----------------------------------------------------------------------
+
+def _offsets(rows, pairs, seed):
+    """Unequal sequences, some empty, with rows before the first and after the last."""
+    rng = np.random.default_rng(seed)
+    cuts = np.sort(rng.integers(rows // 10, rows - rows // 10 + 1, 2 * pairs + 1))
+    return cuts.astype(np.int32)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols,pairs", [(1, 5, 1), (7, 10, 2), (64, 33, 5), (40, 1000, 3), (33, 9001, 2),
+                                             (700, 100, 1), (9, 131071, 2), (2000, 17, 40), (12, 70001, 1)])
+def test_preference_loss_matches_the_oracle(dtype, rows, cols, pairs):
+    for case, (smoothing, with_ref, with_weights, pad) in enumerate([(0.0, True, False, 0), (0.1, False, True, 5)]):
+        _say("preference", dtype, rows, cols, pairs, case)
+        z, y = _case(dtype, rows, cols, rows + cols + case, banned=-INF if case else None)
+        rng = np.random.default_rng(case)
+        o = _offsets(rows, pairs, rows + case)
+        e = _Expected(z, y)
+        ref = (e.lp + rng.normal(size=rows) * 0.3).astype(np.float32) if with_ref else None
+        w = rng.uniform(size=pairs).astype(np.float32) if with_weights else None
+        if with_weights:
+            w[0] = 0.0
+        beta, scale = 0.3, 1.7
+        loss, margin, _, g = O.preference(e.z, e.y, o, ref, beta, smoothing, scale, w)
+        _, zg = _place(z, pad, case)
+        got = ops.preference_loss(zg, y.cuda(), torch.from_numpy(o).cuda(),
+                                  None if ref is None else torch.from_numpy(ref).cuda(), beta=beta,
+                                  label_smoothing=smoothing, scale=scale,
+                                  pair_weights=None if w is None else torch.from_numpy(w).cuda())
+        _close(got[2], e.lp, e.lp_tol, "logprobs")
+        # A margin carries its rows' errors (their 32-bit storage included); the loss follows it
+        # with a slope of at most 1, its slope with one of at most 1/4.
+        h_tol = np.array([beta * (e.lp_tol + u * np.abs(e.lp))[o[2 * i]:o[2 * i + 2]].sum() for i in range(pairs)])
+        _close(got[1], margin, h_tol + 2 * u * np.abs(margin), "margins")
+        _close(got[0], loss, h_tol + 2 * u * np.abs(loss), "loss")
+        g_tol = np.zeros(rows)
+        for i in range(pairs):
+            wi = 1.0 if w is None else w[i]
+            g_tol[o[2 * i]:o[2 * i + 2]] = 0.25 * scale * beta * wi * h_tol[i]
+        _close(got[3], *e.gradient(g, dtype, g_tol + 2 * u * np.abs(g)), "gradient")
+        only = ops.preference_loss(zg, y.cuda(), torch.from_numpy(o).cuda(),
+                                   None if ref is None else torch.from_numpy(ref).cuda(), beta=beta,
+                                   label_smoothing=smoothing, gradient=False)
+        assert only[3] is None
+        for a, b in zip(only[:3], got[:3]):
+            assert torch.equal(a, b)
+
+
+def test_preference_loss_edges():
+    _say("preference edges")
+    z, y = _case("f32", 20, 50, 1)
+    z, y = z.cuda(), y.cuda()
+    none = torch.zeros(1, dtype=torch.int32, device="cuda")
+    loss, margin, lp, dz = ops.preference_loss(z, y, none)
+    assert loss.numel() == 0 and not dz.any() and torch.equal(lp, ops.token_logprobs(z, y)[0])
+    # Two empty sequences: h = 0.
+    zero = torch.full((3,), 7, dtype=torch.int32, device="cuda")
+    loss, margin, _, dz = ops.preference_loss(z, y, zero)
+    assert loss.item() == pytest.approx(np.log(2), abs=1e-7) and margin.item() == 0 and not dz.any()
+    # No rows at all.
+    loss, margin, lp, dz = ops.preference_loss(z[:0], y[:0], torch.zeros(5, dtype=torch.int32, device="cuda"))
+    assert (loss - np.log(2)).abs().max().item() < 1e-7 and dz.shape == (0, 50)
+    # Offsets outside of the rows are taken as their bounds.
+    wild = torch.tensor([-9, 8, 1 << 30], dtype=torch.int32, device="cuda")
+    tame = torch.tensor([0, 8, 20], dtype=torch.int32, device="cuda")
+    for a, b in zip(ops.preference_loss(z, y, wild), ops.preference_loss(z, y, tame)):
+        assert torch.equal(a, b)
+    # A margin far out: finite loss, gradient of at most the slope's bound, none NaN.
+    far = torch.full((20,), 1e6, device="cuda")
+    loss, margin, _, dz = ops.preference_loss(z, y, tame, far, beta=5.0)
+    assert loss.isfinite().all() and dz.isfinite().all()
+    # NaN in one pair's rows stays in that pair; a pair of weight 0 lets nothing through.
+    two = torch.tensor([0, 4, 9, 13, 20], dtype=torch.int32, device="cuda")
+    y = torch.arange(20, dtype=torch.int32, device="cuda")
+    want = ops.preference_loss(z, y, two)
+    bad = z.clone()
+    bad[2, 3] = float("nan")
+    loss, margin, lp, dz = ops.preference_loss(bad, y, two)
+    assert loss[0].isnan() and loss[1] == want[0][1] and torch.equal(dz[9:], want[3][9:]) and dz[:9].isnan().all()
+    loss, _, _, dz = ops.preference_loss(bad, y, two, pair_weights=torch.tensor([0.0, 1.0], device="cuda"))
+    assert not dz[:9].any() and torch.equal(dz[9:], want[3][9:])
+
+
+# ---- policy loss --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [1, 5, 10, 33, 64, 129, 1000, 1025, 2049, 4097, 8191, 16391, 32768, 50021, 65537, 131071,
+                                  131072, 131080, 200001])
+def test_policy_loss_matches_the_oracle(dtype, cols):
+    for case, (kl, weighted, pad, shift, banned) in enumerate([(0.0, False, 0, 0, None), (0.3, True, 7, 1, -INF),
+                                                               (0.05, False, 0, 5, "lowest")]):
+        _say("policy", dtype, cols, case)
+        rows = max(_rows_for(cols), 9)
+        low = torch.finfo(DTYPES[dtype]).min if banned == "lowest" else banned
+        z, y = _case(dtype, rows, cols, cols + case, banned=low)
+        e = _Expected(z, y)
+        rng = np.random.default_rng(case + cols)
+        # Ratios at fixed distances from 1: inside, and clear of both bounds.
+        shift_lp = rng.choice([-0.6, -0.1, 0.05, 0.5], rows)
+        old = (e.lp - shift_lp).astype(np.float32)
+        adv = rng.normal(size=rows).astype(np.float32)
+        adv[0] = 0.0
+        ref = (e.lp + 0.4 * rng.normal(size=rows)).astype(np.float32)
+        w = rng.uniform(size=rows).astype(np.float32) if weighted else None
+        if weighted:
+            w[1] = 0.0
+        kw = dict(clip_low=0.2, clip_high=0.28, kl=kl, scale=0.7)
+        loss, lp, g = O.policy(e.z, e.y, old, adv, ref, weights=w, **kw)
+        _, zg = _place(z, pad, shift, fill=100.0)
+        buf, out = _place(torch.zeros_like(z), pad, shift, fill=77.0)
+        args = dict(kw, ref_logprobs=torch.from_numpy(ref).cuda() if kl else None,
+                    token_weights=None if w is None else torch.from_numpy(w).cuda())
+        dev = [torch.from_numpy(old).cuda(), torch.from_numpy(adv).cuda()]
+        got = ops.policy_loss(zg, y.cuda(), *dev, out=out, **args)
+        on = e.on if w is None else e.on & (w != 0)
+        ratio, off = np.exp(e.lp - old), np.exp(ref.astype(np.float64) - e.lp)
+        # The log-probability's error (its storage included) acts on the ratio and on exp(ref - l);
+        # each exponential adds 4 u and what its argument's rounding gives, each product and sum u.
+        l_err = np.where(on, e.lp_tol + 2 * u * (np.abs(e.lp) + np.abs(old) + np.abs(ref)), 0.0)
+        part = np.abs(adv) * np.where(on, ratio, 0) * (l_err + 8 * u)
+        kl_part = kl * (np.abs(off - 1) * l_err + off * 8 * u + 8 * u)
+        _close(got[1], lp, np.where(on, e.lp_tol, 0.0), "logprobs")
+        _close(got[0], loss, part + np.where(on, kl_part, 0) + 4 * u * (np.abs(loss) + np.abs(adv) * 1.3), "loss")
+        slope_tol = part + kl * off * (l_err + 8 * u) + kl * 4 * u
+        g_tol = np.where(on, 0.7 * (1.0 if w is None else w) * slope_tol, 0.0) + 6 * u * np.abs(g)
+        _close(got[2], *e.gradient(g, dtype, g_tol), "gradient")
+        only = ops.policy_loss(zg, y.cuda(), *dev, gradient=False, **args)
+        assert only[2] is None and torch.equal(only[0], got[0]) and torch.equal(only[1], got[1])
+        out.fill_(77.0)
+        assert (buf == 77.0).all(), "values outside of the output were written"
+
+
+def test_policy_loss_infinite_ratios():
+    """Ratios that overflow: bounded where the bound holds, no NaN from a zero advantage."""
+    _say("policy infinite ratios")
+    z = torch.randn(4, 100, device="cuda")
+    y = torch.zeros(4, dtype=torch.int32, device="cuda")
+    old = torch.full((4,), -1e4, device="cuda")
+    adv = torch.tensor([1.0, 0.0, 2.0, 0.5], device="cuda")
+    loss, _, dz = ops.policy_loss(z, y, old, adv, clip_low=0.2, clip_high=0.5)
+    assert loss.tolist() == [-1.5, 0.0, -3.0, -0.75] and not dz.any()
+
+
+# ---- what holds for all -------------------------------------------------------------------
+
+def _everything(z, y, extra=None):
+    """Every logits operator's outputs for these inputs."""
+    rows = z.shape[0]
+    lp, stats = ops.token_logprobs(z, y)
+    g = torch.linspace(-1, 1, rows, device="cuda") if extra is None else extra
+    offsets = torch.tensor([0, rows // 3, rows], dtype=torch.int32, device="cuda")
+    old, adv = lp.detach() + 0.05, g + 0.5
+    return ([lp, stats, ops.token_logprobs_backward(z, y, stats, g)] +
+            list(ops.policy_loss(z, y, old, adv, ref_logprobs=old + 0.1, kl=0.1)) +
+            list(ops.preference_loss(z, y, offsets, old, beta=0.2)))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [10, 129, 1001, 5000, 30001, 131071, 200001])
+def test_results_depend_on_the_rows_values_alone(dtype, cols):
+    """The same bits again, at other alignments and strides, in place, and for a row by itself."""
+    _say("same bits", dtype, cols)
+    z, y = _case(dtype, 9, cols, 3)
+    yg = y.cuda()
+    want = _everything(z.cuda(), yg)
+    for pad, shift in [(0, 0), (0, 1), (1, 0), (6, 2), (8, 8), (13, 7)]:
+        for a, b in zip(_everything(_place(z, pad, shift)[1], yg), want):
+            assert torch.equal(a, b), (pad, shift)
+    lp, stats, dz, loss, _, dz_policy, _, _, _, dz_pair = want
+    g = torch.linspace(-1, 1, 9, device="cuda")
+    for t in range(9):
+        zt, yt = z[t:t + 1].cuda(), yg[t:t + 1]
+        lpt, st = ops.token_logprobs(zt, yt)
+        assert torch.equal(lpt, lp[t:t + 1]) and torch.equal(st, stats[t:t + 1])
+        assert torch.equal(ops.token_logprobs_backward(zt, yt, st, g[t:t + 1]), dz[t:t + 1])
+    a = z.cuda()
+    assert ops.token_logprobs_backward(a, yg, stats, g, out=a) is a and torch.equal(a, dz)
+    a = z.cuda()
+    got = ops.policy_loss(a, yg, lp + 0.05, g + 0.5, ref_logprobs=lp + 0.05 + 0.1, kl=0.1, out=a)
+    assert torch.equal(got[0], loss) and torch.equal(a, dz_policy)
+    a = z.cuda()
+    offsets = torch.tensor([0, 3, 9], dtype=torch.int32, device="cuda")
+    ops.preference_loss(a, yg, offsets, lp + 0.05, beta=0.2, out=a)
+    assert torch.equal(a, dz_pair)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_offsets_past_32_bits(dtype):
+    """Rows 2^31 values apart: the third starts past 2^32."""
+    _say("far rows", dtype)
+    rows, cols, stride = 3, 1001, (1 << 31) + 3
+    buf = torch.empty((rows - 1) * stride + cols, dtype=DTYPES[dtype], device="cuda")
+    far = buf.as_strided((rows, cols), (stride, 1))
+    z, y = _case(dtype, rows, cols, 8)
+    y = torch.tensor([5, 0, cols - 1], dtype=torch.int32).cuda()
+    near = z.cuda()
+    want = _everything(near, y)
+    far.copy_(near)
+    for a, b in zip(_everything(far, y), want):
+        assert torch.equal(a, b)
+    g = torch.ones(rows, device="cuda")
+    want = ops.token_logprobs_backward(near, y, want[1], g)
+    stats = ops.token_logprobs(far, y)[1]
+    assert torch.equal(ops.token_logprobs_backward(far, y, stats, g, out=far), want)
+    far.copy_(near)
+    want = ops.dropout(near, 0.4, 77, residual=near)
+    assert torch.equal(ops.dropout(far, 0.4, 77, residual=far), want)
+    assert torch.equal(ops.dropout(far, 0.4, 77, residual=far, out=far), want)
+
+
+def test_many_rows():
+    """More rows than one launch has blocks or waves for at once; rows of 3 columns in 64 bits by torch."""
+    _say("many rows")
+    rows, cols = 5_000_003, 3
+    z = torch.randn(rows, cols, device="cuda")
+    y = torch.randint(-1, cols, (rows,), device="cuda").to(torch.int32)
+    lp, stats = ops.token_logprobs(z, y)
+    x = torch.log_softmax(z.double(), 1)
+    on = y >= 0
+    want = torch.where(on, x.gather(1, y.clamp(min=0).long()[:, None])[:, 0], 0.0)
+    # |z| < 8, three terms: the bounds above give less than 40 u.
+    assert (lp.double() - want).abs().max().item() < 100 * u
+    dz = ops.token_logprobs_backward(z, y, stats, torch.ones(rows, device="cuda"))
+    one = torch.zeros_like(x).scatter_(1, y.clamp(min=0).long()[:, None], 1.0)
+    want = torch.where(on[:, None], one - x.exp(), 0.0)
+    assert (dz.double() - want).abs().max().item() < 100 * u
+    z2 = ops.dropout(z, 0.5, 9)
+    tail = O.dropout(z[-5:].cpu().double().numpy(), 0.5, 9, range(rows - 5, rows))
+    np.testing.assert_array_equal(_np(z2[-5:]), tail)
+
+
+def test_results_repeat_bit_for_bit_and_follow_the_stream():
+    _say("streams")
+    z, y = _case("bf16", 300, 20001, 5)
+    z, y = z.cuda(), y.cuda()
+    want = _everything(z, y)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        late = torch.zeros_like(z)
+        for _ in range(20):
+            late.copy_(z)                   # the operators have to wait for what the stream did before
+        got = _everything(late, y)
+        x = ops.dropout(late, 0.2, 4)
+    side.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    assert torch.equal(x, ops.dropout(z, 0.2, 4))
+
+
+@pytest.mark.parametrize("dtype,rows,cols", [("bf16", 65, 50021), ("f32", 33, 10), ("f16", 9, 131072)])
+def test_operators_can_be_captured_into_a_graph(dtype, rows, cols):
+    _say("graph", dtype, rows, cols)
+    cases = [_case(dtype, rows, cols, s) for s in range(3)]
+    z, y = cases[0][0].cuda(), cases[0][1].cuda()
+    g = torch.linspace(-1, 1, rows, device="cuda")
+    wants = []
+    for a, b in cases:
+        wants.append([t.clone() for t in _everything(a.cuda(), b.cuda(), g)] + [ops.dropout(a.cuda(), 0.3, 21)])
+    torch.cuda.synchronize()
+    offsets = torch.tensor([0, rows // 3, rows], dtype=torch.int32, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lp, stats = ops.token_logprobs(z, y)
+        old = lp + 0.05
+        got = [lp, stats, ops.token_logprobs_backward(z, y, stats, g),
+               *ops.policy_loss(z, y, old, g + 0.5, ref_logprobs=old + 0.1, kl=0.1),
+               *ops.preference_loss(z, y, offsets, old, beta=0.2), ops.dropout(z, 0.3, 21)]
+    for replay in (0, 1, 2, 1, 0):
+        z.copy_(cases[replay][0])
+        y.copy_(cases[replay][1])
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for i, (a, b) in enumerate(zip(got, wants[replay])):
+            assert torch.equal(a, b), (replay, i)
+
+
+def test_autograd_and_differences():
+    """Through torch's autograd, against central differences of the 64-bit oracle along a random
+    direction: truncation and rounding of the differences are below 1e-7, the 32-bit gradient's
+    error below (64 + 8) u of its terms' absolute sum (below 40 here)."""
+    _say("autograd")
+    rows, cols = 12, 30
+    rng = np.random.default_rng(4)
+    h = rng.normal(size=(rows, cols))
+    r = rng.normal(size=(rows, cols))
+    y = rng.integers(0, cols, rows).astype(np.int32)
+    c = rng.normal(size=rows)
+    hg = torch.from_numpy(h).float().cuda().requires_grad_()
+    rg = torch.from_numpy(r).float().cuda().requires_grad_()
+    z = ops.dropout(hg, 0.3, 8, residual=rg, first_row=40)
+    lp, stats = ops.token_logprobs(z, torch.from_numpy(y).cuda())
+    assert not stats.requires_grad
+    (lp * torch.from_numpy(c).float().cuda()).sum().backward()
+
+    def value(hh, rr):
+        zz = O.dropout(hh, 0.3, 8, range(40, 40 + rows), rr)
+        return (c * O.token_logprobs(zz, y)).sum()
+
+    v, w, step = rng.normal(size=h.shape), rng.normal(size=h.shape), 1e-5
+    dh = (value(h + step * v, r) - value(h - step * v, r)) / (2 * step)
+    dr = (value(h, r + step * w) - value(h, r - step * w)) / (2 * step)
+    tol = 1e-7 + 72 * u * 400
+    assert abs((_np(hg.grad) * v).sum() - dh) < tol and abs((_np(rg.grad) * w).sum() - dr) < tol
+
+    # The losses' gradients along a direction, against differences of the oracle's losses.
+    z64 = rng.normal(size=(rows, cols))
+    z32 = torch.from_numpy(z64).float()
+    z64 = z32.double().numpy()
+    offsets, ref = np.array([0, 4, 7, 9, 12], np.int32), rng.normal(size=rows).astype(np.float32)
+    got = ops.preference_loss(z32.cuda(), torch.from_numpy(y).cuda(), torch.from_numpy(offsets).cuda(),
+                              torch.from_numpy(ref).cuda(), beta=0.5, label_smoothing=0.1)[3]
+    d = sum(s * O.preference(z64 + s * step * v, y, offsets, ref, 0.5, 0.1)[0].sum() for s in (1, -1)) / (2 * step)
+    assert abs((_np(got) * v).sum() - d) < tol
+    lp = O.token_logprobs(z64, y)
+    old = (lp - rng.choice([-0.5, -0.1, 0.1, 0.5], rows)).astype(np.float32)
+    adv = rng.normal(size=rows).astype(np.float32)
+    got = ops.policy_loss(z32.cuda(), torch.from_numpy(y).cuda(), torch.from_numpy(old).cuda(),
+                          torch.from_numpy(adv).cuda(), ref_logprobs=torch.from_numpy(ref).cuda(), kl=0.01)[2]
+    d = sum(s * O.policy(z64 + s * step * v, y, old, adv, ref, kl=0.01)[0].sum() for s in (1, -1)) / (2 * step)
+    assert abs((_np(got) * v).sum() - d) < tol
+
+
+def test_the_binding_refuses_what_does_not_fit():
+    _say("refusals")
+    z = torch.randn(6, 40, device="cuda")
+    y = torch.zeros(6, dtype=torch.int32, device="cuda")
+    f = torch.zeros(6, device="cuda")
+    lp, stats = ops.token_logprobs(z, y)
+    o = torch.tensor([0, 3, 6], dtype=torch.int32, device="cuda")
+    bad = [
+        lambda: ops.dropout(z[0], 0.1, 1), lambda: ops.dropout(z.double(), 0.1, 1), lambda: ops.dropout(z.t(), 0.1, 1),
+        lambda: ops.dropout(z, 0.1, 1, residual=z[:5]), lambda: ops.dropout(z, 0.1, 1, residual=z.half()),
+        lambda: ops.dropout(z, 0.1, 1, row_ids=y), lambda: ops.dropout(z, 0.1, 1, out=z[:, :39]),
+        lambda: ops.dropout(z[:1].expand(6, 40), 0.1, 1),
+        lambda: ops.dropout(z.clone().requires_grad_(), 0.1, 1, out=torch.empty_like(z)),
+        lambda: ops.token_logprobs(z, y.long()), lambda: ops.token_logprobs(z, y[:5]),
+        lambda: ops.token_logprobs(z, y.cpu()), lambda: ops.token_logprobs_backward(z, y, stats[:, 0], f),
+        lambda: ops.token_logprobs_backward(z, y, stats, f.double()),
+        lambda: ops.preference_loss(z, y, o[:2]), lambda: ops.preference_loss(z, y, o.long()),
+        lambda: ops.preference_loss(z, y, o, ref_logprobs=f[:3]),
+        lambda: ops.preference_loss(z, y, o, pair_weights=f),
+        lambda: ops.preference_loss(z, y, o, workspace=torch.empty(4096, dtype=torch.int8, device="cuda")),
+        lambda: ops.policy_loss(z, y, f[:2], f), lambda: ops.policy_loss(z, y, f, f, token_weights=y),
+        lambda: ops.policy_loss(z, y, f, f, out=z.half()),
+    ]
+    for call in bad:
+        with pytest.raises(ValueError):
+            call()
+    refused = [
+        lambda: ops.dropout(z, 1.5, 1), lambda: ops.dropout(z[:, :20], 0.1, 1, out=z[:, 10:30]),
+        lambda: ops.policy_loss(z, y, f, f, kl=0.1), lambda: ops.policy_loss(z, y, f, f, clip_low=2.0),
+        lambda: ops.preference_loss(z, y, o, label_smoothing=-1.0),
+        lambda: ops.preference_loss(z, y, o, workspace=torch.empty(0, dtype=torch.uint8, device="cuda")),
+    ]
+    for call in refused:
+        with pytest.raises(P.PGCError) as e:
+            call()
+        assert e.value.status == P.PGC_EINVAL and str(e.value)
+    assert ops.dropout(z[:0], 0.1, 1).shape == (0, 40) and ops.dropout(z[:, :0], 0.1, 1).shape == (6, 0)
+    lp, stats = ops.token_logprobs(z[:0], y[:0])
+    assert lp.shape == (0,) and stats.shape == (0, 2)
