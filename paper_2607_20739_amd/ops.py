@@ -14,6 +14,8 @@ There is no fallback: without the library, or off the GPU, every call raises.
 
 import ctypes
 
+import torch
+
 from . import _lib
 from ._lib import PGCError, PGC_OK
 
@@ -56,21 +58,20 @@ _SIGNATURES = {
     "pgc_policy_loss": (ctypes.c_int, [ctypes.POINTER(pgc_logits), ctypes.POINTER(pgc_policy_args), _P]),
 }
 
+_DTYPES = {torch.float32: PGC_F32, torch.bfloat16: PGC_BF16, torch.float16: PGC_F16}
+
 _handle = None
-_dtypes = None
 
 
 def lib():
     """The loaded library with this module's entry points typed."""
-    global _handle, _dtypes
+    global _handle
     if _handle is None:
-        import torch
         handle = _lib.lib()
         for name, (res, args) in _SIGNATURES.items():
             fn = getattr(handle, name)
             fn.restype = res
             fn.argtypes = args
-        _dtypes = {torch.float32: PGC_F32, torch.bfloat16: PGC_BF16, torch.float16: PGC_F16}
         _handle = handle
     return _handle
 
@@ -86,7 +87,7 @@ def _check(status):
 
 def _matrix(name, x, like=None):
     """Row stride of a 2-D GPU matrix; of `like`'s shape, type and GPU where given."""
-    if x.dim() != 2 or x.dtype not in _dtypes or not x.is_cuda:
+    if x.dim() != 2 or x.dtype not in _DTYPES or not x.is_cuda:
         raise ValueError("%s must be a 2-D float32, bfloat16 or float16 tensor on the GPU" % name)
     if like is not None and (x.shape != like.shape or x.dtype != like.dtype or x.device != like.device):
         raise ValueError("%s must have the shape, dtype and device %s, %s, %s"
@@ -113,21 +114,30 @@ def _array(name, x, like, dtype, shape):
 
 def _call(like, name, *args):
     """Calls an entry point on torch's current stream of the GPU that `like` is on."""
-    import torch
-    fn = getattr(lib(), name)
-    device = like.device
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+    fn = getattr(_handle or lib(), name)
+    index = like.device.index
+    if index == torch.cuda.current_device():
+        status = fn(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(device):
-            _check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
+        with torch.cuda.device(index):
+            status = fn(*args, _raw_stream(index))
+    if status != PGC_OK:
+        _check(status)
+
+
+def _raw_stream(index):
+    """Handle of torch's current stream of a GPU."""
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# The same without a Stream object around it, where torch has that (2 us of a call's 12 less).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
 
 
 def _output(like, out):
     """The tensor that receives a result of `like`'s shape, and its row stride."""
-    import torch
     if out is None:
-        return torch.empty(like.shape, dtype=like.dtype, device=like.device), like.shape[1]
+        return like.new_empty(like.shape), like.shape[1]
     stride = _matrix("out", out, like)
     if not out.is_inference():
         torch.autograd.graph.increment_version(out)   # autograd notices a saved tensor that this changes
@@ -135,22 +145,19 @@ def _output(like, out):
 
 
 def _wants_grad(*tensors):
-    import torch
     return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
 # ---- dropout ----------------------------------------------------------------------------
 
 def _dropout(name, x, p, seed, residual, row_ids, first_row, out):
-    import torch
-    lib()
     stride = _matrix("x", x)
     rows, cols = x.shape
     out, out_stride = _output(x, out)
     ids = _array("row_ids", row_ids, x, torch.int64, (rows,))
     args = pgc_dropout_args(x.data_ptr(), None if residual is None else residual.data_ptr(), out.data_ptr(), ids,
                             rows, cols, stride, 0 if residual is None else _matrix("residual", residual, x),
-                            out_stride, first_row, int(seed) & 0xFFFFFFFFFFFFFFFF, p, _dtypes[x.dtype])
+                            out_stride, first_row, int(seed) & 0xFFFFFFFFFFFFFFFF, p, _DTYPES[x.dtype])
     _call(x, name, ctypes.byref(args))
     return out
 
@@ -166,7 +173,7 @@ def dropout(x, p, seed, residual=None, row_ids=None, first_row=0, out=None):
     if _wants_grad(x, residual):
         if out is not None:
             raise ValueError("out cannot be given where a gradient is asked for")
-        return _dropout_function().apply(x, residual, p, seed, row_ids, first_row)
+        return _Dropout.apply(x, residual, p, seed, row_ids, first_row)
     return _dropout("pgc_dropout", x, p, seed, residual, row_ids, first_row, out)
 
 
@@ -179,11 +186,9 @@ def dropout_backward(dout, p, seed, row_ids=None, first_row=0, out=None):
 
 def _logits(logits, targets):
     """The logits' description and the targets' address."""
-    import torch
-    lib()
     stride = _matrix("logits", logits)
     rows, cols = logits.shape
-    return (pgc_logits(logits.data_ptr(), rows, cols, stride, _dtypes[logits.dtype]),
+    return (pgc_logits(logits.data_ptr(), rows, cols, stride, _DTYPES[logits.dtype]),
             _array("targets", targets, logits, torch.int32, (rows,)))
 
 
@@ -191,22 +196,20 @@ def token_logprobs(logits, targets):
     """(logprobs [rows], stats [rows, 2]): each row's log-probability of its target, and its maximum
     and the log of its sum of exp(z - maximum), which the backward pass takes."""
     if _wants_grad(logits):
-        return _logprobs_function().apply(logits, targets)
+        return _TokenLogprobs.apply(logits, targets)
     return _token_logprobs(logits, targets)
 
 
 def _token_logprobs(logits, targets):
-    import torch
     z, y = _logits(logits, targets)
-    logprobs = torch.empty(z.rows, dtype=torch.float32, device=logits.device)
-    stats = torch.empty((z.rows, 2), dtype=torch.float32, device=logits.device)
+    logprobs = logits.new_empty(z.rows, dtype=torch.float32)
+    stats = logits.new_empty((z.rows, 2), dtype=torch.float32)
     _call(logits, "pgc_token_logprobs", ctypes.byref(z), y, logprobs.data_ptr(), stats.data_ptr())
     return logprobs, stats
 
 
 def token_logprobs_backward(logits, targets, stats, grad, out=None):
     """Gradient of the logits from the gradient of the log-probabilities.  `out` may be the logits."""
-    import torch
     z, y = _logits(logits, targets)
     stats = _array("stats", stats, logits, torch.float32, (z.rows, 2))
     grad = _array("grad", grad, logits, torch.float32, (z.rows,))
@@ -233,19 +236,17 @@ def preference_loss(logits, targets, offsets, ref_logprobs=None, beta=0.1, label
     `out` receives it and may be the logits.  `workspace` (uint8, preference_workspace_bytes(rows))
     is allocated where it is not given.
     """
-    import torch
     z, y = _logits(logits, targets)
-    device = logits.device
     pairs = (offsets.numel() - 1) // 2
     offsets = _array("offsets", offsets, logits, torch.int32, (2 * max(pairs, 0) + 1,))
     ref = _array("ref_logprobs", ref_logprobs, logits, torch.float32, (z.rows,))
     weights = _array("pair_weights", pair_weights, logits, torch.float32, (pairs,))
     if workspace is None:
-        workspace = torch.empty(preference_workspace_bytes(z.rows), dtype=torch.uint8, device=device)
+        workspace = logits.new_empty(preference_workspace_bytes(z.rows), dtype=torch.uint8)
     ws = _array("workspace", workspace, logits, torch.uint8, workspace.shape)
-    loss = torch.empty(pairs, dtype=torch.float32, device=device)
-    margins = torch.empty(pairs, dtype=torch.float32, device=device)
-    logprobs = torch.empty(z.rows, dtype=torch.float32, device=device)
+    loss = logits.new_empty(pairs, dtype=torch.float32)
+    margins = logits.new_empty(pairs, dtype=torch.float32)
+    logprobs = logits.new_empty(z.rows, dtype=torch.float32)
     stride = 0
     if gradient:
         out, stride = _output(logits, out)
@@ -262,15 +263,14 @@ def policy_loss(logits, targets, old_logprobs, advantages, ref_logprobs=None, cl
     dlogits is the gradient of scale * sum(token_weights * loss), None with gradient=False.  `out`
     receives it and may be the logits.
     """
-    import torch
     z, y = _logits(logits, targets)
-    device, f32, rows = logits.device, torch.float32, (z.rows,)
+    f32, rows = torch.float32, (z.rows,)
     old = _array("old_logprobs", old_logprobs, logits, f32, rows)
     adv = _array("advantages", advantages, logits, f32, rows)
     ref = _array("ref_logprobs", ref_logprobs, logits, f32, rows)
     weights = _array("token_weights", token_weights, logits, f32, rows)
-    loss = torch.empty(rows, dtype=f32, device=device)
-    logprobs = torch.empty(rows, dtype=f32, device=device)
+    loss = logits.new_empty(rows, dtype=f32)
+    logprobs = logits.new_empty(rows, dtype=f32)
     stride = 0
     if gradient:
         out, stride = _output(logits, out)
@@ -282,46 +282,29 @@ def policy_loss(logits, targets, old_logprobs, advantages, ref_logprobs=None, cl
 
 # ---- autograd -------------------------------------------------------------------------------
 
-_functions = {}
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, p, seed, row_ids, first_row):
+        ctx.args = (p, seed, row_ids, first_row)
+        return _dropout("pgc_dropout", x, p, seed, residual, row_ids, first_row, None)
+
+    @staticmethod
+    def backward(ctx, dout):
+        dx = dropout_backward(dout.contiguous(), *ctx.args) if ctx.needs_input_grad[0] else None
+        return dx, dout if ctx.needs_input_grad[1] else None, None, None, None, None
 
 
-def _dropout_function():
-    """torch.autograd.Function of dropout (made on first use: importing this module needs no torch)."""
-    if "dropout" not in _functions:
-        import torch
+class _TokenLogprobs(torch.autograd.Function):
+    """The stats carry no gradient."""
 
-        class Dropout(torch.autograd.Function):
-            @staticmethod
-            def forward(ctx, x, residual, p, seed, row_ids, first_row):
-                ctx.args = (p, seed, row_ids, first_row)
-                return _dropout("pgc_dropout", x, p, seed, residual, row_ids, first_row, None)
+    @staticmethod
+    def forward(ctx, logits, targets):
+        logprobs, stats = _token_logprobs(logits, targets)
+        ctx.save_for_backward(logits, targets, stats)
+        ctx.mark_non_differentiable(stats)
+        return logprobs, stats
 
-            @staticmethod
-            def backward(ctx, dout):
-                dx = dropout_backward(dout.contiguous(), *ctx.args) if ctx.needs_input_grad[0] else None
-                return dx, dout if ctx.needs_input_grad[1] else None, None, None, None, None
-
-        _functions["dropout"] = Dropout
-    return _functions["dropout"]
-
-
-def _logprobs_function():
-    """torch.autograd.Function of token_logprobs; its stats carry no gradient."""
-    if "logprobs" not in _functions:
-        import torch
-
-        class TokenLogprobs(torch.autograd.Function):
-            @staticmethod
-            def forward(ctx, logits, targets):
-                logprobs, stats = _token_logprobs(logits, targets)
-                ctx.save_for_backward(logits, targets, stats)
-                ctx.mark_non_differentiable(stats)
-                return logprobs, stats
-
-            @staticmethod
-            def backward(ctx, grad, _):
-                logits, targets, stats = ctx.saved_tensors
-                return token_logprobs_backward(logits, targets, stats, grad.contiguous()), None
-
-        _functions["logprobs"] = TokenLogprobs
-    return _functions["logprobs"]
+    @staticmethod
+    def backward(ctx, grad, _):
+        logits, targets, stats = ctx.saved_tensors
+        return token_logprobs_backward(logits, targets, stats, grad.contiguous()), None
