@@ -1,17 +1,22 @@
 // Token log-probabilities, their gradient, the policy loss and the preference loss's pair
 // sums (include/pgc_ops.h), for gfx950.
 //
-// A row of logits belongs to a group of LANES lanes (4 to 1,024): lane i takes the 16-byte
-// vectors i, i + LANES, ... counted from the row's first value, wherever that lies in memory
-// (loads and stores work at any alignment), and the last values that fill no vector go to one
-// lane each.  Which lane sums what, and hence every bit of the result, depends on the number of
-// columns alone.  Each lane keeps a running maximum and sum; lanes and waves join theirs once.
+// A row of up to 32 vectors of 16 bytes belongs to 4 to 32 lanes of a wave, a longer one to 1 to
+// 16 waves, each with a run of neighbouring vectors.  Which lane sums what, and hence every bit of
+// the result, depends on the number of columns alone, not on where the row lies.  Each lane keeps
+// a running maximum and sum; lanes and waves join theirs once.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "pgc_lanes.h"
 #include "pgc_ops_kernels.h"
+
+// A product and a sum are rounded apart unless a fused operation is written: otherwise the compiler
+// fuses them in some copies of the same code and not in others, and bits would depend on where a
+// row lies.
+#pragma clang fp contract(off)
 
 namespace pgc {
 namespace {
@@ -31,13 +36,17 @@ struct Vec {
 
   // Vector `first + lane` of a row; `first` is the same for all lanes, so the address is a
   // scalar and a lane's 32-bit offset.
+  template <bool kAgain = false>   // whether it is read again soon
   static __device__ __forceinline__ u4v load(const T* row, uint32_t first, uint32_t lane) {
-    const char* p = reinterpret_cast<const char*>(row) + static_cast<uint64_t>(first) * 16 + lane * 16;
-    return __builtin_nontemporal_load(reinterpret_cast<const u4v_unaligned*>(p));
+    const auto* p = reinterpret_cast<const u4v_unaligned*>(at(row, first, lane));
+    if constexpr (kAgain) return *p;
+    return __builtin_nontemporal_load(p);
   }
   static __device__ __forceinline__ void store(T* row, uint32_t first, uint32_t lane, u4v v) {
-    char* p = reinterpret_cast<char*>(row) + static_cast<uint64_t>(first) * 16 + lane * 16;
-    __builtin_nontemporal_store(v, reinterpret_cast<u4v_unaligned*>(p));
+    __builtin_nontemporal_store(v, reinterpret_cast<u4v_unaligned*>(const_cast<char*>(at(row, first, lane))));
+  }
+  static __device__ __forceinline__ const char* at(const T* row, uint32_t first, uint32_t lane) {
+    return reinterpret_cast<const char*>(row) + static_cast<uint64_t>(first) * 16 + lane * 16;
   }
   static __device__ __forceinline__ Floats floats(u4v v) {
     return __builtin_convertvector(__builtin_bit_cast(Packed, v), Floats);
@@ -45,9 +54,19 @@ struct Vec {
   static __device__ __forceinline__ u4v packed(Floats f) {
     return __builtin_bit_cast(u4v, __builtin_convertvector(f, Packed));
   }
+  // One value as it lies in memory, and as a number: apart, so that nothing waits for the load.
+  static __device__ __forceinline__ uint32_t raw(const T* p) {
+    if constexpr (sizeof(T) == 4) return *reinterpret_cast<const uint32_t*>(p);
+    return *reinterpret_cast<const uint16_t*>(p);
+  }
+  static __device__ __forceinline__ float value(uint32_t raw) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(raw);
+    else return static_cast<float>(__builtin_bit_cast(T, static_cast<uint16_t>(raw)));
+  }
+  static constexpr uint32_t kRawNone = sizeof(T) == 4 ? 0xFF800000u : std::is_same_v<T, __bf16> ? 0xFF80u : 0xFC00u;
   // A vector of -inf: counts for nothing in a maximum or a sum.
   static __device__ __forceinline__ u4v none() {
-    const uint32_t bits = sizeof(T) == 4 ? 0xFF800000u : std::is_same_v<T, __bf16> ? 0xFF80FF80u : 0xFC00FC00u;
+    constexpr uint32_t bits = sizeof(T) == 4 ? kRawNone : kRawNone * 0x10001u;
     return u4v{bits, bits, bits, bits};
   }
 };
@@ -65,7 +84,7 @@ struct Stat {
 __device__ __forceinline__ float finite_top(float top) { return top == -INFINITY ? 0.f : top; }
 
 template <class T, int U>
-__device__ __forceinline__ void add_few(Stat& s, const u4v* h) {
+__device__ __forceinline__ void add_vectors(Stat& s, const u4v (&h)[U]) {
   constexpr int kN = Vec<T>::kN;
   float top = s.top;
 #pragma unroll
@@ -88,15 +107,6 @@ __device__ __forceinline__ void add_few(Stat& s, const u4v* h) {
     sum += f[0];
   }
   s = {top, sum};
-}
-
-// U vectors, four at a time: their 32 values are all that is unpacked at once.
-template <class T, int U>
-__device__ __forceinline__ void add_vectors(Stat& s, const u4v (&h)[U]) {
-  constexpr int kFew = U < 4 ? U : 4;
-  static_assert(U % kFew == 0, "whole groups");
-#pragma unroll
-  for (int i = 0; i < U; i += kFew) add_few<T, kFew>(s, h + i);
 }
 
 __device__ __forceinline__ void add_value(Stat& s, float v) {
@@ -122,22 +132,22 @@ __device__ __forceinline__ Stat join_lanes(Stat s) {
   return {top, lane_group_sum<LANES>(s.sum * exp2_fast((s.top - finite_top(top)) * kLog2E))};
 }
 
-// A group of LANES lanes and its row: block `group` of the launch holds kRows of them.
+// Groups of LANES lanes, kRows of them to a block, and their rows.
 template <int LANES>
 struct Place {
   static constexpr int kThreads = LANES < kBlock ? kBlock : LANES;
   static constexpr int kRows = kThreads / LANES;
   __device__ static uint32_t lane() { return threadIdx.x % LANES; }
-  __device__ static int64_t row(int64_t group) {
-    if constexpr (LANES >= kThreads) return group;
+  __device__ static int64_t row(int64_t block) {
+    if constexpr (LANES >= kThreads) return block;
     uint32_t r = threadIdx.x / LANES;
     if constexpr (LANES >= kWave) r = __builtin_amdgcn_readfirstlane(r);
-    return group * kRows + r;
+    return block * kRows + r;
   }
-  static int64_t groups(int64_t rows) { return (rows + kRows - 1) / kRows; }
+  static int64_t blocks(int64_t rows) { return (rows + kRows - 1) / kRows; }
 };
 
-// Grids of up to 2^31 groups (of one dimension, HIP takes fewer threads than that needs).
+// Grids of up to 2^31 blocks (of one dimension, HIP takes fewer threads than that needs).
 constexpr int64_t kGridX = 1 << 20, kGridYZ = 65535;
 
 // What the policy loss reads of a row besides its logits.
@@ -179,201 +189,481 @@ struct RowGradient {
   float g, scaled, top, shift;
   bool none;
 
-  __device__ RowGradient(float g_, float top_, float log_sum)
+  __device__ __forceinline__ RowGradient(float g_, float top_, float log_sum)
       : g(g_), scaled(-g_ * 0x1p-24f), top(top_), shift(24.f - log_sum * kLog2E),
         none(g_ == 0.f || (top_ == -INFINITY && log_sum == 0.f)) {}
 
-  __device__ __forceinline__ float of(float z) const {
-    return scaled * exp2_fast(__builtin_fmaf(z - top, kLog2E, shift));
+  __device__ __forceinline__ float of(float z, bool target) const {
+    const float v = scaled * exp2_fast(__builtin_fmaf(z - top, kLog2E, shift));
+    return target ? v + g : v;
   }
-  // Gradient of the vector that starts at column `first`.
-  __device__ __forceinline__ u4v of_vector(u4v z, uint32_t y_in_vector) const {
+  // Gradient of a vector, as if the target were in none.
+  __device__ __forceinline__ u4v of_vector(u4v z) const {
     constexpr uint32_t kN = Vec<T>::kN;
+    if (none) return u4v{0, 0, 0, 0};
     auto f = Vec<T>::floats(z);
 #pragma unroll
-    for (uint32_t k = 0; k < kN; ++k) f[k] = of(f[k]);
-    if (y_in_vector < kN) {
-#pragma unroll
-      for (uint32_t k = 0; k < kN; ++k) f[k] += k == y_in_vector ? g : 0.f;
-    }
+    for (uint32_t k = 0; k < kN; ++k) f[k] = of(f[k], false);
     return Vec<T>::packed(f);
   }
 };
 
-// kForward and kPolicy.  The policy loss holds a lane's first HOLD vectors in registers from
-// the sum to the gradient, so rows of up to LANES * HOLD vectors are read once; of longer ones
-// the rest is read again.  Forward alone goes through the row HOLD vectors at a time.
-template <class T, RowMode kMode, int LANES, int HOLD, bool kLonger>
-__global__ __launch_bounds__(Place<LANES>::kThreads)
-void row_kernel(LogitsArgs a) {
-  constexpr int kN = Vec<T>::kN, kWaves = LANES / kWave, kMore = HOLD < 4 ? HOLD : 4;
+// The row's log-probability from its joined maximum and sum.
+__device__ __forceinline__ float row_logprob(Stat s, float target_logit, float* log_sum) {
+  if (s.top == -INFINITY && s.sum == 0.f) return -INFINITY;
+  *log_sum = kLn2 * log2f(s.sum);
+  return (target_logit - s.top) - *log_sum;
+}
+
+__device__ __forceinline__ void write_forward(const LogitsArgs& a, int64_t row, float lp, float top, float log_sum) {
+  a.logprobs[row] = lp;
+  if (a.stats) {
+    a.stats[2 * row] = top;
+    a.stats[2 * row + 1] = log_sum;
+  }
+  if (a.zero_grad) a.zero_grad[row] = 0.f;
+}
+
+// kForward and kPolicy for rows of at most LANES vectors, several to a wave.
+template <class T, RowMode kMode, int LANES>
+__global__ __launch_bounds__(kBlock)
+void short_row_kernel(LogitsArgs a) {
+  constexpr int kN = Vec<T>::kN;
   constexpr bool kPolicy = kMode == RowMode::kPolicy;
-  __shared__ Stat parts[kWaves > 1 ? kWaves : 1];
-  __shared__ float target_logit;
   const uint32_t lane = Place<LANES>::lane(), cols = static_cast<uint32_t>(a.cols);
   const uint32_t full = cols / kN, rem = cols % kN;
   const int64_t row = Place<LANES>::row(static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x);
-  if (row < a.rows) {
-    const T* z = static_cast<const T*>(a.logits) + row * a.stride;
-    const int32_t y = a.targets[row];
-    PolicyRow pr{};
-    if constexpr (kPolicy) pr = policy_row(a, row);
-    const bool counts = y >= 0 && y < a.cols && !(kPolicy && pr.weight == 0.f);
-    u4v held[HOLD];
-    float tail = -INFINITY, lp = 0.f, loss = 0.f, g = 0.f, log_sum = 0.f;
-    Stat s{-INFINITY, 0.f};
-    if (counts) {
-#pragma unroll
-      for (int i = 0; i < HOLD; ++i) {
-        const uint32_t first = i * LANES;
-        held[i] = first + lane < full ? Vec<T>::load(z, first, lane) : Vec<T>::none();
-      }
-      if (lane < rem) tail = static_cast<float>(z[full * kN + lane]);
-      float zy = kWaves > 1 && threadIdx.x != 0 ? 0.f : static_cast<float>(z[y]);
-      add_vectors<T>(s, held);
-      if constexpr (kLonger) {
-        for (uint32_t v0 = HOLD * LANES; v0 < full; v0 += kMore * LANES) {
-          u4v more[kMore];
-#pragma unroll
-          for (int i = 0; i < kMore; ++i) {
-            const uint32_t first = v0 + i * LANES;
-            more[i] = first + lane < full ? Vec<T>::load(z, first, lane) : Vec<T>::none();
-          }
-          add_vectors<T>(s, more);
-        }
-      }
-      if (lane < rem) add_value(s, tail);
-      s = join_lanes<(LANES < kWave ? LANES : kWave)>(s);
-      if constexpr (kWaves > 1) {
-        // The target's logit is read by one wave, before the others can write over it.
-        if (threadIdx.x % kWave == 0) parts[threadIdx.x / kWave] = s;
-        if (threadIdx.x == 0) target_logit = zy;
-        __syncthreads();
-        s = join_lanes<(kWaves > 1 ? kWaves : 1)>(parts[threadIdx.x % kWaves]);
-        zy = target_logit;
-      }
-      if (s.top == -INFINITY && s.sum == 0.f) {
-        lp = -INFINITY;
-      } else {
-        log_sum = kLn2 * log2f(s.sum);
-        lp = (zy - s.top) - log_sum;
-      }
-      if constexpr (kPolicy) g = policy_slope(a, pr, lp, &loss);
-    }
+  if (row >= a.rows) return;
+  const T* z = static_cast<const T*>(a.logits) + row * a.stride;
+  const int32_t y = a.targets[row];
+  PolicyRow pr{};
+  if constexpr (kPolicy) pr = policy_row(a, row);
+  const bool counts = y >= 0 && y < a.cols && !(kPolicy && pr.weight == 0.f);
+  u4v held[1] = {Vec<T>::none()};
+  float tail = -INFINITY, target_logit = 0.f, lp = 0.f, loss = 0.f, g = 0.f, log_sum = 0.f;
+  Stat s{-INFINITY, 0.f};
+  if (counts) {
+    if (lane < full) held[0] = Vec<T>::load(z, 0, lane);
+    if (lane < rem) tail = static_cast<float>(z[full * kN + lane]);
+    target_logit = static_cast<float>(z[y]);
+    add_vectors<T>(s, held);
+    if (lane < rem) add_value(s, tail);
+    s = join_lanes<LANES>(s);
+    lp = row_logprob(s, target_logit, &log_sum);
+    if constexpr (kPolicy) g = policy_slope(a, pr, lp, &loss);
+  }
+  if constexpr (!kPolicy) {
+    if (lane == 0) write_forward(a, row, lp, counts ? s.top : 0.f, log_sum);
+  } else {
     if (lane == 0) {
       a.logprobs[row] = lp;
-      if constexpr (kPolicy) a.loss[row] = loss;
-      if (kMode == RowMode::kForward && a.stats) {
-        a.stats[2 * row] = counts ? s.top : 0.f;
-        a.stats[2 * row + 1] = log_sum;
-      }
-      if (kMode == RowMode::kForward && a.zero_grad) a.zero_grad[row] = 0.f;
+      a.loss[row] = loss;
     }
-    if constexpr (kPolicy) {
-      if (a.dlogits == nullptr) return;
-      T* dz = static_cast<T*>(a.dlogits) + row * a.out_stride;
-      const RowGradient<T> grad(g, s.top, log_sum);
-      const uint32_t yv = static_cast<uint32_t>(y);
-#pragma unroll
-      for (int i = 0; i < HOLD; ++i) {
-        const uint32_t first = i * LANES;
-        asm("" : "+v"(held[i]));   // unpacked anew: twice the registers would go to its values
-        if (first + lane < full)
-          Vec<T>::store(dz, first, lane, grad.none ? u4v{0, 0, 0, 0} : grad.of_vector(held[i], yv - (first + lane) * kN));
-      }
-      if constexpr (kLonger)
-        for (uint32_t first = HOLD * LANES; first < full; first += LANES)
-          if (first + lane < full)
-            Vec<T>::store(dz, first, lane, grad.none ? u4v{0, 0, 0, 0}
-                                                     : grad.of_vector(Vec<T>::load(z, first, lane), yv - (first + lane) * kN));
-      if (lane < rem) {
-        const uint32_t j = full * kN + lane;
-        dz[j] = static_cast<T>(grad.none ? 0.f : grad.of(tail) + (j == yv ? g : 0.f));
-      }
+    if (a.dlogits == nullptr) return;
+    T* dz = static_cast<T*>(a.dlogits) + row * a.out_stride;
+    const RowGradient<T> grad(g, s.top, log_sum);
+    const uint32_t yv = static_cast<uint32_t>(y);
+    if (lane < full) Vec<T>::store(dz, 0, lane, grad.of_vector(held[0]));
+    if (lane < full && lane == yv / kN && !grad.none) dz[yv] = static_cast<T>(grad.of(target_logit, true));
+    if (lane < rem) {
+      const uint32_t j = full * kN + lane;
+      dz[j] = static_cast<T>(grad.none ? 0.f : grad.of(tail, j == yv));
     }
   }
+}
+
+// The whole vectors of a long row.  The values left over, 1 to kN of them, go to a lane each, so that
+// the vectors of a shifted row, too, end within it.
+template <class T>
+__device__ __forceinline__ uint32_t long_row_vectors(uint32_t cols) { return (cols - 1) / Vec<T>::kN; }
+
+// A long row as a wave sees it: a run of neighbouring vectors, `whole` times 64 and `part` more.
+//
+// Loads are issued by all lanes at all times (past the run's end the last vector stands in), so
+// that the number in flight is known where one is waited for, and the sum starts when the first
+// vectors have come.
+//
+// Values of 16 bits may start at an address that is no multiple of 4, where a load of 16 bytes
+// takes longer (rows of 131,071 bf16 logits: 412 us where aligned ones take 320).  The run is then
+// loaded from the second value on, and `values` puts the vectors together that the row has when
+// counted from its first value, from two lanes' loads each.
+template <class T>
+struct WaveRun {
+  static constexpr uint32_t kN = Vec<T>::kN;
+  uint32_t lane, begin, whole, part;
+  uint32_t last;                // the last vector, counted from the one that z points to
+  uint32_t odd;                 // 1 where shifted
+  const T* z;                   // the run's first vector as it is loaded; of an empty run the row's last
+
+  // Up to `most` vectors from number `first` on of the row's `full` ones (at least one).
+  __device__ __forceinline__ WaveRun(const T* row, uint32_t full, uint32_t first, uint32_t most) {
+    lane = threadIdx.x % kWave;
+    begin = first < full ? first : full - 1;
+    const uint32_t count = first < full ? (full - begin < most ? full - begin : most) : 0;
+    whole = count / kWave;
+    part = count % kWave;
+    last = count > 0 ? count - 1 : 0;
+    odd = sizeof(T) == 2 ? static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row) >> 1) & 1 : 0;
+    z = row + odd + static_cast<uint64_t>(begin) * kN;
+  }
+  __device__ __forceinline__ bool any(uint32_t i) const { return i < whole || (i == whole && part > 0); }
+  __device__ __forceinline__ uint32_t vector(uint32_t i) const {
+    const uint32_t v = i * kWave + lane;
+    return v < last ? v : last;
+  }
+  template <bool kAgain = false>
+  __device__ __forceinline__ u4v load(uint32_t i) const { return Vec<T>::template load<kAgain>(z, 0, vector(i)); }
+  // From memory to LDS without a wait, lane by lane.
+  __device__ __forceinline__ void load_to_lds(uint32_t i, u4v* to) const {
+    const char* from = Vec<T>::at(z, 0, vector(i));
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)from,
+                                     (__attribute__((address_space(3))) uint32_t*)to, 16, 0, 0);
+  }
+  // The value before the run's first loaded one, raw, in lane 0 of a shifted row; 16 bits higher it
+  // is the carry that `values` starts from.
+  __device__ __forceinline__ uint32_t before() const { return sizeof(T) == 2 ? Vec<T>::raw(z - (lane == 0 ? odd : 0)) : 0; }
+
+  // The row's vector, counted from its first value, out of what was loaded.
+  __device__ __forceinline__ u4v values(u4v h, uint32_t& carry) const {
+    if (sizeof(T) == 4 || !odd) return h;
+    // Lane 0 takes `carry`, the others the lane below's last value (DPP wave shift by one).
+    const uint32_t below = __builtin_amdgcn_update_dpp(static_cast<int>(carry), static_cast<int>(h[3]), 0x138, 0xF, 0xF, false);
+    carry = __builtin_amdgcn_readlane(static_cast<int>(h[3]), kWave - 1);
+    return u4v{__builtin_amdgcn_alignbit(h[0], below, 16), __builtin_amdgcn_alignbit(h[1], h[0], 16),
+               __builtin_amdgcn_alignbit(h[2], h[1], 16), __builtin_amdgcn_alignbit(h[3], h[2], 16)};
+  }
+  // Maximum and sum of the vectors i0 .. i0 + N - 1, as loaded.
+  template <int N>
+  __device__ __forceinline__ void add(Stat& s, uint32_t i0, const u4v* loaded, uint32_t& carry) const {
+    if (!any(i0)) return;
+    u4v h[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) h[k] = values(loaded[k], carry);
+    if (i0 + N > whole) {
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (!(i0 + k < whole || (i0 + k == whole && lane < part))) h[k] = Vec<T>::none();
+    }
+    add_vectors<T>(s, h);
+  }
+  // Gradient of vector i, as loaded, to the row at dz.
+  __device__ __forceinline__ void store(T* dz, const RowGradient<T>& grad, uint32_t i, u4v v) const {
+    if (!any(i)) return;
+    T* out = dz + odd + static_cast<uint64_t>(begin) * kN;
+    const u4v d = grad.of_vector(v);
+    if (i < whole) Vec<T>::store(out, i * kWave, lane, d);
+    else if (lane < part) Vec<T>::store(out, i * kWave, lane, d);
+  }
+  // The target's gradient, by the lane that stored its vector.
+  __device__ __forceinline__ void store_target(T* dz, const RowGradient<T>& grad, uint32_t y, float target_logit) const {
+    const uint32_t v = (y - odd) / kN - begin;    // of y = 0 in a shifted row: past any run
+    if (!grad.none && v < whole * kWave + part && v % kWave == lane) dz[y] = static_cast<T>(grad.of(target_logit, true));
+  }
+};
+
+// Waves' parts of a row.
+template <int WAVES>
+struct RowParts {
+  Stat stat[WAVES];
+  float target_logit;
+};
+
+// kForward for long rows: a block (or, with WAVES = 1, a wave) per row, U vectors in flight per lane.
+template <class T, int WAVES, int U>
+__global__ __launch_bounds__(Place<WAVES * kWave>::kThreads)
+void long_forward_kernel(LogitsArgs a) {
+  constexpr int kN = Vec<T>::kN, LANES = WAVES * kWave;
+  __shared__ RowParts<WAVES> parts;
+  const int64_t row = Place<LANES>::row(static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x);
+  if (row >= a.rows) return;
+  const uint32_t tid = Place<LANES>::lane(), cols = static_cast<uint32_t>(a.cols);
+  const T* z = static_cast<const T*>(a.logits) + row * a.stride;
+  const uint32_t full = long_row_vectors<T>(cols), rem = cols - full * kN;
+  const int32_t y = __builtin_amdgcn_readfirstlane(a.targets[row]);
+  const bool counts = y >= 0 && y < a.cols;
+  float lp = 0.f, log_sum = 0.f;
+  Stat s{-INFINITY, 0.f};
+  if (counts) {
+    const uint32_t target = Vec<T>::raw(z + y);
+    const uint32_t tail = Vec<T>::raw(z + full * kN + (tid < rem ? tid : rem - 1));
+    // The waves' runs of U vectors per lane side by side: the block reads neighbouring memory.
+    for (uint32_t first = __builtin_amdgcn_readfirstlane(tid / kWave) * (kWave * U); first < full; first += LANES * U) {
+      const WaveRun<T> run(z, full, first, kWave * U);
+      const uint32_t before = run.before();
+      u4v h[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) h[i] = run.load(i);
+      uint32_t carry = before << 16;
+      run.template add<U>(s, 0, h, carry);
+    }
+    if (tid < rem) add_value(s, Vec<T>::value(tail));
+    s = join_lanes<kWave>(s);
+    if constexpr (WAVES > 1) {
+      if (tid % kWave == 0) parts.stat[tid / kWave] = s;
+      __syncthreads();
+      s = join_lanes<WAVES>(parts.stat[tid % WAVES]);
+    }
+    lp = row_logprob(s, Vec<T>::value(target), &log_sum);
+  }
+  if (tid == 0) write_forward(a, row, lp, counts ? s.top : 0.f, log_sum);
+}
+
+// The same value in all lanes, to a scalar register.
+__device__ __forceinline__ float uniform(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
+__device__ __forceinline__ int32_t uniform(int32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// What a row's turn in the policy loss starts from, besides its vectors.
+template <class T>
+struct PolicyTurn {
+  PolicyRow row;
+  int32_t y;
+
+  __device__ __forceinline__ void read(const LogitsArgs& a, int64_t r) {
+    y = a.targets[r];
+    row = policy_row(a, r);
+  }
+  __device__ __forceinline__ void make_uniform() {
+    y = uniform(y);
+    row = {uniform(row.advantage), uniform(row.old_logprob), uniform(row.ref_logprob), uniform(row.weight)};
+  }
+  __device__ __forceinline__ bool counts(const LogitsArgs& a) const {
+    return uniform(static_cast<int32_t>(y >= 0 && y < a.cols && row.weight != 0.f)) != 0;
+  }
+};
+
+// This lane's part of a row's values outside of its vectors, and their gradient.
+template <class T>
+struct RowEnds {
+  uint32_t tail;   // value full * kN + tid, of the first rem lanes (the others: the row's last)
+  uint32_t head;   // lane 0 of the first wave, shifted rows: the first value
+
+  __device__ __forceinline__ void load(const WaveRun<T>& run, const T* z, uint32_t full, uint32_t tid, uint32_t rem) {
+    tail = Vec<T>::raw(z + full * Vec<T>::kN + (tid < rem ? tid : rem - 1));
+    head = run.before();
+  }
+  __device__ __forceinline__ void store(T* dz, const RowGradient<T>& grad, uint32_t full, uint32_t odd, uint32_t tid,
+                                        uint32_t rem, uint32_t y) const {
+    if (tid < rem && !(odd && tid == 0)) {   // a shifted row's vectors go one value further
+      const uint32_t j = full * Vec<T>::kN + tid;
+      dz[j] = static_cast<T>(grad.none ? 0.f : grad.of(Vec<T>::value(tail), j == y));
+    }
+    if (odd && tid == 0) dz[0] = static_cast<T>(grad.none ? 0.f : grad.of(Vec<T>::value(head), y == 0));
+  }
+};
+
+// A row's loss and gradient factor from the lanes' maxima and sums; one lane writes the loss.
+template <class T, int WAVES>
+__device__ __forceinline__ RowGradient<T> finish_policy_row(const LogitsArgs& a, int64_t row, const PolicyTurn<T>& turn, bool counts,
+                                                            Stat s, float target_logit, RowParts<WAVES>& parts, uint32_t tid) {
+  float lp = 0.f, loss = 0.f, g = 0.f, log_sum = 0.f;
+  if (counts) {
+    s = join_lanes<kWave>(s);
+    if constexpr (WAVES > 1) {
+      // One wave reads the target's logit, before the others can write over it in place.
+      if (tid % kWave == 0) parts.stat[tid / kWave] = s;
+      if (tid == 0) parts.target_logit = target_logit;
+      __syncthreads();
+      s = join_lanes<WAVES>(parts.stat[tid % WAVES]);
+      target_logit = parts.target_logit;
+    }
+    lp = row_logprob(s, target_logit, &log_sum);
+    g = policy_slope(a, turn.row, lp, &loss);
+  }
+  if (tid == 0) {
+    a.logprobs[row] = lp;
+    a.loss[row] = loss;
+  }
+  return RowGradient<T>(uniform(g), uniform(s.top), uniform(log_sum));
+}
+
+// kPolicy for long rows: a block (or, with WAVES = 1, a wave) per row.  Two blocks or more share a
+// CU, so that one's loads and stores go on while another computes.  From the sum to the gradient a
+// lane keeps its first HOLD vectors in registers and the next STAGE in LDS, where they are loaded
+// without passing through registers; the rest of a row that is longer still is read again.
+template <class T, int WAVES, int HOLD, int STAGE>
+__global__ __launch_bounds__(Place<WAVES * kWave>::kThreads)
+void long_policy_kernel(LogitsArgs a) {
+  constexpr int kN = Vec<T>::kN, LANES = WAVES * kWave;
+  // Vectors unpacked at once: with LDS in use as well, fewer, to stay within 128 registers.
+  constexpr int kFew = STAGE > 0 ? 16 / kN : HOLD % 4 == 0 ? 4 : HOLD % 3 == 0 ? 3 : HOLD % 2 == 0 ? 2 : 1;
+  __shared__ RowParts<WAVES> parts;
+  __shared__ u4v stage[STAGE > 0 ? WAVES * STAGE * kWave : 1];
+  const int64_t row = Place<LANES>::row(static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x);
+  if (row >= a.rows) return;
+  const uint32_t tid = Place<LANES>::lane(), cols = static_cast<uint32_t>(a.cols);
+  const uint32_t full = long_row_vectors<T>(cols), rem = cols - full * kN, wave = uniform(static_cast<int32_t>(tid / kWave));
+  const uint32_t per = (full + LANES - 1) / LANES * kWave;
+  const T* z = static_cast<const T*>(a.logits) + row * a.stride;
+  const WaveRun<T> run(z, full, wave * per, per);
+  PolicyTurn<T> turn;
+  turn.read(a, row);
+  turn.make_uniform();
+  const bool counts = turn.counts(a);
+  u4v held[HOLD];
+  u4v* mine = stage + wave * (STAGE * kWave);
+  RowEnds<T> ends;
+  uint32_t target = 0;
+  Stat s{-INFINITY, 0.f};
+  if (counts) {
+    target = Vec<T>::raw(z + turn.y);
+    ends.load(run, z, full, tid, rem);
+#pragma unroll
+    for (int i = 0; i < HOLD; ++i) held[i] = run.load(i);
+    if constexpr (STAGE > 0) {
+#pragma unroll
+      for (int i = 0; i < STAGE; ++i) run.load_to_lds(HOLD + i, mine + i * kWave);
+    }
+    uint32_t carry = ends.head << 16;
+#pragma unroll
+    for (int i = 0; i < HOLD; i += kFew) run.template add<kFew>(s, i, held + i, carry);
+    if constexpr (STAGE > 0) {
+      constexpr int kThree = 3;
+      static_assert(STAGE % kThree == 0, "whole groups");
+      for (int i = 0; i < STAGE; i += kThree) {
+        u4v h[kThree];
+#pragma unroll
+        for (int k = 0; k < kThree; ++k) h[k] = mine[(i + k) * kWave + run.lane];
+        run.template add<kThree>(s, HOLD + i, h, carry);
+      }
+      for (uint32_t i = HOLD + STAGE; run.any(i); i += kFew) {
+        u4v h[kFew];
+#pragma unroll
+        for (int k = 0; k < kFew; ++k) h[k] = run.template load<true>(i + k);
+        run.template add<kFew>(s, i, h, carry);
+      }
+    }
+    if (tid < rem) add_value(s, Vec<T>::value(ends.tail));
+  }
+  const RowGradient<T> grad = finish_policy_row<T, WAVES>(a, row, turn, counts, s, Vec<T>::value(target), parts, tid);
+  if (a.dlogits == nullptr) return;
+  T* dz = static_cast<T*>(a.dlogits) + row * a.out_stride;
+  const uint32_t y = static_cast<uint32_t>(turn.y);
+  constexpr int kMore = STAGE > 0 ? 4 : 1;
+  u4v more[kMore];   // what is read again: on its way while the rest is stored
+  auto load_more = [&](uint32_t i) {
+    if (grad.none || !run.any(i)) return;
+#pragma unroll
+    for (int k = 0; k < kMore; ++k) more[k] = run.load(i + k);
+  };
+  if constexpr (STAGE > 0) load_more(HOLD + STAGE);
+#pragma unroll
+  for (int i = 0; i < HOLD; ++i) {
+    asm("" : "+v"(held[i]));   // unpacked anew: twice the registers would go to its values
+    run.store(dz, grad, i, held[i]);
+  }
+  if constexpr (STAGE > 0) {
+#pragma unroll 1
+    for (int i = 0; i < STAGE; ++i) run.store(dz, grad, HOLD + i, mine[i * kWave + run.lane]);
+    for (uint32_t i = HOLD + STAGE; run.any(i); i += kMore) {
+#pragma unroll
+      for (int k = 0; k < kMore; ++k) run.store(dz, grad, i + k, more[k]);
+      load_more(i + kMore);
+    }
+  }
+  run.store_target(dz, grad, y, Vec<T>::value(target));
+  ends.store(dz, grad, full, run.odd, tid, rem, y);
 }
 
 // kBackward: every value by itself.  A group of LANES lanes takes LANES * U vectors of a row;
-// the runs of a longer row go to different blocks.
+// the runs of a longer row go to different blocks.  Rows of 16-bit values that start at no multiple
+// of 4 bytes are taken from their second value on.
 template <class T, int LANES, int U>
 __global__ __launch_bounds__(Place<LANES>::kThreads)
 void gradient_kernel(LogitsArgs a) {
-  constexpr int kN = Vec<T>::kN;
-  const uint32_t lane = Place<LANES>::lane(), cols = static_cast<uint32_t>(a.cols);
-  const uint32_t full = cols / kN, rem = cols % kN;
+  constexpr uint32_t kN = Vec<T>::kN;
   const int64_t row = Place<LANES>::row(static_cast<int64_t>(blockIdx.z) * gridDim.y + blockIdx.y);
   if (row >= a.rows) return;
+  const T* z = static_cast<const T*>(a.logits) + row * a.stride;
+  T* dz = static_cast<T*>(a.dlogits) + row * a.out_stride;
+  const uint32_t odd = sizeof(T) == 2 ? static_cast<uint32_t>(reinterpret_cast<uintptr_t>(z) >> 1) & 1 : 0;
+  const uint32_t lane = Place<LANES>::lane(), cols = static_cast<uint32_t>(a.cols);
+  const uint32_t full = (cols - odd) / kN, rem = cols - odd - full * kN, v0 = blockIdx.x * (LANES * U);
   const int32_t y = a.targets[row];
   const float g = a.grad[row], top = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
   const RowGradient<T> grad(y >= 0 && y < a.cols ? g : 0.f, top, log_sum);
-  const uint32_t yv = static_cast<uint32_t>(y);
-  const T* z = static_cast<const T*>(a.logits) + row * a.stride;
-  T* dz = static_cast<T*>(a.dlogits) + row * a.out_stride;
-  const uint32_t v0 = blockIdx.x * (LANES * U);
+  // Columns outside of the vectors: up to kN - 1 at the end, one at the start of a shifted row.
+  const uint32_t yv = static_cast<uint32_t>(y), last = cols - rem + lane;
+  const bool has_tail = blockIdx.x == gridDim.x - 1 && lane < rem, has_head = blockIdx.x == 0 && lane < odd;
   if (grad.none) {
 #pragma unroll
     for (int i = 0; i < U; ++i)
-      if (v0 + i * LANES + lane < full) Vec<T>::store(dz, v0 + i * LANES, lane, u4v{0, 0, 0, 0});
-  } else {
-    u4v h[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      h[i] = u4v{0, 0, 0, 0};
-      if (v0 + i * LANES + lane < full) h[i] = Vec<T>::load(z, v0 + i * LANES, lane);
-    }
-#pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const uint32_t first = v0 + i * LANES;
-      if (first + lane < full) Vec<T>::store(dz, first, lane, grad.of_vector(h[i], yv - (first + lane) * kN));
-    }
+      if (v0 + i * LANES + lane < full) Vec<T>::store(dz + odd, v0 + i * LANES, lane, u4v{0, 0, 0, 0});
+    if (has_tail) dz[last] = static_cast<T>(0.f);
+    if (has_head) dz[0] = static_cast<T>(0.f);
+    return;
   }
-  if (blockIdx.x == gridDim.x - 1 && lane < rem) {
-    const uint32_t j = full * kN + lane;
-    dz[j] = static_cast<T>(grad.none ? 0.f : grad.of(static_cast<float>(z[j])) + (j == yv ? grad.g : 0.f));
+  const uint32_t target = (yv - odd) / kN - v0;   // the target's vector, and whether this lane has it
+  const bool has_target = target < LANES * U && target + v0 < full && target % LANES == lane;
+  u4v h[U];
+  uint32_t z_target = 0, z_tail = 0, z_head = 0;
+#pragma unroll
+  for (int i = 0; i < U; ++i) {
+    h[i] = u4v{0, 0, 0, 0};
+    if (v0 + i * LANES + lane < full) h[i] = Vec<T>::load(z + odd, v0 + i * LANES, lane);
   }
+  if (has_target) z_target = Vec<T>::raw(z + yv);
+  if (has_tail) z_tail = Vec<T>::raw(z + last);
+  if (has_head) z_head = Vec<T>::raw(z);
+#pragma unroll
+  for (int i = 0; i < U; ++i)
+    if (v0 + i * LANES + lane < full) Vec<T>::store(dz + odd, v0 + i * LANES, lane, grad.of_vector(h[i]));
+  if (has_target) dz[yv] = static_cast<T>(grad.of(Vec<T>::value(z_target), true));
+  if (has_tail) dz[last] = static_cast<T>(grad.of(Vec<T>::value(z_tail), last == yv));
+  if (has_head) dz[0] = static_cast<T>(grad.of(Vec<T>::value(z_head), yv == 0));
 }
 
-template <class T, RowMode kMode, int LANES, int HOLD, bool kLonger = false>
-hipError_t launch_rows(const LogitsArgs& a, hipStream_t stream) {
-  const int64_t groups = Place<LANES>::groups(a.rows), x = std::min(groups, kGridX);
-  const dim3 grid(static_cast<uint32_t>(x), static_cast<uint32_t>((groups + x - 1) / x));
-  row_kernel<T, kMode, LANES, HOLD, kLonger><<<grid, Place<LANES>::kThreads, 0, stream>>>(a);
+// One block per kRows rows.
+template <int LANES, class Kernel>
+hipError_t launch_rows(Kernel kernel, const LogitsArgs& a, hipStream_t stream) {
+  const int64_t blocks = Place<LANES>::blocks(a.rows), x = std::min(blocks, kGridX);
+  const dim3 grid(static_cast<uint32_t>(x), static_cast<uint32_t>((blocks + x - 1) / x));
+  kernel<<<grid, Place<LANES>::kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 template <class T, int LANES, int U>
 hipError_t launch_gradient(const LogitsArgs& a, hipStream_t stream) {
   constexpr int64_t kRun = int64_t{LANES} * U;
-  const int64_t full = a.cols / Vec<T>::kN, groups = Place<LANES>::groups(a.rows), y = std::min(groups, kGridYZ);
+  const int64_t full = a.cols / Vec<T>::kN, blocks = Place<LANES>::blocks(a.rows), y = std::min(blocks, kGridYZ);
   const dim3 grid(static_cast<uint32_t>(std::max<int64_t>(1, (full + kRun - 1) / kRun)), static_cast<uint32_t>(y),
-                  static_cast<uint32_t>((groups + y - 1) / y));
+                  static_cast<uint32_t>((blocks + y - 1) / y));
   gradient_kernel<T, LANES, U><<<grid, Place<LANES>::kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
-// Lanes and vectors per lane by the row's whole vectors.
+// Lanes or waves and vectors per lane by the row's vectors.
 template <class T, RowMode kMode>
 hipError_t launch_by_row(const LogitsArgs& a, hipStream_t stream) {
   const int64_t full = a.cols / Vec<T>::kN;
   if constexpr (sizeof(T) == 4)
-    if (full <= 4) return launch_rows<T, kMode, 4, 1>(a, stream);
-  if (full <= 8) return launch_rows<T, kMode, 8, 1>(a, stream);
-  if (full <= 16) return launch_rows<T, kMode, 16, 1>(a, stream);
-  if (full <= 32) return launch_rows<T, kMode, 32, 1>(a, stream);
-  if (full <= 64) return launch_rows<T, kMode, 64, 1>(a, stream);
-  if (full <= 128) return launch_rows<T, kMode, 64, 2>(a, stream);
-  if (full <= 256) return launch_rows<T, kMode, 64, 4>(a, stream);
-  if (full <= 512) return launch_rows<T, kMode, 64, 8>(a, stream);
-  if (full <= 1024) return launch_rows<T, kMode, 256, 4>(a, stream);
+    if (full <= 4) return launch_rows<4>(short_row_kernel<T, kMode, 4>, a, stream);
+  if (full <= 8) return launch_rows<8>(short_row_kernel<T, kMode, 8>, a, stream);
+  if (full <= 16) return launch_rows<16>(short_row_kernel<T, kMode, 16>, a, stream);
+  if (full <= 32) return launch_rows<32>(short_row_kernel<T, kMode, 32>, a, stream);
   if constexpr (kMode == RowMode::kForward) {
-    return launch_rows<T, kMode, 1024, 4, true>(a, stream);
+    if (full <= 64) return launch_rows<64>(long_forward_kernel<T, 1, 1>, a, stream);
+    if (full <= 128) return launch_rows<64>(long_forward_kernel<T, 1, 2>, a, stream);
+    if (full <= 512) return launch_rows<64>(long_forward_kernel<T, 1, 4>, a, stream);
+    if (full <= 1024) return launch_rows<256>(long_forward_kernel<T, 4, 4>, a, stream);
+    return launch_rows<1024>(long_forward_kernel<T, 16, 4>, a, stream);
   } else {
-    if (full <= 2048) return launch_rows<T, kMode, 256, 8>(a, stream);
-    if (full <= 4096) return launch_rows<T, kMode, 512, 8>(a, stream);
-    if (full <= 8192) return launch_rows<T, kMode, 1024, 8>(a, stream);
-    if (full <= 16384) return launch_rows<T, kMode, 1024, 16>(a, stream);
-    return launch_rows<T, kMode, 1024, 16, true>(a, stream);
+    if (full <= 64) return launch_rows<64>(long_policy_kernel<T, 1, 1, 0>, a, stream);
+    if (full <= 128) return launch_rows<64>(long_policy_kernel<T, 1, 2, 0>, a, stream);
+    if (full <= 192) return launch_rows<64>(long_policy_kernel<T, 1, 3, 0>, a, stream);
+    if (full <= 256) return launch_rows<64>(long_policy_kernel<T, 1, 4, 0>, a, stream);
+    if (full <= 384) return launch_rows<64>(long_policy_kernel<T, 1, 6, 0>, a, stream);
+    if (full <= 512) return launch_rows<64>(long_policy_kernel<T, 1, 8, 0>, a, stream);
+    if (full <= 768) return launch_rows<256>(long_policy_kernel<T, 4, 3, 0>, a, stream);
+    if (full <= 1024) return launch_rows<256>(long_policy_kernel<T, 4, 4, 0>, a, stream);
+    if (full <= 1536) return launch_rows<256>(long_policy_kernel<T, 4, 6, 0>, a, stream);
+    if (full <= 2048) return launch_rows<256>(long_policy_kernel<T, 4, 8, 0>, a, stream);
+    if (full <= 3072) return launch_rows<512>(long_policy_kernel<T, 8, 6, 0>, a, stream);
+    if (full <= 4096) return launch_rows<512>(long_policy_kernel<T, 8, 8, 0>, a, stream);
+    if (full <= 5120) return launch_rows<512>(long_policy_kernel<T, 8, 10, 0>, a, stream);
+    if (full <= 6144) return launch_rows<512>(long_policy_kernel<T, 8, 12, 0>, a, stream);
+    if (full <= 7168) return launch_rows<512>(long_policy_kernel<T, 8, 14, 0>, a, stream);
+    if (full <= 8192) return launch_rows<512>(long_policy_kernel<T, 8, 16, 0>, a, stream);
+    return launch_rows<512>(long_policy_kernel<T, 8, 16, 9>, a, stream);
   }
 }
 
