@@ -19,7 +19,7 @@ constexpr uint64_t kGamma = 0x9E3779B97F4A7C15ull;
 constexpr int64_t kGridYZ = 65535;
 
 typedef uint32_t u4v __attribute__((ext_vector_type(4)));
-typedef u4v u4v_unaligned __attribute__((aligned(2)));
+typedef u4v u4v_unaligned __attribute__((aligned(2), may_alias));
 
 __device__ __forceinline__ uint64_t mix64(uint64_t z) {
   z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
