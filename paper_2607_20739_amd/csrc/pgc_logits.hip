@@ -203,20 +203,23 @@ __device__ __forceinline__ float policy_slope(const LogitsArgs& a, const PolicyR
   return slope * a.scale * r.weight;
 }
 
-// A row's gradient g (onehot(y) - exp(z - top - log_sum)), value by value.  The exponential is
-// taken 2^24 times larger and g as much smaller, so that what lies below 2^-126 is not lost
-// before the product.
+// A row's gradient g (onehot(y) - exp(z - top) / sum), value by value.  The exponential is taken 8
+// times larger, which costs near the maximum no more than its own rounding, so that for |g| up
+// to 8 nothing is lost that 32 bits hold.
 template <class T>
 struct RowGradient {
-  float g, scaled, top, shift;
-  bool none;
+  float g, scaled, top;
+  bool none;   // zeros: no gradient comes in, or nothing can occur
 
-  __device__ __forceinline__ RowGradient(float g_, float top_, float log_sum)
-      : g(g_), scaled(-g_ * 0x1p-24f), top(top_), shift(24.f - log_sum * kLog2E),
-        none(g_ == 0.f || (top_ == -INFINITY && log_sum == 0.f)) {}
+  __device__ __forceinline__ RowGradient(float g_, float top_, float inverse_sum, bool empty)
+      : g(g_), scaled(-g_ * inverse_sum * 0.125f), top(top_), none(g_ == 0.f || empty) {}
+  // From the maximum and the log of the sum.
+  static __device__ __forceinline__ RowGradient of_stats(float g, float top, float log_sum) {
+    return RowGradient(g, top, expf(-log_sum), top == -INFINITY && log_sum == 0.f);
+  }
 
   __device__ __forceinline__ float of(float z, bool target) const {
-    const float v = scaled * exp2_fast(__builtin_fmaf(z - top, kLog2E, shift));
+    const float v = scaled * exp2_fast(__builtin_fmaf(z - top, kLog2E, 3.f));
     return target ? v + g : v;
   }
   // Gradient of a vector, as if the target were in none.
@@ -325,7 +328,8 @@ void short_row_kernel(LogitsArgs a) {
     if (a.dlogits == nullptr) return;
   }
   T* dz = static_cast<T*>(a.dlogits) + row * a.out_stride;
-  const RowGradient<T> grad(g, s.top, log_sum);
+  const RowGradient<T> grad = kPolicy ? RowGradient<T>(g, s.top, 1.f / s.sum, s.top == -INFINITY && s.sum == 0.f)
+                                      : RowGradient<T>::of_stats(g, s.top, log_sum);
   const uint32_t yv = static_cast<uint32_t>(y);
   if (cols < kN) {
     if (!there) return;
@@ -564,7 +568,7 @@ __device__ __forceinline__ RowGradient<T> finish_policy_row(const LogitsArgs& a,
     a.logprobs[row] = lp;
     a.loss[row] = loss;
   }
-  return RowGradient<T>(uniform(g), uniform(s.top), uniform(log_sum));
+  return RowGradient<T>(uniform(g), uniform(s.top), uniform(1.f / s.sum), uniform(s.top) == -INFINITY && uniform(s.sum) == 0.f);
 }
 
 // kPolicy for long rows: a block (or, with WAVES = 1, a wave) per row.  Two blocks or more share a
@@ -671,7 +675,7 @@ void gradient_kernel(LogitsArgs a) {
   const uint32_t full = (cols - odd) / kN, rem = cols - odd - full * kN, v0 = blockIdx.x * (LANES * U);
   const int32_t y = a.targets[row];
   const float g = a.grad[row], top = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
-  const RowGradient<T> grad(y >= 0 && y < a.cols ? g : 0.f, top, log_sum);
+  const RowGradient<T> grad = RowGradient<T>::of_stats(y >= 0 && y < a.cols ? g : 0.f, top, log_sum);
   // Columns outside of the vectors: up to kN - 1 at the end, one at the start of a shifted row.
   const uint32_t yv = static_cast<uint32_t>(y), last = cols - rem + lane;
   const bool has_tail = blockIdx.x == gridDim.x - 1 && lane < rem, has_head = blockIdx.x == 0 && lane < odd;

@@ -87,19 +87,22 @@ def _check(status):
 
 def _matrix(name, x, like=None):
     """Row stride of a 2-D GPU matrix; of `like`'s shape, type and GPU where given."""
-    if x.dim() != 2 or x.dtype not in _DTYPES or not x.is_cuda:
+    shape = x.shape
+    if like is not None:
+        if shape != like.shape or x.dtype != like.dtype or x.device != like.device:
+            raise ValueError("%s must have the shape, dtype and device %s, %s, %s"
+                             % (name, tuple(like.shape), like.dtype, like.device))
+    elif len(shape) != 2 or x.dtype not in _DTYPES or not x.is_cuda:
         raise ValueError("%s must be a 2-D float32, bfloat16 or float16 tensor on the GPU" % name)
-    if like is not None and (x.shape != like.shape or x.dtype != like.dtype or x.device != like.device):
-        raise ValueError("%s must have the shape, dtype and device %s, %s, %s"
-                         % (name, tuple(like.shape), like.dtype, like.device))
-    rows, cols = x.shape
-    if cols > 1 and x.stride(1) != 1:
+    rows, cols = shape
+    stride, step = x.stride()
+    if step != 1 and cols > 1:
         raise ValueError("the columns of %s must be adjacent" % name)
-    if rows > 1:
-        if x.stride(0) < cols:
-            raise ValueError("the rows of %s must not overlap" % name)
-        return x.stride(0)
-    return cols
+    if rows <= 1:
+        return cols
+    if stride < cols:
+        raise ValueError("the rows of %s must not overlap" % name)
+    return stride
 
 
 def _array(name, x, like, dtype, shape):
@@ -137,15 +140,11 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
 def _output(like, out):
     """The tensor that receives a result of `like`'s shape, and its row stride."""
     if out is None:
-        return like.new_empty(like.shape), like.shape[1]
+        return torch.empty_like(like, memory_format=torch.contiguous_format), like.shape[1]
     stride = _matrix("out", out, like)
     if not out.is_inference():
         torch.autograd.graph.increment_version(out)   # autograd notices a saved tensor that this changes
     return out, stride
-
-
-def _wants_grad(*tensors):
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
 
 
 # ---- dropout ----------------------------------------------------------------------------
@@ -170,7 +169,7 @@ def dropout(x, p, seed, residual=None, row_ids=None, first_row=0, out=None):
     first_row + i.  Use another seed for each step and layer (pgc_splitmix64(seed, t)).
     `out` may be x or residual (not under autograd).
     """
-    if _wants_grad(x, residual):
+    if torch.is_grad_enabled() and (x.requires_grad or residual is not None and residual.requires_grad):
         if out is not None:
             raise ValueError("out cannot be given where a gradient is asked for")
         return _Dropout.apply(x, residual, p, seed, row_ids, first_row)
@@ -195,7 +194,7 @@ def _logits(logits, targets):
 def token_logprobs(logits, targets):
     """(logprobs [rows], stats [rows, 2]): each row's log-probability of its target, and its maximum
     and the log of its sum of exp(z - maximum), which the backward pass takes."""
-    if _wants_grad(logits):
+    if torch.is_grad_enabled() and logits.requires_grad:
         return _TokenLogprobs.apply(logits, targets)
     return _token_logprobs(logits, targets)
 
