@@ -123,7 +123,7 @@ __device__ __forceinline__ void drop_value(const DropoutArgs& a, uint64_t key, c
 // other, so that no lane is without one and neighbouring lanes have neighbouring memory.  The rows'
 // keys are drawn once, into LDS.  A row's last vector, where it is not whole, is loaded from the row's
 // last 16 bytes, moved into place, and stored in up to three pieces.
-constexpr uint32_t kShortVectors = 128;
+constexpr uint32_t kShortVectors = 512;
 template <class T, bool kResidual, int U>
 __global__ __launch_bounds__(kThreads)
 void short_dropout_kernel(DropoutArgs a, uint32_t rows_per_block) {
@@ -145,7 +145,7 @@ void short_dropout_kernel(DropoutArgs a, uint32_t rows_per_block) {
     }
     return;
   }
-  const uint32_t inverse = (1u << 20) / vectors + 1;   // n / vectors = n * inverse >> 20 for n up to 1,024, vectors up to 129
+  const uint32_t inverse = (1u << 20) / vectors + 1;   // n / vectors = n * inverse >> 20 for n up to 1,024, vectors up to 513
   u4v h[U] = {}, r[kResidual ? U : 1] = {};
   uint32_t row[U], v[U];
 #pragma unroll
@@ -176,28 +176,27 @@ void short_dropout_kernel(DropoutArgs a, uint32_t rows_per_block) {
   }
 }
 
-// Longer rows: a group of LANES lanes takes LANES * U vectors of a row, the runs of a longer row go
-// to different blocks, and the values that fill no vector to one lane each.  Rows of 16-bit values
-// that start at no multiple of 4 bytes, where loads take longer, are taken from their second value
-// on: their vectors' fields come from three draws, not two.
-template <class T, bool kResidual, int LANES, int U>
+// Longer rows: a block takes kThreads * U vectors of a row, and of its last run the values that fill
+// no vector, one per lane.  Rows of 16-bit values that start at no multiple of 4 bytes, where loads
+// take longer, are taken from their second value on: their vectors' fields come from three draws,
+// not two.
+template <class T, bool kResidual, int U>
 __global__ __launch_bounds__(kThreads)
 void dropout_kernel(DropoutArgs a) {
-  constexpr uint32_t kN = Vec<T>::kN, kRows = kThreads / LANES;
-  int64_t row = static_cast<int64_t>(blockIdx.z) * gridDim.y + blockIdx.y;
-  if constexpr (kRows > 1) row = row * kRows + __builtin_amdgcn_readfirstlane(threadIdx.x / LANES);
+  constexpr uint32_t kN = Vec<T>::kN;
+  const int64_t row = static_cast<int64_t>(blockIdx.z) * gridDim.y + blockIdx.y;
   if (row >= a.rows) return;
   const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
   const T* res = kResidual ? static_cast<const T*>(a.residual) + row * a.residual_stride : nullptr;
   T* out = static_cast<T*>(a.out) + row * a.out_stride;
   const uint32_t odd = sizeof(T) == 2 ? static_cast<uint32_t>(reinterpret_cast<uintptr_t>(x) >> 1) & 1 : 0;
-  const uint32_t lane = threadIdx.x % LANES, cols = static_cast<uint32_t>(a.cols);
-  const uint32_t full = (cols - odd) / kN, rem = cols - odd - full * kN, v0 = blockIdx.x * (LANES * U);
+  const uint32_t lane = threadIdx.x, cols = static_cast<uint32_t>(a.cols);
+  const uint32_t full = (cols - odd) / kN, rem = cols - odd - full * kN, v0 = blockIdx.x * (kThreads * U);
   u4v h[U] = {}, r[kResidual ? U : 1] = {};
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    const uint32_t column = (v0 + i * LANES) * kN + odd;
-    if (v0 + i * LANES + lane < full) {
+    const uint32_t column = (v0 + i * kThreads) * kN + odd;
+    if (v0 + i * kThreads + lane < full) {
       h[i] = Vec<T>::load(x, column, lane);
       if (kResidual) r[i] = Vec<T>::load(res, column, lane);
     }
@@ -205,9 +204,9 @@ void dropout_kernel(DropoutArgs a) {
   const uint64_t key = row_key(a, row);
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    const uint32_t v = v0 + i * LANES + lane;
+    const uint32_t v = v0 + i * kThreads + lane;
     if (v < full)
-      Vec<T>::store(out, (v0 + i * LANES) * kN + odd, lane,
+      Vec<T>::store(out, (v0 + i * kThreads) * kN + odd, lane,
                     Vec<T>::template dropped<kResidual>(a, key, v * (kN / 4), odd != 0, h[i], r[kResidual ? i : 0]));
   }
   if (blockIdx.x == gridDim.x - 1 && lane < rem) drop_value<T, kResidual>(a, key, x, res, out, cols - rem + lane);
@@ -225,14 +224,14 @@ hipError_t launch_short(const DropoutArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <class T, bool kResidual, int LANES, int U>
+template <class T, bool kResidual, int U>
 hipError_t launch_long(const DropoutArgs& a, hipStream_t stream) {
-  constexpr int64_t kRows = kThreads / LANES, kRun = int64_t{LANES} * U;
+  constexpr int64_t kRun = int64_t{kThreads} * U;
   const int64_t full = a.cols / Vec<T>::kN;
-  const int64_t groups = (a.rows + kRows - 1) / kRows, y = std::min(groups, kGridYZ);
+  const int64_t y = std::min(a.rows, kGridYZ);
   const dim3 grid(static_cast<uint32_t>(std::max<int64_t>(1, (full + kRun - 1) / kRun)), static_cast<uint32_t>(y),
-                  static_cast<uint32_t>((groups + y - 1) / y));
-  dropout_kernel<T, kResidual, LANES, U><<<grid, kThreads, 0, stream>>>(a);
+                  static_cast<uint32_t>((a.rows + y - 1) / y));
+  dropout_kernel<T, kResidual, U><<<grid, kThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -241,8 +240,8 @@ template <class T, bool kResidual>
 hipError_t launch_by_row(const DropoutArgs& a, hipStream_t stream) {
   const int64_t full = a.cols / Vec<T>::kN;
   if (full <= kShortVectors) return launch_short<T, kResidual>(a, stream);
-  if (full <= 256) return launch_long<T, kResidual, 64, 4>(a, stream);
-  return launch_long<T, kResidual, 256, 4>(a, stream);
+  if constexpr (sizeof(T) == 4) return launch_long<T, kResidual, 1>(a, stream);
+  else return launch_long<T, kResidual, 4>(a, stream);
 }
 
 template <class T>

@@ -271,30 +271,33 @@ int pgc_preference_loss(const pgc_logits* logits, const pgc_preference_args* a, 
   float* stats = static_cast<float*>(workspace);
   float* grad = reinterpret_cast<float*>(static_cast<char*>(workspace) + align_up(8 * static_cast<size_t>(rows)));
   pgc::LogitsArgs k = logits_args(logits, a->targets);
+  k.logprobs = a->logprobs;
+  pgc::PairArgs p{};
+  p.targets = a->targets;
+  p.offsets = a->offsets;
+  p.logprobs = a->logprobs;
+  p.ref_logprobs = a->ref_logprobs;
+  p.weights = a->pair_weights;
+  p.loss = a->loss;
+  p.margins = a->margins;
+  p.grad = a->dlogits ? grad : nullptr;
+  p.rows = rows;
+  p.cols = logits->cols;
+  p.pairs = pairs;
+  p.beta = a->beta;
+  p.smoothing = a->label_smoothing;
+  p.scale = a->scale;
+  if (pgc::preference_is_small(k, p, logits->dtype)) {
+    k.dlogits = a->dlogits;
+    k.out_stride = a->dlogits_stride;
+    return launched(pgc::launch_small_preference(k, p, logits->dtype, stream), "preference loss kernel");
+  }
   if (rows > 0) {
-    k.logprobs = a->logprobs;
     k.stats = stats;
     k.zero_grad = grad;
     CHECK(launched(pgc::launch_logits(k, pgc::RowMode::kForward, logits->dtype, stream), "log-probability kernel"));
   }
-  if (pairs > 0) {
-    pgc::PairArgs p{};
-    p.targets = a->targets;
-    p.offsets = a->offsets;
-    p.logprobs = a->logprobs;
-    p.ref_logprobs = a->ref_logprobs;
-    p.weights = a->pair_weights;
-    p.loss = a->loss;
-    p.margins = a->margins;
-    p.grad = a->dlogits ? grad : nullptr;
-    p.rows = rows;
-    p.cols = logits->cols;
-    p.pairs = pairs;
-    p.beta = a->beta;
-    p.smoothing = a->label_smoothing;
-    p.scale = a->scale;
-    CHECK(launched(pgc::launch_pairs(p, stream), "pair kernel"));
-  }
+  if (pairs > 0) CHECK(launched(pgc::launch_pairs(p, stream), "pair kernel"));
   if (rows > 0 && a->dlogits) {
     k.grad = grad;
     k.dlogits = a->dlogits;

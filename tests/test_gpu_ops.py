@@ -654,3 +654,23 @@ def test_the_binding_refuses_what_does_not_fit():
     assert ops.dropout(z[:0], 0.1, 1).shape == (0, 40) and ops.dropout(z[:, :0], 0.1, 1).shape == (6, 0)
     lp, stats = ops.token_logprobs(z[:0], y[:0])
     assert lp.shape == (0,) and stats.shape == (0, 2)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_every_operator_gives_a_row_the_same_logprobs(dtype):
+    """The preference loss of few logits (one launch), of many (a launch per step), and the scores."""
+    for cols in (1, 7, 8, 31, 64, 129, 500, 1024, 1025, 1500, 1600, 2047, 2500, 3300, 4100, 9001):
+        _say("same logprobs", dtype, cols)
+        z, y = _case(dtype, 24, cols, cols)
+        z, y = z.cuda(), y.cuda()
+        want = ops.token_logprobs(z, y)[0]
+        o = torch.tensor([1, 5, 9, 9, 20], dtype=torch.int32, device="cuda")
+        few = ops.preference_loss(z, y, o, want + 0.1, beta=0.7, label_smoothing=0.2)
+        assert torch.equal(few[2], want)
+        # The same two pairs ahead of so many further rows that no size takes one launch.
+        more = max(5000, 2_000_000 // cols // z.element_size())
+        zz, yy = torch.cat([z, z[:1].expand(more, cols)]), torch.cat([y, y[:1].expand(more)])
+        many = ops.preference_loss(zz, yy, o, torch.cat([want, want[:1].expand(more)]) + 0.1, beta=0.7, label_smoothing=0.2)
+        for a, b in zip(few, many):
+            assert torch.equal(a, b[:len(a)])
+        assert not many[3][24:].any()
