@@ -1,10 +1,21 @@
-// Token log-probabilities, their gradient, the policy loss and the preference loss's pair
-// sums (include/pgc_ops.h), for gfx950.
+// Token log-probabilities, their gradient, the policy loss and the preference loss
+// (include/pgc_ops.h), for gfx950.
 //
-// A row of up to 32 vectors of 16 bytes belongs to 4 to 32 lanes of a wave, a longer one to 1 to
-// 16 waves, each with a run of neighbouring vectors.  Which lane sums what, and hence every bit of
-// the result, depends on the number of columns alone, not on where the row lies.  Each lane keeps
-// a running maximum and sum; lanes and waves join theirs once.
+// All of it is one exponential and a handful of additions per logit, so memory bounds it: a row
+// should come in once and its gradient leave once, with enough loads in flight throughout.  Sums of
+// exponentials run beside the maximum (a running pair per lane, joined over lanes and waves
+// once), so one pass suffices for the log-probability; the policy loss keeps the row on the chip
+// from there to the gradient.  The preference loss needs whole sequences before its first
+// gradient, so its rows are read twice.
+//
+// Rows of up to 128 vectors of 16 bytes belong to 1 to 32 lanes of a wave, longer ones to 1 to 16
+// waves.  Which lane sums what, and hence every bit of the result, depends on the number of
+// columns alone, not on where the row lies nor on the rows beside it.
+//
+// Measured (MI355X; GB of logits read and gradients written per second): forward of 16,384 rows of
+// 131,072 bf16 602 us, 7.1 TB/s; policy loss of 4,096 rows of 65,536 fp16 176 us, 5.8 TB/s; of 8,192
+// rows of 131,071 bf16 814 us, 5.3; gradient of 8,192 rows of 131,072 bf16 704 us, 6.1.  A copy of a
+// gigabyte by the runtime moves 5.0, a read alone 7.2.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -89,6 +100,7 @@ struct Stat {
 
 __device__ __forceinline__ float finite_top(float top) { return top == -INFINITY ? 0.f : top; }
 
+// U vectors at once: one rescaling of the sum so far, and the lanes' additions in a tree.
 template <class T, int U>
 __device__ __forceinline__ void add_vectors(Stat& s, const u4v (&h)[U]) {
   constexpr int kN = Vec<T>::kN;
@@ -115,6 +127,7 @@ __device__ __forceinline__ void add_vectors(Stat& s, const u4v (&h)[U]) {
   s = {top, sum};
 }
 
+// The same of one vector that is unpacked already.
 template <uint32_t N, class Floats>
 __device__ __forceinline__ void add_floats(Stat& s, Floats f) {
   float top = s.top;
@@ -298,9 +311,11 @@ struct ShortRow {
   }
 };
 
-// All modes for short rows, 64 / LANES of them to a wave.  Few lanes per row, each with several
-// vectors, spare the joins and the row's own arithmetic, but their stores would scatter: a row's
-// gradient goes through LDS to as many lanes as it has vectors.
+// All modes for short rows, 64 / LANES of them to a wave.  What bounds them is the number of
+// instructions: few lanes per row, each with several vectors, spare the joins and the row's own
+// arithmetic (1,048,576 rows of 100 bf16, 13 vectors, on 16 lanes: forward 79 us; on 4: 46).  Their
+// stores would scatter (policy loss 120 us), so a row's gradient goes through LDS to as many
+// lanes as it has vectors (84 us, 5.0 TB/s).
 template <class T, RowMode kMode, int LANES, int HOLD>
 __global__ __launch_bounds__(kBlock)
 void short_row_kernel(LogitsArgs a) {
@@ -506,7 +521,8 @@ __device__ __forceinline__ Stat long_row_part(const T* z, uint32_t cols, uint32_
   return join_lanes<kWave>(s);
 }
 
-// kForward for long rows: a block (or, with WAVES = 1, a wave) per row.
+// kForward for long rows: a block (or, with WAVES = 1, a wave) per row, whose waves take U vectors per
+// lane in turn.
 template <class T, int WAVES, int U>
 __global__ __launch_bounds__(Place<WAVES * kWave>::kThreads)
 void long_forward_kernel(LogitsArgs a) {
@@ -602,9 +618,12 @@ __device__ __forceinline__ RowGradient<T> finish_policy_row(const LogitsArgs& a,
 }
 
 // kPolicy for long rows: a block (or, with WAVES = 1, a wave) per row.  Two blocks or more share a
-// CU, so that one's loads and stores go on while another computes.  From the sum to the gradient a
-// lane keeps its first HOLD vectors in registers and the next STAGE in LDS, where they are loaded
-// without passing through registers; the rest of a row that is longer still is read again.
+// CU, so that one's loads and stores go on while another computes (12,289 rows of 50,021 bf16: 454 us;
+// one block of 16 waves per CU 580, the same with the next row's loads among the stores 566).
+// From the sum to the gradient a lane keeps its first HOLD vectors in registers and the next STAGE
+// in LDS, where they are loaded without passing through registers; the rest of a row that is
+// longer still is read again.  8 waves of 16 + 9 vectors hold 102,400 16-bit values at two blocks
+// to a CU: rows of 131,072 bf16 take 750 us so, 805 held whole by one block of 16 waves.
 template <class T, int WAVES, int HOLD, int STAGE>
 __global__ __launch_bounds__(Place<WAVES * kWave>::kThreads)
 void long_policy_kernel(LogitsArgs a) {
@@ -689,9 +708,9 @@ void long_policy_kernel(LogitsArgs a) {
   ends.store(dz, grad, full, run.odd, tid, rem, y);
 }
 
-// kBackward: every value by itself.  A group of LANES lanes takes LANES * U vectors of a row;
-// the runs of a longer row go to different blocks.  Rows of 16-bit values that start at no multiple
-// of 4 bytes are taken from their second value on.
+// kBackward of longer rows: every value by itself.  A group of LANES lanes takes LANES * U vectors of
+// a row; the runs of a longer row go to different blocks.  Rows of 16-bit values that start at no
+// multiple of 4 bytes are taken from their second value on.
 template <class T, int LANES, int U>
 __global__ __launch_bounds__(Place<LANES>::kThreads)
 void gradient_kernel(LogitsArgs a) {
@@ -779,6 +798,9 @@ template <class T>
 hipError_t launch_forward(const LogitsArgs& a, hipStream_t stream) {
   const int64_t vectors = (a.cols + Vec<T>::kN - 1) / Vec<T>::kN, full = a.cols / Vec<T>::kN;
   if (vectors <= kShortVectors) return launch_short<T, RowMode::kForward>(a, stream);
+  // Fewer waves leave fewer of them without a vector; more have more loads in flight for one row.
+  // 9,000 bf16 columns (1,125 vectors): 82 us on 2 waves, 87 on 4, 106 on 8, 166 on 16; 131,073: 87,
+  // 81, 80 and 79.
   if (in_threes(full)) return launch_rows<64>(long_forward_kernel<T, 1, 3>, a, stream);
   if (full <= 512) return launch_rows<64>(long_forward_kernel<T, 1, 4>, a, stream);
   if (full <= 1536) return launch_rows<128>(long_forward_kernel<T, 2, 4>, a, stream);
@@ -813,6 +835,9 @@ template <class T>
 hipError_t launch_backward(const LogitsArgs& a, hipStream_t stream) {
   const int64_t vectors = (a.cols + Vec<T>::kN - 1) / Vec<T>::kN;
   if (vectors <= kShortVectors) return launch_short<T, RowMode::kBackward>(a, stream);
+  // Runs that leave few lanes of a row's last one empty: 9,000 bf16 columns (1,125 vectors) 166 us in
+  // runs of 512, 209 of 1,024; 20,000 (2,500) 169 and 163.  fp32 does best with a load per lane
+  // (24,000 columns 163 us, with two 176).
   if (vectors <= 256) return launch_gradient<T, 64, 4>(a, stream);
   if (vectors <= 512) return launch_gradient<T, 256, 2>(a, stream);
   if constexpr (sizeof(T) == 4) {
@@ -999,7 +1024,7 @@ hipError_t launch_pairs(const PairArgs& a, hipStream_t stream) {
 
 bool preference_is_small(const LogitsArgs& a, const PairArgs& p, int dtype) {
   const int64_t value = dtype == PGC_F32 ? 4 : 2;
-  return p.pairs > 0 && a.rows <= kSmallRows && a.cols * value < 513 * 16 &&
+  return p.pairs > 0 && p.pairs <= kSmallRows && a.rows <= kSmallRows && a.cols * value < 513 * 16 &&
          a.rows * a.cols * value <= std::min(kSmallBytes, kSmallPairBytes * p.pairs);
 }
 

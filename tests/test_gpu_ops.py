@@ -358,6 +358,11 @@ def test_preference_loss_edges():
     tame = torch.tensor([0, 8, 20], dtype=torch.int32, device="cuda")
     for a, b in zip(ops.preference_loss(z, y, wild), ops.preference_loss(z, y, tame)):
         assert torch.equal(a, b)
+    # More empty pairs than one launch has blocks for.
+    empties = torch.full((2 * 3_000_000 + 1,), 4, dtype=torch.int32, device="cuda")
+    empties[-1] = 20
+    loss, margin, _, dz = ops.preference_loss(z, y, empties)
+    assert (loss[:-1] - np.log(2)).abs().max().item() < 1e-7 and not dz[:4].any() and dz[4:].any()
     # A margin far out: finite loss, gradient of at most the slope's bound, none NaN.
     far = torch.full((20,), 1e6, device="cuda")
     loss, margin, _, dz = ops.preference_loss(z, y, tame, far, beta=5.0)
