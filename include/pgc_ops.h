@@ -135,11 +135,12 @@ typedef struct pgc_preference_args {
   int64_t dlogits_stride;
 } pgc_preference_args;
 
-/* Bytes of device workspace for `rows` rows (a multiple of 256). */
-int pgc_preference_workspace_bytes(int64_t rows, size_t* bytes);
+/* Bytes of device workspace that the call on such logits (their data is not looked at)
+ * and so many pairs needs: a multiple of 256, 0 for small ones.  Host only. */
+int pgc_preference_workspace_bytes(const pgc_logits* logits, int64_t pairs, size_t* bytes);
 
 /* workspace: at least that many bytes, 256-byte aligned, used until the stream has
- * passed the call. */
+ * passed the call; may be NULL where none are needed. */
 int pgc_preference_loss(const pgc_logits* logits, const pgc_preference_args* args,
                         void* workspace, size_t workspace_bytes, void* hip_stream);
 

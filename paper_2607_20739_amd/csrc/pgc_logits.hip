@@ -867,19 +867,34 @@ struct PairRows {
 };
 
 // The pair's loss, written by one thread, and the gradient of its preferred rows' log-probabilities
-// (the others' is the negative).  The sum runs over kPairThreads threads in a fixed order, in 64
-// bits; `logprob` gives a row's log-probability.
+// (the others' is the negative).  The sum runs over kPairThreads threads, four neighbouring rows
+// to each at a time and two such loads in flight, in a fixed order, in 64 bits; `logprobs4` gives four
+// rows' log-probabilities.
 constexpr int kPairThreads = 1024;
-template <class Logprob>
+typedef float f4_unaligned __attribute__((ext_vector_type(4), aligned(4)));
+typedef int32_t i4_unaligned __attribute__((ext_vector_type(4), aligned(4)));
+
+template <class Logprobs>
 __device__ __forceinline__ float pair_slope(const PairArgs& a, int64_t pair, const PairRows& rows, double (&sums)[kPairThreads / kWave],
-                                            Logprob logprob) {
+                                            Logprobs logprobs) {
   double sum = 0.0;
-  for (int64_t t = rows.at[0] + threadIdx.x; t < rows.at[2]; t += kPairThreads) {
-    const int32_t y = a.targets[t];
-    const float ref = a.ref_logprobs ? a.ref_logprobs[t] : 0.f, lp = logprob(t);
-    if (y < 0 || y >= a.cols) continue;
+  auto add = [&](int64_t t, int32_t y, float lp, float ref) {
+    if (y < 0 || y >= a.cols) return;
     const double v = static_cast<double>(lp) - ref;
     sum += t < rows.at[1] ? v : -v;
+  };
+#pragma unroll 2
+  for (int64_t t = rows.at[0] + 4 * threadIdx.x; t < rows.at[2]; t += 4 * kPairThreads) {
+    if (t + 4 <= rows.at[2]) {
+      const i4_unaligned y = *reinterpret_cast<const i4_unaligned*>(a.targets + t);
+      f4_unaligned ref = {0.f, 0.f, 0.f, 0.f};
+      if (a.ref_logprobs) ref = *reinterpret_cast<const f4_unaligned*>(a.ref_logprobs + t);
+      const f4_unaligned lp = logprobs(t);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) add(t + k, y[k], lp[k], ref[k]);
+    } else {
+      for (int64_t u = t; u < rows.at[2]; ++u) add(u, a.targets[u], logprobs.one(u), a.ref_logprobs ? a.ref_logprobs[u] : 0.f);
+    }
   }
   for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d, kWave);
   if (threadIdx.x % kWave == 0) sums[threadIdx.x / kWave] = sum;
@@ -899,14 +914,29 @@ __device__ __forceinline__ float pair_slope(const PairArgs& a, int64_t pair, con
   return weight == 0.0 ? 0.f : static_cast<float>(slope * a.beta * a.scale * weight);
 }
 
+// Log-probabilities by row, from memory or from LDS.
+struct RowLogprobs {
+  const float* p;
+  __device__ __forceinline__ f4_unaligned operator()(int64_t t) const { return *reinterpret_cast<const f4_unaligned*>(p + t); }
+  __device__ __forceinline__ float one(int64_t t) const { return p[t]; }
+};
+
 __global__ __launch_bounds__(kPairThreads)
 void pair_kernel(PairArgs a) {
   __shared__ double sums[kPairThreads / kWave];
   for (int64_t pair = blockIdx.x; pair < a.pairs; pair += gridDim.x) {
     const PairRows rows(a, pair);
-    const float g = pair_slope(a, pair, rows, sums, [&](int64_t t) { return a.logprobs[t]; });
-    if (a.grad)
-      for (int64_t t = rows.at[0] + threadIdx.x; t < rows.at[2]; t += kPairThreads) a.grad[t] = t < rows.at[1] ? g : -g;
+    const float g = pair_slope(a, pair, rows, sums, RowLogprobs{a.logprobs});
+    if (a.grad) {
+      for (int64_t t = rows.at[0] + 4 * threadIdx.x; t < rows.at[2]; t += 4 * kPairThreads) {
+        f4_unaligned v;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = t + k < rows.at[1] ? g : -g;
+        if (t + 4 <= rows.at[2]) *reinterpret_cast<f4_unaligned*>(a.grad + t) = v;
+        else
+          for (int64_t u = t; u < rows.at[2]; ++u) a.grad[u] = v[u - t];
+      }
+    }
     __syncthreads();   // before the sums of the next pair
   }
 }
@@ -954,7 +984,7 @@ void small_preference_kernel(LogitsArgs a, PairArgs p) {
     }
   }
   __syncthreads();
-  const float g = pair_slope(p, pair, rows, sums, [&](int64_t t) { return logprobs[t]; });
+  const float g = pair_slope(p, pair, rows, sums, RowLogprobs{logprobs});
   if (a.dlogits == nullptr) return;
   for (int64_t row = from + group; row < to; row += kGroups) {
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
@@ -1022,10 +1052,10 @@ hipError_t launch_pairs(const PairArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-bool preference_is_small(const LogitsArgs& a, const PairArgs& p, int dtype) {
-  const int64_t value = dtype == PGC_F32 ? 4 : 2;
-  return p.pairs > 0 && p.pairs <= kSmallRows && a.rows <= kSmallRows && a.cols * value < 513 * 16 &&
-         a.rows * a.cols * value <= std::min(kSmallBytes, kSmallPairBytes * p.pairs);
+bool preference_is_small(int64_t rows, int64_t cols, int64_t pairs, int dtype) {
+  const int64_t row_bytes = cols * (dtype == PGC_F32 ? 4 : 2);
+  return pairs > 0 && pairs <= kSmallRows && rows <= kSmallRows && row_bytes < 513 * 16 &&
+         rows * row_bytes <= std::min(kSmallBytes, kSmallPairBytes * pairs);
 }
 
 hipError_t launch_small_preference(const LogitsArgs& a, const PairArgs& p, int dtype, hipStream_t stream) {

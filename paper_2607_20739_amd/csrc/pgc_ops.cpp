@@ -73,6 +73,10 @@ int check_extents(int64_t rows, int64_t cols) {
   return PGC_OK;
 }
 
+int check_pairs(int64_t pairs) {
+  return pairs < 0 || pairs > kMaxExtent / 2 ? fail(PGC_EINVAL, "pairs must lie in [0, 2^30 - 1]") : PGC_OK;
+}
+
 int check_stride(const char* name, int64_t stride, int64_t cols) {
   if (stride < cols || stride > (int64_t{1} << 40))
     return fail(PGC_EINVAL, "%s stride must lie in [columns, 2^40]", name);
@@ -225,11 +229,15 @@ int pgc_token_logprobs_backward(const pgc_logits* logits, const int32_t* targets
                   "log-probability gradient kernel");
 }
 
-// The rows' (M, ln S) pairs, then their gradients.
-int pgc_preference_workspace_bytes(int64_t rows, size_t* bytes) {
-  if (bytes == nullptr) return fail(PGC_EINVAL, "bytes is NULL");
-  if (rows < 0 || rows > kMaxExtent) return fail(PGC_EINVAL, "rows must lie in [0, 2^31 - 1]");
-  *bytes = align_up(8 * static_cast<size_t>(rows)) + align_up(4 * static_cast<size_t>(rows));
+// The rows' (M, ln S) pairs, then their gradients; nothing where one launch does it all.
+int pgc_preference_workspace_bytes(const pgc_logits* logits, int64_t pairs, size_t* bytes) {
+  if (logits == nullptr || bytes == nullptr) return fail(PGC_EINVAL, "null arguments");
+  if (!known(logits->dtype)) return fail(PGC_EINVAL, "unknown dtype %d", logits->dtype);
+  CHECK(check_extents(logits->rows, logits->cols));
+  CHECK(check_pairs(pairs));
+  const size_t rows = static_cast<size_t>(logits->rows);
+  const bool none = pgc::preference_is_small(logits->rows, logits->cols, pairs, logits->dtype);
+  *bytes = none ? 0 : align_up(8 * rows) + align_up(4 * rows);
   return PGC_OK;
 }
 
@@ -238,7 +246,7 @@ int pgc_preference_loss(const pgc_logits* logits, const pgc_preference_args* a, 
   if (logits == nullptr || a == nullptr) return fail(PGC_EINVAL, "null arguments");
   CHECK(check_logits(logits, a->targets));
   const int64_t rows = logits->rows, pairs = a->pairs;
-  if (pairs < 0 || pairs > kMaxExtent / 2) return fail(PGC_EINVAL, "pairs must lie in [0, 2^30 - 1]");
+  CHECK(check_pairs(pairs));
   if (!finite32(a->beta) || !finite32(a->scale)) return fail(PGC_EINVAL, "beta and scale must be finite");
   if (!(a->label_smoothing >= 0.0 && a->label_smoothing <= 1.0))
     return fail(PGC_EINVAL, "label_smoothing must lie in [0, 1]");
@@ -250,7 +258,7 @@ int pgc_preference_loss(const pgc_logits* logits, const pgc_preference_args* a, 
   CHECK(check_floats("logprobs", a->logprobs, rows, true));
   if (a->dlogits) CHECK(check_dlogits(logits, a->dlogits, a->dlogits_stride));
   size_t need = 0;
-  CHECK(pgc_preference_workspace_bytes(rows, &need));
+  CHECK(pgc_preference_workspace_bytes(logits, pairs, &need));
   const Span ws = {"workspace", reinterpret_cast<uintptr_t>(workspace), need, 0};
   CHECK(check_pointer(ws, kAlign, true));
   if (workspace_bytes < need)
@@ -287,7 +295,7 @@ int pgc_preference_loss(const pgc_logits* logits, const pgc_preference_args* a, 
   p.beta = a->beta;
   p.smoothing = a->label_smoothing;
   p.scale = a->scale;
-  if (pgc::preference_is_small(k, p, logits->dtype)) {
+  if (need == 0 && rows > 0) {
     k.dlogits = a->dlogits;
     k.out_stride = a->dlogits_stride;
     return launched(pgc::launch_small_preference(k, p, logits->dtype, stream), "preference loss kernel");

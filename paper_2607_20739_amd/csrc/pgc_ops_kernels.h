@@ -63,7 +63,7 @@ hipError_t launch_pairs(const PairArgs& a, hipStream_t stream);
 
 // Forward, pairs and backward of few logits in one launch, without a workspace (a.dlogits null: no
 // gradient; p.logprobs and p.grad are not used).
-bool preference_is_small(const LogitsArgs& a, const PairArgs& p, int dtype);
+bool preference_is_small(int64_t rows, int64_t cols, int64_t pairs, int dtype);
 hipError_t launch_small_preference(const LogitsArgs& a, const PairArgs& p, int dtype, hipStream_t stream);
 
 }  // namespace pgc

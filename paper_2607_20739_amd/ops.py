@@ -52,7 +52,7 @@ _SIGNATURES = {
     "pgc_dropout_backward": (ctypes.c_int, [ctypes.POINTER(pgc_dropout_args), _P]),
     "pgc_token_logprobs": (ctypes.c_int, [ctypes.POINTER(pgc_logits), _P, _P, _P, _P]),
     "pgc_token_logprobs_backward": (ctypes.c_int, [ctypes.POINTER(pgc_logits), _P, _P, _P, _P, _I64, _P]),
-    "pgc_preference_workspace_bytes": (ctypes.c_int, [_I64, ctypes.POINTER(_SIZE)]),
+    "pgc_preference_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(pgc_logits), _I64, ctypes.POINTER(_SIZE)]),
     "pgc_preference_loss": (ctypes.c_int, [ctypes.POINTER(pgc_logits), ctypes.POINTER(pgc_preference_args),
                                            _P, _SIZE, _P]),
     "pgc_policy_loss": (ctypes.c_int, [ctypes.POINTER(pgc_logits), ctypes.POINTER(pgc_policy_args), _P]),
@@ -219,10 +219,15 @@ def token_logprobs_backward(logits, targets, stats, grad, out=None):
 
 # ---- losses ---------------------------------------------------------------------------------
 
-def preference_workspace_bytes(rows):
-    """Bytes of the workspace that preference_loss uses for `rows` rows of logits."""
+def preference_workspace_bytes(logits, pairs):
+    """Bytes of the workspace that preference_loss needs for such logits and so many pairs."""
+    rows, cols = logits.shape
+    return _workspace_bytes(pgc_logits(None, rows, cols, cols, _DTYPES[logits.dtype]), pairs)
+
+
+def _workspace_bytes(z, pairs):
     out = _SIZE()
-    _check(lib().pgc_preference_workspace_bytes(rows, ctypes.byref(out)))
+    _check(lib().pgc_preference_workspace_bytes(ctypes.byref(z), pairs, ctypes.byref(out)))
     return out.value
 
 
@@ -232,17 +237,18 @@ def preference_loss(logits, targets, offsets, ref_logprobs=None, beta=0.1, label
 
     Sequence q holds the rows [offsets[q], offsets[q + 1]) (int32); pair i prefers sequence 2 i to
     2 i + 1.  dlogits is the gradient of scale * sum(pair_weights * loss), None with gradient=False.
-    `out` receives it and may be the logits.  `workspace` (uint8, preference_workspace_bytes(rows))
-    is allocated where it is not given.
+    `out` receives it and may be the logits.  `workspace` (uint8, preference_workspace_bytes(logits,
+    pairs)) is allocated where it is not given.
     """
     z, y = _logits(logits, targets)
     pairs = (offsets.numel() - 1) // 2
     offsets = _array("offsets", offsets, logits, torch.int32, (2 * max(pairs, 0) + 1,))
     ref = _array("ref_logprobs", ref_logprobs, logits, torch.float32, (z.rows,))
     weights = _array("pair_weights", pair_weights, logits, torch.float32, (pairs,))
-    if workspace is None:
-        workspace = logits.new_empty(preference_workspace_bytes(z.rows), dtype=torch.uint8)
-    ws = _array("workspace", workspace, logits, torch.uint8, workspace.shape)
+    nbytes = _workspace_bytes(z, pairs) if workspace is None else workspace.numel()
+    if workspace is None and nbytes > 0:
+        workspace = logits.new_empty(nbytes, dtype=torch.uint8)
+    ws = None if workspace is None else _array("workspace", workspace, logits, torch.uint8, workspace.shape)
     loss = logits.new_empty(pairs, dtype=torch.float32)
     margins = logits.new_empty(pairs, dtype=torch.float32)
     logprobs = logits.new_empty(z.rows, dtype=torch.float32)
@@ -251,7 +257,7 @@ def preference_loss(logits, targets, offsets, ref_logprobs=None, beta=0.1, label
         out, stride = _output(logits, out)
     args = pgc_preference_args(y, offsets, ref, weights, pairs, beta, label_smoothing, scale, loss.data_ptr(),
                                margins.data_ptr(), logprobs.data_ptr(), out.data_ptr() if gradient else None, stride)
-    _call(logits, "pgc_preference_loss", ctypes.byref(z), ctypes.byref(args), ws, workspace.numel())
+    _call(logits, "pgc_preference_loss", ctypes.byref(z), ctypes.byref(args), ws, nbytes)
     return loss, margins, logprobs, out if gradient else None
 
 

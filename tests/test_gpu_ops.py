@@ -650,7 +650,7 @@ def test_the_binding_refuses_what_does_not_fit():
         lambda: ops.dropout(z, 1.5, 1), lambda: ops.dropout(z[:, :20], 0.1, 1, out=z[:, 10:30]),
         lambda: ops.policy_loss(z, y, f, f, kl=0.1), lambda: ops.policy_loss(z, y, f, f, clip_low=2.0),
         lambda: ops.preference_loss(z, y, o, label_smoothing=-1.0),
-        lambda: ops.preference_loss(z, y, o, workspace=torch.empty(0, dtype=torch.uint8, device="cuda")),
+        lambda: ops.preference_loss(z, y, o[:1], workspace=torch.empty(0, dtype=torch.uint8, device="cuda")),
     ]
     for call in refused:
         with pytest.raises(P.PGCError) as e:

@@ -258,24 +258,41 @@ def _preference(**change):
     (dict(ref_logprobs=4 * BASE + 1), "ref_logprobs must"), (dict(pair_weights=9 * BASE + 2), "pair_weights must"),
     (dict(dlogits_stride=3), "dlogits stride"), (dict(dlogits=BASE, dlogits_stride=11), "overlaps logits"),
     (dict(margins=5 * BASE + 4), "margins overlaps loss"), (dict(logprobs=4 * BASE), "logprobs overlaps ref"),
-    (dict(logprobs=12 * BASE), "workspace overlaps logprobs"), (dict(dlogits=3 * BASE), "dlogits overlaps offsets"),
+    (dict(dlogits=3 * BASE), "dlogits overlaps offsets"),
 ])
 def test_preference_loss_refuses(change, text):
     args = _preference(**change)
     _refused(ops.lib().pgc_preference_loss(ctypes.byref(_logits()), ctypes.byref(args), 12 * BASE, 1 << 20, None), text)
 
 
-def test_preference_workspace_refusals():
-    lib, z, a = ops.lib(), _logits(), _preference()
-    need = ops.preference_workspace_bytes(6)
-    assert need % 256 == 0 and need >= 6 * 12
-    assert ops.preference_workspace_bytes(0) == 0
-    _refused(lib.pgc_preference_loss(ctypes.byref(z), ctypes.byref(a), 12 * BASE, need - 1, None), "too small")
-    _refused(lib.pgc_preference_loss(ctypes.byref(z), ctypes.byref(a), None, need, None), "workspace is NULL")
-    _refused(lib.pgc_preference_loss(ctypes.byref(z), ctypes.byref(a), 12 * BASE + 128, need, None), "256-byte")
-    _refused(lib.pgc_preference_workspace_bytes(5, None), "NULL")
-    with pytest.raises(P.PGCError):
-        ops.preference_workspace_bytes(-1)
+def _workspace(z, pairs):
+    out = ctypes.c_size_t(1)
+    return ops.lib().pgc_preference_workspace_bytes(ctypes.byref(z), pairs, ctypes.byref(out)), out.value
+
+
+def test_preference_workspace_sizes_and_refusals():
+    lib = ops.lib()
+    big = _logits(rows=5000, cols=100, stride=100)
+    status, need = _workspace(big, 2)
+    assert status == P.PGC_OK and need % 256 == 0 and need >= 5000 * 12
+    assert _workspace(_logits(rows=0), 0) == (P.PGC_OK, 0)
+    # Few logits need none; as many in one pair, in none, or of long rows, do.
+    assert _workspace(_logits(rows=1000, cols=64, stride=64), 8) == (P.PGC_OK, 0)
+    for rows, cols, pairs in [(1200, 64, 1), (1000, 64, 0), (40, 8192, 8), (4097, 10, 100), (1000, 64, 5000)]:
+        assert _workspace(_logits(rows=rows, cols=cols, stride=cols), pairs)[1] >= rows * 12, (rows, cols, pairs)
+    assert ops.preference_workspace_bytes(torch.empty(5000, 100, dtype=torch.float16), 2) == need
+    _refused(_workspace(big, -1)[0], "pairs")
+    _refused(_workspace(_logits(rows=-1), 1)[0], "rows")
+    _refused(_workspace(_logits(dtype=7), 1)[0], "dtype")
+    _refused(lib.pgc_preference_workspace_bytes(ctypes.byref(big), 1, None), "null")
+    _refused(lib.pgc_preference_workspace_bytes(None, 1, ctypes.byref(ctypes.c_size_t())), "null")
+    a = _preference(dlogits_stride=100)
+    args = [ctypes.byref(big), ctypes.byref(a)]
+    _refused(lib.pgc_preference_loss(*args, 12 * BASE, need - 1, None), "too small")
+    _refused(lib.pgc_preference_loss(*args, None, need, None), "workspace is NULL")
+    _refused(lib.pgc_preference_loss(*args, 12 * BASE + 128, need, None), "256-byte")
+    _refused(lib.pgc_preference_loss(*args, 7 * BASE, need, None), "workspace overlaps logprobs")
+    _refused(lib.pgc_preference_loss(*args, BASE, need, None), "workspace overlaps logits")
 
 
 def _policy(**change):
