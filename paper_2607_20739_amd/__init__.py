@@ -4,6 +4,9 @@ The computation lives in libpgc.so (C ABI: include/pgc.h; HIP kernels in
 csrc/).  `_lib` binds every entry point by name; `PGCSession` is plumbing that
 lets torch own the workspace memory and the stream.  There is no fallback:
 if the library is missing, every call raises.
+
+The submodule `ops` binds include/pgc_ops.h: dropout, token log-probabilities,
+the preference loss and the policy loss, to compute a partition's gradient with.
 """
 
 from ._lib import *  # noqa: F401,F403  (the C entry points, same names)
