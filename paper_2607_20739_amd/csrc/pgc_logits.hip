@@ -709,8 +709,11 @@ void long_policy_kernel(LogitsArgs a) {
 }
 
 // kBackward of longer rows: every value by itself.  A group of LANES lanes takes LANES * U vectors of
-// a row; the runs of a longer row go to different blocks.  Rows of 16-bit values that start at no
-// multiple of 4 bytes are taken from their second value on.
+// a row; the runs of a longer row go to different blocks.  Nothing is summed, so the vectors may start
+// anywhere: they start at the row's first cache line, and each value before it goes to a lane of its
+// own.  8,192 x 131,071 bf16 737 us against 774 with the vectors at the row's first multiple of 4
+// bytes and 765 at that of 16; 131,072 x 2,001 187 against 213.
+constexpr uint32_t kLine = 128;
 template <class T, int LANES, int U>
 __global__ __launch_bounds__(Place<LANES>::kThreads)
 void gradient_kernel(LogitsArgs a) {
@@ -719,41 +722,41 @@ void gradient_kernel(LogitsArgs a) {
   if (row >= a.rows) return;
   const T* z = static_cast<const T*>(a.logits) + row * a.stride;
   T* dz = static_cast<T*>(a.dlogits) + row * a.out_stride;
-  const uint32_t odd = sizeof(T) == 2 ? static_cast<uint32_t>(reinterpret_cast<uintptr_t>(z) >> 1) & 1 : 0;
+  const uint32_t head = static_cast<uint32_t>(-reinterpret_cast<uintptr_t>(z) % kLine / sizeof(T));
   const uint32_t lane = Place<LANES>::lane(), cols = static_cast<uint32_t>(a.cols);
-  const uint32_t full = (cols - odd) / kN, rem = cols - odd - full * kN, v0 = blockIdx.x * (LANES * U);
+  const uint32_t full = (cols - head) / kN, rem = cols - head - full * kN, v0 = blockIdx.x * (LANES * U);
   const int32_t y = a.targets[row];
   const float g = a.grad[row], top = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
   const RowGradient<T> grad = RowGradient<T>::of_stats(y >= 0 && y < a.cols ? g : 0.f, top, log_sum);
-  // Columns outside of the vectors: up to kN - 1 at the end, one at the start of a shifted row.
+  // Columns outside of the vectors: up to kN - 1 at the end, less than a cache line at the start.
   const uint32_t yv = static_cast<uint32_t>(y), last = cols - rem + lane;
-  const bool has_tail = blockIdx.x == gridDim.x - 1 && lane < rem, has_head = blockIdx.x == 0 && lane < odd;
+  const bool has_tail = blockIdx.x == gridDim.x - 1 && lane < rem, has_head = blockIdx.x == 0 && lane < head;
   if (grad.none) {
 #pragma unroll
     for (int i = 0; i < U; ++i)
-      if (v0 + i * LANES + lane < full) Vec<T>::store(dz + odd, v0 + i * LANES, lane, u4v{0, 0, 0, 0});
+      if (v0 + i * LANES + lane < full) Vec<T>::store(dz + head, v0 + i * LANES, lane, u4v{0, 0, 0, 0});
     if (has_tail) dz[last] = static_cast<T>(0.f);
-    if (has_head) dz[0] = static_cast<T>(0.f);
+    if (has_head) dz[lane] = static_cast<T>(0.f);
     return;
   }
-  const uint32_t target = (yv - odd) / kN - v0;   // the target's vector, and whether this lane has it
+  const uint32_t target = (yv - head) / kN - v0;   // the target's vector, and whether this lane has it
   const bool has_target = target < LANES * U && target + v0 < full && target % LANES == lane;
   u4v h[U];
   uint32_t z_target = 0, z_tail = 0, z_head = 0;
 #pragma unroll
   for (int i = 0; i < U; ++i) {
     h[i] = u4v{0, 0, 0, 0};
-    if (v0 + i * LANES + lane < full) h[i] = Vec<T>::load(z + odd, v0 + i * LANES, lane);
+    if (v0 + i * LANES + lane < full) h[i] = Vec<T>::load(z + head, v0 + i * LANES, lane);
   }
   if (has_target) z_target = Vec<T>::raw(z + yv);
   if (has_tail) z_tail = Vec<T>::raw(z + last);
-  if (has_head) z_head = Vec<T>::raw(z);
+  if (has_head) z_head = Vec<T>::raw(z + lane);
 #pragma unroll
   for (int i = 0; i < U; ++i)
-    if (v0 + i * LANES + lane < full) Vec<T>::store(dz + odd, v0 + i * LANES, lane, grad.of_vector(h[i]));
+    if (v0 + i * LANES + lane < full) Vec<T>::store(dz + head, v0 + i * LANES, lane, grad.of_vector(h[i]));
   if (has_target) dz[yv] = static_cast<T>(grad.of(Vec<T>::value(z_target), true));
   if (has_tail) dz[last] = static_cast<T>(grad.of(Vec<T>::value(z_tail), last == yv));
-  if (has_head) dz[0] = static_cast<T>(grad.of(Vec<T>::value(z_head), yv == 0));
+  if (has_head) dz[lane] = static_cast<T>(grad.of(Vec<T>::value(z_head), lane == yv));
 }
 
 // One block per kRows rows.
@@ -838,7 +841,10 @@ hipError_t launch_backward(const LogitsArgs& a, hipStream_t stream) {
   // Runs that leave few lanes of a row's last one empty: 9,000 bf16 columns (1,125 vectors) 166 us in
   // runs of 512, 209 of 1,024; 20,000 (2,500) 169 and 163.  fp32 does best with a load per lane
   // (24,000 columns 163 us, with two 176).
+  // 384 vectors and fewer: 2,501 bf16 columns 161 us in runs of 384, 168 in runs of 512; 3,501 (438) 270
+  // and 215.
   if (vectors <= 256) return launch_gradient<T, 64, 4>(a, stream);
+  if (vectors <= 384) return launch_gradient<T, 128, 3>(a, stream);
   if (vectors <= 512) return launch_gradient<T, 256, 2>(a, stream);
   if constexpr (sizeof(T) == 4) {
     if (vectors > 768) return launch_gradient<T, 256, 1>(a, stream);
