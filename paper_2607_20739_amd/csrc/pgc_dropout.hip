@@ -66,17 +66,17 @@ struct Vec {
   static __device__ __forceinline__ void store(T* row, uint32_t column, uint32_t lane, u4v v) {
     __builtin_nontemporal_store(v, reinterpret_cast<u4v_unaligned*>(const_cast<char*>(at(row, column, lane))));
   }
-  // The vector whose first value is column `word` * 4 + `odd` of the row with this key.
+  // The vector whose first value is column `word` * 4 + `shift` of the row with this key.
   template <bool kResidual>
-  static __device__ __forceinline__ u4v dropped(const DropoutArgs& a, uint64_t key, uint32_t word, bool odd, u4v x, u4v residual) {
+  static __device__ __forceinline__ u4v dropped(const DropoutArgs& a, uint64_t key, uint32_t word, uint32_t shift, u4v x, u4v residual) {
     auto f = __builtin_convertvector(__builtin_bit_cast(Packed, x), Floats);
     uint64_t bits[kN / 4];
 #pragma unroll
     for (uint32_t w = 0; w < kN / 4; ++w) bits[w] = draw(key, word + w);
-    if (kN == 8 && odd) {   // the fields one further on
-      const uint64_t next = draw(key, word + 2);
-      bits[0] = bits[0] >> 16 | bits[kN / 4 - 1] << 48;
-      bits[kN / 4 - 1] = bits[kN / 4 - 1] >> 16 | next << 48;
+    if (shift > 0) {   // the fields that many further on
+      const uint64_t next = draw(key, word + kN / 4);
+      if (kN == 8) bits[0] = bits[0] >> 16 * shift | bits[kN / 4 - 1] << (64 - 16 * shift);
+      bits[kN / 4 - 1] = bits[kN / 4 - 1] >> 16 * shift | next << (64 - 16 * shift);
     }
 #pragma unroll
     for (uint32_t k = 0; k < kN; ++k) f[k] = field(bits[k / 4], k % 4) >= a.threshold ? f[k] * a.factor : 0.f;
@@ -173,17 +173,19 @@ void short_dropout_kernel(DropoutArgs a, uint32_t rows_per_block) {
       h[i] = moved_down(h[i], (kN - rem) * sizeof(T));
       if (kResidual) r[kResidual ? i : 0] = moved_down(r[kResidual ? i : 0], (kN - rem) * sizeof(T));
     }
-    const u4v o = Vec<T>::template dropped<kResidual>(a, keys[row[i]], v[i] * (kN / 4), false, h[i], r[kResidual ? i : 0]);
+    const u4v o = Vec<T>::template dropped<kResidual>(a, keys[row[i]], v[i] * (kN / 4), 0, h[i], r[kResidual ? i : 0]);
     T* to = out + row[i] * a.out_stride;
     if (part) store_first(reinterpret_cast<char*>(to + v[i] * kN), o, rem * sizeof(T));
     else Vec<T>::store(to, v[i] * kN, 0, o);
   }
 }
 
-// Longer rows: a block takes kThreads * U vectors of a row, and of its last run the values that fill
-// no vector, one per lane.  Rows of 16-bit values that start at no multiple of 4 bytes, where loads
-// take longer, are taken from their second value on: their vectors' fields come from three draws,
-// not two.
+// Longer rows: a block takes kThreads * U vectors of a row, which start at the row's first cache
+// line, and the values that fill no vector, one per lane: the first block those before, the last one
+// those after.  The fields of vectors that start at no multiple of 4 columns come from three draws,
+// not two.  65,536 x 8,191 bf16 368 us, 390 with the vectors at the row's first multiple of 4 bytes
+// (8,192 columns: 361); 32,768 x 16,385 346 and 375.
+constexpr uint32_t kLine = 128;
 template <class T, bool kResidual, int U>
 __global__ __launch_bounds__(kThreads)
 void dropout_kernel(DropoutArgs a) {
@@ -193,13 +195,13 @@ void dropout_kernel(DropoutArgs a) {
   const T* x = static_cast<const T*>(a.x) + row * a.x_stride;
   const T* res = kResidual ? static_cast<const T*>(a.residual) + row * a.residual_stride : nullptr;
   T* out = static_cast<T*>(a.out) + row * a.out_stride;
-  const uint32_t odd = sizeof(T) == 2 ? static_cast<uint32_t>(reinterpret_cast<uintptr_t>(x) >> 1) & 1 : 0;
+  const uint32_t head = static_cast<uint32_t>(-reinterpret_cast<uintptr_t>(x) % kLine / sizeof(T));
   const uint32_t lane = threadIdx.x, cols = static_cast<uint32_t>(a.cols);
-  const uint32_t full = (cols - odd) / kN, rem = cols - odd - full * kN, v0 = blockIdx.x * (kThreads * U);
+  const uint32_t full = (cols - head) / kN, rem = cols - head - full * kN, v0 = blockIdx.x * (kThreads * U);
   u4v h[U] = {}, r[kResidual ? U : 1] = {};
 #pragma unroll
   for (int i = 0; i < U; ++i) {
-    const uint32_t column = (v0 + i * kThreads) * kN + odd;
+    const uint32_t column = (v0 + i * kThreads) * kN + head;
     if (v0 + i * kThreads + lane < full) {
       h[i] = Vec<T>::load(x, column, lane);
       if (kResidual) r[i] = Vec<T>::load(res, column, lane);
@@ -210,11 +212,11 @@ void dropout_kernel(DropoutArgs a) {
   for (int i = 0; i < U; ++i) {
     const uint32_t v = v0 + i * kThreads + lane;
     if (v < full)
-      Vec<T>::store(out, (v0 + i * kThreads) * kN + odd, lane,
-                    Vec<T>::template dropped<kResidual>(a, key, v * (kN / 4), odd != 0, h[i], r[kResidual ? i : 0]));
+      Vec<T>::store(out, (v0 + i * kThreads) * kN + head, lane,
+                    Vec<T>::template dropped<kResidual>(a, key, v * (kN / 4) + head / 4, head % 4, h[i], r[kResidual ? i : 0]));
   }
   if (blockIdx.x == gridDim.x - 1 && lane < rem) drop_value<T, kResidual>(a, key, x, res, out, cols - rem + lane);
-  if (blockIdx.x == 0 && lane < odd) drop_value<T, kResidual>(a, key, x, res, out, 0);
+  if (blockIdx.x == 0 && lane < head) drop_value<T, kResidual>(a, key, x, res, out, lane);
 }
 
 template <class T, bool kResidual>
