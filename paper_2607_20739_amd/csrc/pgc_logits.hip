@@ -14,7 +14,7 @@
 //
 // Measured (MI355X; GB of logits read and gradients written per second): forward of 16,384 rows of
 // 131,072 bf16 602 us, 7.1 TB/s; policy loss of 4,096 rows of 65,536 fp16 176 us, 5.8 TB/s; of 8,192
-// rows of 131,071 bf16 814 us, 5.3; gradient of 8,192 rows of 131,072 bf16 704 us, 6.1.  A copy of a
+// rows of 131,071 bf16 810 us, 5.3; gradient of 8,192 rows of 131,072 bf16 704 us, 6.1.  A copy of a
 // gigabyte by the runtime moves 5.0, a read alone 7.2.
 #include <hip/hip_runtime.h>
 
