@@ -288,14 +288,20 @@ def policy_loss(logits, targets, old_logprobs, advantages, ref_logprobs=None, cl
 # ---- autograd -------------------------------------------------------------------------------
 
 class _Dropout(torch.autograd.Function):
+    """Linear in x and residual, so the gradient is a dropout that has one itself."""
+
     @staticmethod
     def forward(ctx, x, residual, p, seed, row_ids, first_row):
-        ctx.args = (p, seed, row_ids, first_row)
+        ctx.args = p, seed, first_row
+        ctx.save_for_backward(row_ids)
         return _dropout("pgc_dropout", x, p, seed, residual, row_ids, first_row, None)
 
     @staticmethod
     def backward(ctx, dout):
-        dx = dropout_backward(dout.contiguous(), *ctx.args) if ctx.needs_input_grad[0] else None
+        dx = None
+        if ctx.needs_input_grad[0]:
+            p, seed, first_row = ctx.args
+            dx = dropout(dout.contiguous(), p, seed, row_ids=ctx.saved_tensors[0], first_row=first_row)
         return dx, dout if ctx.needs_input_grad[1] else None, None, None, None, None
 
 
@@ -312,4 +318,16 @@ class _TokenLogprobs(torch.autograd.Function):
     @staticmethod
     def backward(ctx, grad, _):
         logits, targets, stats = ctx.saved_tensors
-        return token_logprobs_backward(logits, targets, stats, grad.contiguous()), None
+        return _TokenLogprobsGradient.apply(logits, targets, stats, grad.contiguous()), None
+
+
+class _TokenLogprobsGradient(torch.autograd.Function):
+    """A gradient that has none itself: a graph of it can be made, but not gone back through."""
+
+    @staticmethod
+    def forward(ctx, logits, targets, stats, grad):
+        return token_logprobs_backward(logits, targets, stats, grad)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("the gradient of token_logprobs is not differentiable")

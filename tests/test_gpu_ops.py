@@ -620,6 +620,30 @@ def test_autograd_and_differences():
     assert abs((_np(got) * v).sum() - d) < tol
 
 
+def test_second_gradients():
+    """Dropout is linear: its gradient has dropout's own as gradient, bit for bit.  That of the
+    log-probabilities has none and says so, and a mask's row numbers may not change on the way."""
+    _say("second gradients")
+    x = torch.randn(6, 40, device="cuda", requires_grad=True)
+    c = torch.randn(6, 40, device="cuda", requires_grad=True)
+    v = torch.randn(6, 40, device="cuda")
+    ids = torch.tensor([5, 3, 9, 0, 2, 7], device="cuda")
+    y = ops.dropout(x, 0.25, 3, row_ids=ids)
+    dx, = torch.autograd.grad(y, x, c, create_graph=True)
+    assert torch.equal(dx, ops.dropout_backward(c.detach(), 0.25, 3, row_ids=ids))
+    dc, = torch.autograd.grad(dx, c, v)
+    assert torch.equal(dc, ops.dropout(v, 0.25, 3, row_ids=ids))
+    y = ops.dropout(x, 0.25, 3, row_ids=ids)
+    ids += 1
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        y.sum().backward()
+    z = torch.randn(6, 40, device="cuda", requires_grad=True)
+    lp, _ = ops.token_logprobs(z, torch.zeros(6, dtype=torch.int32, device="cuda"))
+    dz, = torch.autograd.grad(lp.sum(), z, create_graph=True)
+    with pytest.raises(RuntimeError, match="not differentiable"):
+        dz.sum().backward()
+
+
 def test_the_binding_refuses_what_does_not_fit():
     _say("refusals")
     z = torch.randn(6, 40, device="cuda")
