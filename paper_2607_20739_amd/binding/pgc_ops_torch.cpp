@@ -1,0 +1,329 @@
+// Calls of the language-model operators (include/pgc_ops.h) on torch's tensors: checks them,
+// allocates the results and passes addresses on.  A compiled module rather than ctypes, because the
+// small calls wait for the host: a kernel of 3 to 8 us is enqueued in 3.5, and the same checks and
+// allocations take 4 to 9 us in Python.
+//
+// Functions take all arguments, by position; ops.py gives them their names and defaults.  Tensors
+// that do not fit raise ValueError, what the library refuses raises PGCError.
+#define PY_SSIZE_T_CLEAN
+#include <Python.h>
+
+#include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
+#include <c10/core/DeviceGuard.h>
+#include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/utils/object_ptr.h>
+
+#include <initializer_list>
+
+#include "pgc_ops.h"
+
+namespace {
+
+PyObject* g_raw_stream = nullptr;   // torch's function from a GPU's index to its current stream
+PyObject* g_error = nullptr;        // PGCError
+
+// dtype of a matrix as the library numbers it, -1 for others.
+int dtype_of(const at::Tensor& t) {
+  switch (t.scalar_type()) {
+    case at::kFloat: return PGC_F32;
+    case at::kBFloat16: return PGC_BF16;
+    case at::kHalf: return PGC_F16;
+    default: return -1;
+  }
+}
+
+const at::Tensor& tensor(const char* name, PyObject* o) {
+  TORCH_CHECK_VALUE(THPVariable_Check(o), name, " must be a tensor");
+  return THPVariable_Unpack(o);
+}
+
+// Row stride of a matrix whose shape has been looked at.
+int64_t row_stride(const char* name, const at::Tensor& t) {
+  const int64_t rows = t.size(0), cols = t.size(1);
+  TORCH_CHECK_VALUE(t.stride(1) == 1 || cols <= 1, "the columns of ", name, " must be adjacent");
+  if (rows <= 1) return cols;
+  TORCH_CHECK_VALUE(t.stride(0) >= cols, "the rows of ", name, " must not overlap");
+  return t.stride(0);
+}
+
+struct Matrix {
+  at::Tensor t;
+  int64_t rows, cols, stride;
+  int dtype;
+
+  Matrix(const char* name, PyObject* o) : t(tensor(name, o)), dtype(dtype_of(t)) {
+    TORCH_CHECK_VALUE(t.dim() == 2 && dtype >= 0 && t.is_cuda() && t.layout() == at::kStrided,
+                      name, " must be a 2-D float32, bfloat16 or float16 tensor on the GPU");
+    rows = t.size(0);
+    cols = t.size(1);
+    stride = row_stride(name, t);
+  }
+  void* data() const { return t.data_ptr(); }
+  pgc_logits logits() const { return {data(), rows, cols, stride, dtype}; }
+  at::Tensor empty(at::IntArrayRef shape, at::ScalarType type) const { return at::empty(shape, t.options().dtype(type)); }
+
+  // Of this one's shape, type and GPU.
+  int64_t like(const char* name, const at::Tensor& other) const {
+    TORCH_CHECK_VALUE(other.sizes() == t.sizes() && other.scalar_type() == t.scalar_type() && other.device() == t.device(),
+                      name, " must have the shape, dtype and device ", t.sizes(), ", ", t.scalar_type(), ", ", t.device());
+    return row_stride(name, other);
+  }
+  // Address of a contiguous array on this one's GPU; null for None.
+  void* array(const char* name, PyObject* o, at::ScalarType type, at::IntArrayRef shape) const {
+    if (o == Py_None) return nullptr;
+    const at::Tensor& a = tensor(name, o);
+    TORCH_CHECK_VALUE(a.scalar_type() == type && a.sizes() == shape && a.device() == t.device() && a.is_contiguous(),
+                      name, " must be a contiguous ", type, " tensor of shape ", shape, " on ", t.device());
+    return a.data_ptr();
+  }
+  float* floats(const char* name, PyObject* o, int64_t count) const {
+    return static_cast<float*>(array(name, o, at::kFloat, {count}));
+  }
+  int32_t* ints(const char* name, PyObject* o, int64_t count) const {
+    return static_cast<int32_t*>(array(name, o, at::kInt, {count}));
+  }
+};
+
+// The tensor that receives a result of a matrix's shape: `o`, or a new one for None.
+struct Output {
+  at::Tensor t;
+  int64_t stride;
+
+  Output(const Matrix& like, PyObject* o) {
+    if (o == Py_None) {
+      t = like.empty({like.rows, like.cols}, like.t.scalar_type());
+      stride = like.cols;
+    } else {
+      t = tensor("out", o);
+      stride = like.like("out", t);
+      if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();   // autograd notices a saved tensor that this changes
+    }
+  }
+};
+
+double number(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) throw python_error();
+  return v;
+}
+
+// The low 64 bits.
+uint64_t integer(PyObject* o) {
+  const unsigned long long v = PyLong_AsUnsignedLongLongMask(o);
+  if (v == ~0ull && PyErr_Occurred()) throw python_error();
+  return v;
+}
+
+bool flag(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw python_error();
+  return v != 0;
+}
+
+void check(int status) {
+  if (status == PGC_OK) return;
+  THPObjectPtr args(Py_BuildValue("(is)", status, pgc_ops_last_error()));
+  if (args) PyErr_SetObject(g_error, args.get());
+  throw python_error();
+}
+
+// Calls an entry point on torch's current stream of the GPU that `like` is on.
+template <class Call>
+void launch(const Matrix& like, Call call) {
+  const c10::Device device = like.t.device();
+  THPObjectPtr index(PyLong_FromLong(device.index()));
+  THPObjectPtr stream(index ? PyObject_CallOneArg(g_raw_stream, index.get()) : nullptr);
+  if (!stream) throw python_error();
+  void* handle = PyLong_AsVoidPtr(stream.get());
+  if (handle == nullptr && PyErr_Occurred()) throw python_error();
+  const c10::DeviceGuard guard(device);
+  int status;
+  Py_BEGIN_ALLOW_THREADS
+  status = call(handle);
+  Py_END_ALLOW_THREADS
+  check(status);
+}
+
+PyObject* tuple(std::initializer_list<at::Tensor> tensors) {
+  THPObjectPtr out(PyTuple_New(static_cast<Py_ssize_t>(tensors.size())));
+  if (!out) throw python_error();
+  Py_ssize_t i = 0;
+  for (const at::Tensor& t : tensors) {
+    PyObject* o = t.defined() ? THPVariable_Wrap(t) : Py_NewRef(Py_None);
+    if (o == nullptr) throw python_error();
+    PyTuple_SET_ITEM(out.get(), i++, o);
+  }
+  return out.release();
+}
+
+void expect(Py_ssize_t n, Py_ssize_t want) { TORCH_CHECK_TYPE(n == want, "expected ", want, " arguments, got ", n); }
+
+PyObject* dropout_by(int (*entry)(const pgc_dropout_args*, void*), PyObject* const* a, Py_ssize_t n) {
+  expect(n, 7);
+  const Matrix x("x", a[0]);
+  pgc_dropout_args k{};
+  if (a[3] != Py_None) {
+    const at::Tensor& residual = tensor("residual", a[3]);
+    k.residual_stride = x.like("residual", residual);
+    k.residual = residual.data_ptr();
+  }
+  k.row_ids = static_cast<int64_t*>(x.array("row_ids", a[4], at::kLong, {x.rows}));
+  k.p = number(a[1]);
+  k.seed = integer(a[2]);
+  k.first_row = static_cast<int64_t>(integer(a[5]));
+  const Output out(x, a[6]);
+  k.x = x.data();
+  k.out = out.t.data_ptr();
+  k.rows = x.rows;
+  k.cols = x.cols;
+  k.x_stride = x.stride;
+  k.out_stride = out.stride;
+  k.dtype = x.dtype;
+  launch(x, [&](void* stream) { return entry(&k, stream); });
+  return THPVariable_Wrap(out.t);
+}
+
+// x, p, seed, residual, row_ids, first_row, out
+PyObject* dropout(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  return dropout_by(pgc_dropout, a, n);
+  END_HANDLE_TH_ERRORS
+}
+
+PyObject* dropout_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  return dropout_by(pgc_dropout_backward, a, n);
+  END_HANDLE_TH_ERRORS
+}
+
+// logits, targets
+PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  expect(n, 2);
+  const Matrix x("logits", a[0]);
+  const int32_t* targets = x.ints("targets", a[1], x.rows);
+  const at::Tensor logprobs = x.empty({x.rows}, at::kFloat), stats = x.empty({x.rows, 2}, at::kFloat);
+  const pgc_logits z = x.logits();
+  launch(x, [&](void* stream) {
+    return pgc_token_logprobs(&z, targets, static_cast<float*>(logprobs.data_ptr()), static_cast<float*>(stats.data_ptr()), stream);
+  });
+  return tuple({logprobs, stats});
+  END_HANDLE_TH_ERRORS
+}
+
+// logits, targets, stats, grad, out
+PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  expect(n, 5);
+  const Matrix x("logits", a[0]);
+  const int32_t* targets = x.ints("targets", a[1], x.rows);
+  const float* stats = static_cast<float*>(x.array("stats", a[2], at::kFloat, {x.rows, 2}));
+  const float* grad = x.floats("grad", a[3], x.rows);
+  const Output out(x, a[4]);
+  const pgc_logits z = x.logits();
+  launch(x, [&](void* stream) { return pgc_token_logprobs_backward(&z, targets, stats, grad, out.t.data_ptr(), out.stride, stream); });
+  return THPVariable_Wrap(out.t);
+  END_HANDLE_TH_ERRORS
+}
+
+// logits, targets, offsets, ref_logprobs, beta, label_smoothing, scale, pair_weights, gradient, out, workspace
+PyObject* preference_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  expect(n, 11);
+  const Matrix x("logits", a[0]);
+  const pgc_logits z = x.logits();
+  pgc_preference_args k{};
+  k.targets = x.ints("targets", a[1], x.rows);
+  k.pairs = (tensor("offsets", a[2]).numel() - 1) / 2;
+  k.offsets = x.ints("offsets", a[2], 2 * k.pairs + 1);
+  k.ref_logprobs = x.floats("ref_logprobs", a[3], x.rows);
+  k.beta = number(a[4]);
+  k.label_smoothing = number(a[5]);
+  k.scale = number(a[6]);
+  k.pair_weights = x.floats("pair_weights", a[7], k.pairs);
+  at::Tensor workspace;
+  size_t bytes = 0;
+  void* at_workspace = nullptr;
+  if (a[10] == Py_None) {
+    check(pgc_preference_workspace_bytes(&z, k.pairs, &bytes));
+    if (bytes > 0) {
+      workspace = x.empty({static_cast<int64_t>(bytes)}, at::kByte);
+      at_workspace = workspace.data_ptr();
+    }
+  } else {
+    const at::Tensor& given = tensor("workspace", a[10]);
+    at_workspace = x.array("workspace", a[10], at::kByte, given.sizes());
+    bytes = static_cast<size_t>(given.numel());
+  }
+  const at::Tensor loss = x.empty({k.pairs}, at::kFloat), margins = x.empty({k.pairs}, at::kFloat);
+  const at::Tensor logprobs = x.empty({x.rows}, at::kFloat);
+  at::Tensor dlogits;
+  if (flag(a[8])) {
+    const Output out(x, a[9]);
+    dlogits = out.t;
+    k.dlogits = dlogits.data_ptr();
+    k.dlogits_stride = out.stride;
+  }
+  k.loss = static_cast<float*>(loss.data_ptr());
+  k.margins = static_cast<float*>(margins.data_ptr());
+  k.logprobs = static_cast<float*>(logprobs.data_ptr());
+  launch(x, [&](void* stream) { return pgc_preference_loss(&z, &k, at_workspace, bytes, stream); });
+  return tuple({loss, margins, logprobs, dlogits});
+  END_HANDLE_TH_ERRORS
+}
+
+// logits, targets, old_logprobs, advantages, ref_logprobs, clip_low, clip_high, kl, scale, token_weights, gradient, out
+PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  expect(n, 12);
+  const Matrix x("logits", a[0]);
+  const pgc_logits z = x.logits();
+  pgc_policy_args k{};
+  k.targets = x.ints("targets", a[1], x.rows);
+  k.old_logprobs = x.floats("old_logprobs", a[2], x.rows);
+  k.advantages = x.floats("advantages", a[3], x.rows);
+  k.ref_logprobs = x.floats("ref_logprobs", a[4], x.rows);
+  k.clip_low = number(a[5]);
+  k.clip_high = number(a[6]);
+  k.kl = number(a[7]);
+  k.scale = number(a[8]);
+  k.token_weights = x.floats("token_weights", a[9], x.rows);
+  const at::Tensor loss = x.empty({x.rows}, at::kFloat), logprobs = x.empty({x.rows}, at::kFloat);
+  at::Tensor dlogits;
+  if (flag(a[10])) {
+    const Output out(x, a[11]);
+    dlogits = out.t;
+    k.dlogits = dlogits.data_ptr();
+    k.dlogits_stride = out.stride;
+  }
+  k.loss = static_cast<float*>(loss.data_ptr());
+  k.logprobs = static_cast<float*>(logprobs.data_ptr());
+  launch(x, [&](void* stream) { return pgc_policy_loss(&z, &k, stream); });
+  return tuple({loss, logprobs, dlogits});
+  END_HANDLE_TH_ERRORS
+}
+
+template <class F>
+constexpr PyMethodDef method(const char* name, F f) {
+  return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr};
+}
+
+PyObject* imported(const char* module, const char* name) {
+  THPObjectPtr m(PyImport_ImportModule(module));
+  return m ? PyObject_GetAttrString(m.get(), name) : nullptr;
+}
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__ops_torch(void) {
+  static PyMethodDef methods[] = {
+      method("dropout", dropout), method("dropout_backward", dropout_backward), method("token_logprobs", token_logprobs),
+      method("token_logprobs_backward", token_logprobs_backward), method("preference_loss", preference_loss),
+      method("policy_loss", policy_loss), {nullptr, nullptr, 0, nullptr}};
+  static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+  if (g_raw_stream == nullptr) g_raw_stream = imported("torch._C", "_cuda_getCurrentRawStream");
+  if (g_error == nullptr && g_raw_stream) g_error = imported("paper_2607_20739_amd._lib", "PGCError");
+  return g_error ? PyModule_Create(&module) : nullptr;
+}

@@ -1,4 +1,5 @@
-"""Build libpgc.so (the C-ABI library of include/pgc.h) for gfx950 with hipcc.
+"""Build libpgc.so (the C-ABI library of include/pgc.h and pgc_ops.h) for gfx950 with hipcc, and the
+Python module that calls its operators on torch's tensors with g++.
 
 Usage: python -m paper_2607_20739_amd.build   (or build() from Python)
 
@@ -9,7 +10,8 @@ Every HIP and C++ source under csrc/ is compiled with
 the host pass reports the feature as unknown, which is harmless and not shown;
 other warnings go to stderr) and linked
 into paper_2607_20739_amd/libpgc.so next to this file, linked against ROCm's
-roctx library for the per-step profiler ranges.
+roctx library for the per-step profiler ranges.  binding/pgc_ops_torch.cpp becomes
+paper_2607_20739_amd/_ops_torch.so, linked against that library and the installed torch.
 """
 
 import concurrent.futures
@@ -17,6 +19,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -24,6 +27,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libpgc.so")
+BINDING = os.path.join(PKG, "binding", "pgc_ops_torch.cpp")
+BINDING_LIB = os.path.join(PKG, "_ops_torch.so")
 SOURCES = sorted(f for f in os.listdir(CSRC) if f.endswith((".cpp", ".hip")))
 ARCH = "gfx950"
 ROCM_LIB = "/opt/rocm/lib"   # librocprofiler-sdk-roctx (per-step profiler ranges)
@@ -49,31 +54,49 @@ def warnings(stderr):
             and not line.endswith("generated when compiling for %s." % ARCH)]
 
 
-def _compile(src):
-    obj = os.path.join(BUILD_DIR, os.path.basename(src) + ".o")
-    cmd = [hipcc()] + common_flags() + ["-c", os.path.join(CSRC, src), "-o", obj]
+def binding_flags():
+    import torch
+    include = os.path.join(os.path.dirname(torch.__file__), "include")
+    return ["-O2", "-std=c++17", "-fPIC", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI,
+            "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"),
+            "-isystem", sysconfig.get_paths()["include"], "-I", INCLUDE]
+
+
+def _run(what, cmd):
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
-        raise RuntimeError("compiling %s failed:\n%s\n%s" % (src, " ".join(cmd), res.stderr))
+        raise RuntimeError("%s failed:\n%s\n%s" % (what, " ".join(cmd), res.stderr))
     for line in warnings(res.stderr):
         print(line, file=sys.stderr)
+
+
+def _compile(src):
+    obj = os.path.join(BUILD_DIR, os.path.basename(src) + ".o")
+    cmd = ["g++"] + binding_flags() if src == BINDING else [hipcc()] + common_flags()
+    _run("compiling " + src, cmd + ["-c", os.path.join(CSRC, src), "-o", obj])
     return obj
 
 
+def _link(what, lib, cmd):
+    tmp = lib + ".tmp"
+    _run("linking " + what, cmd + ["-shared", "-fPIC", "-o", tmp])
+    os.replace(tmp, lib)
+
+
 def build(verbose=False):
-    """Compile and link libpgc.so; returns its path."""
+    """Compile and link libpgc.so and the torch binding; returns libpgc.so's path."""
+    import torch
     os.makedirs(BUILD_DIR, exist_ok=True)
-    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES)) as pool:
-        objs = list(pool.map(_compile, SOURCES))
-    tmp = LIB + ".tmp"
-    cmd = [hipcc(), "--offload-arch=" + ARCH, "-shared", "-fPIC", "-o", tmp] + objs + [
-        "-L" + ROCM_LIB, "-Wl,-rpath," + ROCM_LIB, "-lrocprofiler-sdk-roctx"]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("linking libpgc.so failed:\n%s\n%s" % (" ".join(cmd), res.stderr))
-    os.replace(tmp, LIB)
+    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as pool:
+        *objs, binding = pool.map(_compile, SOURCES + [BINDING])
+    _link("libpgc.so", LIB, [hipcc(), "--offload-arch=" + ARCH] + objs +
+          ["-L" + ROCM_LIB, "-Wl,-rpath," + ROCM_LIB, "-lrocprofiler-sdk-roctx"])
+    torch_lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    _link("_ops_torch.so", BINDING_LIB, ["g++", binding, "-L" + PKG, "-lpgc", "-Wl,-rpath,$ORIGIN", "-L" + torch_lib,
+                                         "-lc10", "-ltorch_cpu", "-ltorch_python"])
     if verbose:
         print("built", LIB)
+        print("built", BINDING_LIB)
     return LIB
 
 

@@ -623,7 +623,7 @@ __device__ __forceinline__ RowGradient<T> finish_policy_row(const LogitsArgs& a,
 // From the sum to the gradient a lane keeps its first HOLD vectors in registers and the next STAGE
 // in LDS, where they are loaded without passing through registers; the rest of a row that is
 // longer still is read again.  8 waves of 16 + 9 vectors hold 102,400 16-bit values at two blocks
-// to a CU: rows of 131,072 bf16 take 750 us so, 805 held whole by one block of 16 waves.
+// to a CU: rows of 131,072 bf16 take 741 us so, 805 held whole by one block of 16 waves.
 template <class T, int WAVES, int HOLD, int STAGE>
 __global__ __launch_bounds__(Place<WAVES * kWave>::kThreads)
 void long_policy_kernel(LogitsArgs a) {

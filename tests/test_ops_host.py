@@ -13,6 +13,7 @@ import pytest
 import torch
 
 import paper_2607_20739_amd as P
+from paper_2607_20739_amd import build as B
 from paper_2607_20739_amd import ops
 from oracle import ops as O
 from oracle import rng as R
@@ -323,3 +324,24 @@ def test_tensors_off_the_gpu_are_refused():
                  lambda: ops.preference_loss(x, y, y)):
         with pytest.raises(ValueError, match="GPU"):
             call()
+
+
+def test_the_binding_refuses_tensors_off_the_gpu():
+    """The compiled binding is built, takes nothing but tensors on the GPU, and says why."""
+    z, y, f = torch.zeros(3, 4), torch.zeros(3, dtype=torch.int32), torch.zeros(3)
+    for call, what in [(lambda: ops.dropout(z, 0.1, 1), "x must be"), (lambda: ops.dropout_backward(z, 0.1, 1), "x must be"),
+                       (lambda: ops.token_logprobs(z, y), "logits must be"),
+                       (lambda: ops.token_logprobs_backward(z, y, f, f), "logits must be"),
+                       (lambda: ops.preference_loss(z, y, y), "logits must be"),
+                       (lambda: ops.policy_loss(z, y, f, f), "logits must be")]:
+        with pytest.raises(ValueError, match=what):
+            call()
+    with pytest.raises(ValueError, match="logits must be a tensor"):
+        ops.policy_loss(None, y, f, f)
+
+
+def test_the_binding_compiles_without_warnings():
+    if shutil.which("g++") is None:
+        pytest.skip("g++ is not available")
+    res = subprocess.run(["g++"] + B.binding_flags() + ["-fsyntax-only", B.BINDING], capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0 and "warning" not in res.stderr, res.stderr[-2000:]
