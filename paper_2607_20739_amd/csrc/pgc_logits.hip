@@ -1018,11 +1018,11 @@ void small_preference_kernel(LogitsArgs a, PairArgs p) {
   }
 }
 
-// Logits of up to so many bytes, and so many per pair, go through one launch: 16 pairs of 64 rows of 1,000
-// bf16 (128 KiB each) 14.9 us instead of the 19.2 that three launches take; but of 256 rows 24.7
-// instead of 19.2, and one pair of 256 rows 43.  Whatever the pairs' lengths, a CU that takes all
-// rows is done in 90 us.
-constexpr int64_t kSmallBytes = int64_t{1} << 20, kSmallPairBytes = int64_t{128} << 10;
+// So many logits, and so many per pair, go through one launch, in which a pair has but one CU: 8 pairs of
+// 32 rows of 1,000 bf16 9.4 us instead of the 13.8 that three launches take (in a graph 9.0 and 9.3),
+// fp32 11.3 and 13.8 (10.9 and 9.2); of 64 rows of bf16 14.1 and 14.0 (13.7 and 9.5).  Whatever the
+// pairs' lengths, a CU that takes all rows is done in 0.12 ms.
+constexpr int64_t kSmallLogits = int64_t{1} << 19, kSmallPairLogits = int64_t{1} << 15;
 
 template <class T>
 hipError_t launch_small(const LogitsArgs& a, const PairArgs& p, hipStream_t stream) {
@@ -1061,7 +1061,7 @@ hipError_t launch_pairs(const PairArgs& a, hipStream_t stream) {
 bool preference_is_small(int64_t rows, int64_t cols, int64_t pairs, int dtype) {
   const int64_t row_bytes = cols * (dtype == PGC_F32 ? 4 : 2);
   return pairs > 0 && pairs <= kSmallRows && rows <= kSmallRows && row_bytes < 513 * 16 &&
-         rows * row_bytes <= std::min(kSmallBytes, kSmallPairBytes * pairs);
+         rows * cols <= std::min(kSmallLogits, kSmallPairLogits * pairs);
 }
 
 hipError_t launch_small_preference(const LogitsArgs& a, const PairArgs& p, int dtype, hipStream_t stream) {
