@@ -262,6 +262,167 @@ __device__ __forceinline__ void write_forward(const LogitsArgs& a, int64_t row, 
   if (a.zero_grad) a.zero_grad[row] = 0.f;
 }
 
+// A pair's rows: sequence 2 i is [at[0], at[1]), sequence 2 i + 1 [at[1], at[2]).
+struct PairRows {
+  int64_t at[3];
+
+  __device__ __forceinline__ PairRows(const PairArgs& a, int64_t pair) {
+    for (int k = 0; k < 3; ++k) at[k] = std::min<int64_t>(std::max<int64_t>(a.offsets[2 * pair + k], 0), a.rows);
+  }
+};
+
+// The gradient of the preferred rows' log-probabilities (the others' is the negative), in 64 bits, from
+// the pair's sum of l - ref, preferred rows less the others; kWrite: writes the loss and the margin, too.
+template <bool kWrite>
+__device__ __forceinline__ float pair_slope(const PairArgs& a, int64_t pair, double sum, bool writes) {
+  const double h = sum * a.beta;
+  const double e = exp(-fabs(h)), small = e / (1.0 + e);   // sigma(-|h|)
+  if (kWrite && writes) {
+    const double rest = log1p(e), minus = rest + fmax(-h, 0.0), plus = rest + fmax(h, 0.0);   // -ln sigma(h), -ln sigma(-h)
+    a.margins[pair] = static_cast<float>(h);
+    a.loss[pair] = static_cast<float>(h != h ? h : (1.0 - a.smoothing) * minus + a.smoothing * plus);
+  }
+  const double weight = a.weights ? a.weights[pair] : 1.f;
+  const double large = 1.0 / (1.0 + e), up = h >= 0 ? large : small, down = h >= 0 ? small : large;
+  const double slope = h != h ? h : a.smoothing * up - (1.0 - a.smoothing) * down;
+  return weight == 0.0 ? 0.f : static_cast<float>(slope * a.beta * a.scale * weight);
+}
+
+// A pair's sum runs in a fixed order, whoever adds it up: kPairWaves waves' lanes take four neighbouring
+// rows at a time, each adds up its own, then the lanes of a wave, then the waves one after the other.
+constexpr int kPairThreads = 1024, kPairWaves = kPairThreads / kWave;
+typedef float f4_unaligned __attribute__((ext_vector_type(4), aligned(4)));
+typedef int32_t i4_unaligned __attribute__((ext_vector_type(4), aligned(4)));
+
+// Four rows' part of the sum, from row t of the pair's on.
+struct FourRows {
+  i4_unaligned y;
+  f4_unaligned lp, ref;
+
+  __device__ __forceinline__ void load(const PairArgs& a, const PairRows& rows, int64_t t) {
+    y = i4_unaligned{-1, -1, -1, -1};
+    lp = ref = f4_unaligned{0.f, 0.f, 0.f, 0.f};
+    if (t + 4 <= rows.at[2]) {
+      y = *reinterpret_cast<const i4_unaligned*>(a.targets + t);
+      lp = *reinterpret_cast<const f4_unaligned*>(a.logprobs + t);
+      if (a.ref_logprobs) ref = *reinterpret_cast<const f4_unaligned*>(a.ref_logprobs + t);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        if (t + k >= rows.at[2]) break;
+        y[k] = a.targets[t + k];
+        lp[k] = a.logprobs[t + k];
+        if (a.ref_logprobs) ref[k] = a.ref_logprobs[t + k];
+      }
+    }
+  }
+  __device__ __forceinline__ void add(const PairArgs& a, const PairRows& rows, int64_t t, double& sum) const {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (y[k] < 0 || y[k] >= a.cols) continue;
+      const double v = static_cast<double>(lp[k]) - ref[k];
+      sum += t + k < rows.at[1] ? v : -v;
+    }
+  }
+};
+
+__device__ __forceinline__ double add_lanes(double sum) {
+  for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d, kWave);
+  return sum;
+}
+
+// By a block of kPairThreads; the first wave writes the loss and the margin, all threads get the slope.
+struct PairSums {
+  double sums[kPairWaves];
+  float slope;
+};
+template <class Add>
+__device__ __forceinline__ float block_pair_slope(const PairArgs& a, int64_t pair, const PairRows& rows, PairSums& shared, Add add) {
+  double sum = 0.0;
+#pragma unroll 2
+  for (int64_t t = rows.at[0] + 4 * threadIdx.x; t < rows.at[2]; t += 4 * kPairThreads) add(t, sum);
+  sum = add_lanes(sum);
+  if (threadIdx.x % kWave == 0) shared.sums[threadIdx.x / kWave] = sum;
+  __syncthreads();
+  if (threadIdx.x < kWave) {   // one wave: the 64-bit functions of all 16 take 1 us more
+    double h = 0.0;
+    for (int w = 0; w < kPairWaves; ++w) h += shared.sums[w];
+    const float slope = pair_slope<true>(a, pair, h, threadIdx.x == 0);
+    if (threadIdx.x == 0) shared.slope = slope;
+  }
+  __syncthreads();
+  return shared.slope;
+}
+
+// By one wave, of at most 4 * kPairThreads rows; two waves' rows at a time are in flight.
+__device__ __forceinline__ double wave_pair_sum(const PairArgs& a, const PairRows& rows) {
+  const uint32_t lane = threadIdx.x % kWave;
+  double h = 0.0;
+  for (int w = 0; w < kPairWaves; w += 2) {
+    const int64_t t0 = rows.at[0] + 4 * (w * kWave + lane), t1 = t0 + 4 * kWave;
+    if (rows.at[0] + 4 * w * kWave >= rows.at[2]) break;   // the others' sums are 0
+    FourRows r0, r1;
+    r0.load(a, rows, t0);
+    r1.load(a, rows, t1);
+    double sum0 = 0.0, sum1 = 0.0;
+    r0.add(a, rows, t0, sum0);
+    r1.add(a, rows, t1, sum1);
+    h += add_lanes(sum0);
+    h += add_lanes(sum1);
+  }
+  return h;
+}
+
+// How many of the offsets are at most `row`, by a wave: each step looks at 64 of them.
+__device__ __forceinline__ int64_t offsets_up_to(const PairArgs& a, int64_t row) {
+  const uint32_t lane = threadIdx.x % kWave;
+  int64_t from = 0, count = 2 * a.pairs + 1;
+  while (true) {
+    const int64_t step = (count + kWave - 1) / kWave, at = lane * step;
+    const uint64_t below = __ballot(at < count && a.offsets[from + (at < count ? at : 0)] <= row);
+    const int64_t n = __popcll(below);
+    if (step == 1 || n == 0) return from + n;
+    from += (n - 1) * step;
+    count = std::min(count - (n - 1) * step, step);
+  }
+}
+
+// Where the gradient kernels take a row's factor from: memory, or the row's pair.  A wave calls with
+// the rows [first, end) that its lanes have, and each lane's own.
+struct GivenFactors {
+  static constexpr bool kPairs = false;
+};
+struct PairFactors {
+  static constexpr bool kPairs = true;
+  PairArgs p;
+
+  __device__ __forceinline__ float operator()(int64_t first, int64_t end, int64_t row) const {
+    float g = 0.f;
+    for (int64_t r = first; r < end;) {
+      const int64_t n = offsets_up_to(p, r);
+      if (n > 2 * p.pairs) break;                              // past the last pair
+      if (n == 0) {                                            // before the first
+        r = std::max<int64_t>(r + 1, p.offsets[0]);
+        continue;
+      }
+      const int64_t pair = (n - 1) / 2;
+      const PairRows rows(p, pair);
+      const float slope = pair_slope<false>(p, pair, wave_pair_sum(p, rows), false);
+      if (row >= r && row < rows.at[2]) g = row < rows.at[1] ? slope : -slope;
+      r = std::max(r + 1, rows.at[2]);
+    }
+    return g;
+  }
+  // The pair's loss and margin.
+  __device__ __forceinline__ void write(int64_t pair) const {
+    const PairRows rows(p, pair);
+    pair_slope<true>(p, pair, wave_pair_sum(p, rows), threadIdx.x % kWave == 0);
+  }
+};
+
+int64_t pairs_of(const GivenFactors&) { return 0; }
+int64_t pairs_of(const PairFactors& f) { return f.p.pairs; }
+
 // A short row as one of LANES lanes sees it: its vectors are lane, lane + LANES, ..., HOLD of them.
 // The row's last vector ends with the row and may overlap the one before it (both have the same
 // gradient; in the sums only one counts the values that both hold).
@@ -311,23 +472,35 @@ struct ShortRow {
   }
 };
 
+// How many waves have a row of `rows` short ones.
+template <int LANES>
+__host__ __device__ __forceinline__ int64_t short_row_waves(int64_t rows) { return (rows + kWave / LANES - 1) / (kWave / LANES); }
+
 // All modes for short rows, 64 / LANES of them to a wave.  What bounds them is the number of
 // instructions: few lanes per row, each with several vectors, spare the joins and the row's own
 // arithmetic (1,048,576 rows of 100 bf16, 13 vectors, on 16 lanes: forward 79 us; on 4: 46).  Their
 // stores would scatter (policy loss 120 us), so a row's gradient goes through LDS to as many
 // lanes as it has vectors (84 us, 5.0 TB/s).
-template <class T, RowMode kMode, int LANES, int HOLD>
+template <class T, RowMode kMode, int LANES, int HOLD, class Factors>
 __global__ __launch_bounds__(kBlock)
-void short_row_kernel(LogitsArgs a) {
+void short_row_kernel(LogitsArgs a, Factors factors) {
   constexpr uint32_t kN = Vec<T>::kN, kRows = kWave / LANES;
   const ShortRow<T, LANES, HOLD> at(static_cast<uint32_t>(a.cols));
   constexpr bool kPolicy = kMode == RowMode::kPolicy, kForward = kMode == RowMode::kForward;
   constexpr bool kTurn = !kForward && HOLD > 1;
   __shared__ u4v turned[kTurn ? kBlock * HOLD : 1];
   const uint32_t vectors = at.vectors;
-  const int64_t row = Place<LANES>::row(static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x);
+  const int64_t block = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x, row = Place<LANES>::row(block);
+  const int64_t wave = block * (kBlock / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), first = wave * kRows;
+  if constexpr (Factors::kPairs) {   // the waves after the last row's take a pair each
+    const int64_t pair = wave - short_row_waves<LANES>(a.rows);
+    if (pair >= 0) {
+      if (pair < factors.p.pairs) factors.write(pair);
+      return;
+    }
+  }
   const bool there = row < a.rows;
-  if (!kTurn && !there) return;
+  if (!kTurn && !Factors::kPairs && !there) return;
   const T* z = static_cast<const T*>(a.logits) + row * a.stride;
   const int32_t y = there ? a.targets[row] : -1;
   u4v h[HOLD];
@@ -342,11 +515,11 @@ void short_row_kernel(LogitsArgs a) {
   }
   if constexpr (kMode == RowMode::kBackward) {
     if (counts) {
-      g = a.grad[row];
+      if constexpr (!Factors::kPairs) g = a.grad[row];
       s.top = a.stats[2 * row];
       log_sum = a.stats[2 * row + 1];
     }
-    counts = counts && g != 0.f;
+    counts = counts && (Factors::kPairs || g != 0.f);
   }
   if (counts) {
     target = Vec<T>::raw(z + y);
@@ -356,6 +529,11 @@ void short_row_kernel(LogitsArgs a) {
       lp = row_logprob(s, Vec<T>::value(target), &log_sum);
     }
     if constexpr (kPolicy) g = policy_slope(a, pr, lp, &loss);
+  }
+  if constexpr (Factors::kPairs) {
+    const float factor = factors(first, std::min<int64_t>(first + kRows, a.rows), row);
+    g = counts ? factor : 0.f;
+    if (!kTurn && !there) return;
   }
   if constexpr (kForward) {
     if (at.lane == 0) write_forward(a, row, lp, counts ? s.top : 0.f, log_sum);
@@ -394,7 +572,6 @@ void short_row_kernel(LogitsArgs a) {
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // lanes of one wave: LDS keeps their order
     __builtin_amdgcn_wave_barrier();
-    const int64_t first = row - threadIdx.x % kWave / LANES;
     const uint32_t inverse = 65536 / vectors + 1;   // n / vectors = n * inverse >> 16 for n up to 256, vectors up to 128
 #pragma unroll
     for (int i = 0; i < HOLD; ++i) {
@@ -714,20 +891,54 @@ void long_policy_kernel(LogitsArgs a) {
 // own.  8,192 x 131,071 bf16 737 us against 774 with the vectors at the row's first multiple of 4
 // bytes and 765 at that of 16; 131,072 x 2,001 187 against 213.
 constexpr uint32_t kLine = 128;
-template <class T, int LANES, int U>
+template <class T, int LANES, int U, class Factors>
 __global__ __launch_bounds__(Place<LANES>::kThreads)
-void gradient_kernel(LogitsArgs a) {
+void gradient_kernel(LogitsArgs a, Factors factors) {
   constexpr uint32_t kN = Vec<T>::kN;
   const int64_t row = Place<LANES>::row(static_cast<int64_t>(blockIdx.z) * gridDim.y + blockIdx.y);
-  if (row >= a.rows) return;
+  if (row >= a.rows) {
+    if constexpr (Factors::kPairs) {   // the groups after the last row's take a pair each
+      const int64_t pair = row - a.rows;
+      if (pair < factors.p.pairs && blockIdx.x == 0 && Place<LANES>::lane() < kWave) factors.write(pair);
+    }
+    return;
+  }
   const T* z = static_cast<const T*>(a.logits) + row * a.stride;
   T* dz = static_cast<T*>(a.dlogits) + row * a.out_stride;
   const uint32_t head = static_cast<uint32_t>(-reinterpret_cast<uintptr_t>(z) % kLine / sizeof(T));
   const uint32_t lane = Place<LANES>::lane(), cols = static_cast<uint32_t>(a.cols);
   const uint32_t full = (cols - head) / kN, rem = cols - head - full * kN, v0 = blockIdx.x * (LANES * U);
   const int32_t y = a.targets[row];
-  const float g = a.grad[row], top = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
-  const RowGradient<T> grad = RowGradient<T>::of_stats(y >= 0 && y < a.cols ? g : 0.f, top, log_sum);
+  const bool has_token = y >= 0 && y < a.cols;
+  u4v h[U];
+  auto load = [&] {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      h[i] = u4v{0, 0, 0, 0};
+      if (v0 + i * LANES + lane < full) h[i] = Vec<T>::load(z + head, v0 + i * LANES, lane);
+    }
+  };
+  float g = 0.f;
+  if constexpr (Factors::kPairs) {
+    if (has_token) {
+      load();      // while the pair is summed
+      if constexpr (Place<LANES>::kRows > 1) {
+        g = factors(row, row + 1, row);
+      } else {     // once per block: by each of 8 waves, 486 rows of 22,737 fp16 take 6 us longer
+        __shared__ float factor;
+        if (threadIdx.x < kWave) {
+          g = factors(row, row + 1, row);
+          if (threadIdx.x == 0) factor = g;
+        }
+        __syncthreads();
+        g = factor;
+      }
+    }
+  } else {
+    g = a.grad[row];
+  }
+  const float top = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
+  const RowGradient<T> grad = RowGradient<T>::of_stats(has_token ? g : 0.f, top, log_sum);
   // Columns outside of the vectors: up to kN - 1 at the end, less than a cache line at the start.
   const uint32_t yv = static_cast<uint32_t>(y), last = cols - rem + lane;
   const bool has_tail = blockIdx.x == gridDim.x - 1 && lane < rem, has_head = blockIdx.x == 0 && lane < head;
@@ -741,13 +952,8 @@ void gradient_kernel(LogitsArgs a) {
   }
   const uint32_t target = (yv - head) / kN - v0;   // the target's vector, and whether this lane has it
   const bool has_target = target < LANES * U && target + v0 < full && target % LANES == lane;
-  u4v h[U];
   uint32_t z_target = 0, z_tail = 0, z_head = 0;
-#pragma unroll
-  for (int i = 0; i < U; ++i) {
-    h[i] = u4v{0, 0, 0, 0};
-    if (v0 + i * LANES + lane < full) h[i] = Vec<T>::load(z + head, v0 + i * LANES, lane);
-  }
+  if constexpr (!Factors::kPairs) load();
   if (has_target) z_target = Vec<T>::raw(z + yv);
   if (has_tail) z_tail = Vec<T>::raw(z + last);
   if (has_head) z_head = Vec<T>::raw(z + lane);
@@ -768,28 +974,38 @@ hipError_t launch_rows(Kernel kernel, const LogitsArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <class T, int LANES, int U>
-hipError_t launch_gradient(const LogitsArgs& a, hipStream_t stream) {
+// A short row's kernel; with pairs, a wave more for each.
+template <class T, RowMode kMode, int LANES, int HOLD, class Factors>
+hipError_t launch_short_rows(const LogitsArgs& a, const Factors& factors, hipStream_t stream) {
+  constexpr int64_t kWaves = kBlock / kWave;
+  const int64_t blocks = (short_row_waves<LANES>(a.rows) + pairs_of(factors) + kWaves - 1) / kWaves, x = std::min(blocks, kGridX);
+  const dim3 grid(static_cast<uint32_t>(x), static_cast<uint32_t>((blocks + x - 1) / x));
+  short_row_kernel<T, kMode, LANES, HOLD><<<grid, kBlock, 0, stream>>>(a, factors);
+  return hipGetLastError();
+}
+
+template <class T, int LANES, int U, class Factors>
+hipError_t launch_gradient(const LogitsArgs& a, const Factors& factors, hipStream_t stream) {
   constexpr int64_t kRun = int64_t{LANES} * U;
-  const int64_t full = a.cols / Vec<T>::kN, blocks = Place<LANES>::blocks(a.rows), y = std::min(blocks, kGridYZ);
+  const int64_t full = a.cols / Vec<T>::kN, blocks = Place<LANES>::blocks(a.rows + pairs_of(factors)), y = std::min(blocks, kGridYZ);
   const dim3 grid(static_cast<uint32_t>(std::max<int64_t>(1, (full + kRun - 1) / kRun)), static_cast<uint32_t>(y),
                   static_cast<uint32_t>((blocks + y - 1) / y));
-  gradient_kernel<T, LANES, U><<<grid, Place<LANES>::kThreads, 0, stream>>>(a);
+  gradient_kernel<T, LANES, U><<<grid, Place<LANES>::kThreads, 0, stream>>>(a, factors);
   return hipGetLastError();
 }
 
 // Rows of up to 128 vectors: lanes by the number of vectors.
-template <class T, RowMode kMode>
-hipError_t launch_short(const LogitsArgs& a, hipStream_t stream) {
+template <class T, RowMode kMode, class Factors = GivenFactors>
+hipError_t launch_short(const LogitsArgs& a, hipStream_t stream, const Factors& factors = {}) {
   const int64_t vectors = (a.cols + Vec<T>::kN - 1) / Vec<T>::kN;
-  if (vectors <= 1) return launch_rows<1>(short_row_kernel<T, kMode, 1, 1>, a, stream);
-  if (vectors <= 2) return launch_rows<1>(short_row_kernel<T, kMode, 1, 2>, a, stream);
-  if (vectors <= 4) return launch_rows<1>(short_row_kernel<T, kMode, 1, 4>, a, stream);
-  if (vectors <= 8) return launch_rows<2>(short_row_kernel<T, kMode, 2, 4>, a, stream);
-  if (vectors <= 16) return launch_rows<4>(short_row_kernel<T, kMode, 4, 4>, a, stream);
-  if (vectors <= 32) return launch_rows<8>(short_row_kernel<T, kMode, 8, 4>, a, stream);
-  if (vectors <= 64) return launch_rows<16>(short_row_kernel<T, kMode, 16, 4>, a, stream);
-  return launch_rows<32>(short_row_kernel<T, kMode, 32, 4>, a, stream);
+  if (vectors <= 1) return launch_short_rows<T, kMode, 1, 1>(a, factors, stream);
+  if (vectors <= 2) return launch_short_rows<T, kMode, 1, 2>(a, factors, stream);
+  if (vectors <= 4) return launch_short_rows<T, kMode, 1, 4>(a, factors, stream);
+  if (vectors <= 8) return launch_short_rows<T, kMode, 2, 4>(a, factors, stream);
+  if (vectors <= 16) return launch_short_rows<T, kMode, 4, 4>(a, factors, stream);
+  if (vectors <= 32) return launch_short_rows<T, kMode, 8, 4>(a, factors, stream);
+  if (vectors <= 64) return launch_short_rows<T, kMode, 16, 4>(a, factors, stream);
+  return launch_short_rows<T, kMode, 32, 4>(a, factors, stream);
 }
 constexpr int64_t kShortVectors = 128;
 
@@ -834,24 +1050,24 @@ hipError_t launch_policy(const LogitsArgs& a, hipStream_t stream) {
   return launch_rows<512>(long_policy_kernel<T, 8, 16, 9>, a, stream);
 }
 
-template <class T>
-hipError_t launch_backward(const LogitsArgs& a, hipStream_t stream) {
+template <class T, class Factors = GivenFactors>
+hipError_t launch_backward(const LogitsArgs& a, hipStream_t stream, const Factors& factors = {}) {
   const int64_t vectors = (a.cols + Vec<T>::kN - 1) / Vec<T>::kN;
-  if (vectors <= kShortVectors) return launch_short<T, RowMode::kBackward>(a, stream);
+  if (vectors <= kShortVectors) return launch_short<T, RowMode::kBackward>(a, stream, factors);
   // Runs that leave few lanes of a row's last one empty: 9,000 bf16 columns (1,125 vectors) 166 us in
   // runs of 512, 209 of 1,024; 20,000 (2,500) 169 and 163.  fp32 does best with a load per lane
   // (24,000 columns 163 us, with two 176).
   // 384 vectors and fewer: 2,501 bf16 columns 161 us in runs of 384, 168 in runs of 512; 3,501 (438) 270
   // and 215.
-  if (vectors <= 256) return launch_gradient<T, 64, 4>(a, stream);
-  if (vectors <= 384) return launch_gradient<T, 128, 3>(a, stream);
-  if (vectors <= 512) return launch_gradient<T, 256, 2>(a, stream);
+  if (vectors <= 256) return launch_gradient<T, 64, 4>(a, factors, stream);
+  if (vectors <= 384) return launch_gradient<T, 128, 3>(a, factors, stream);
+  if (vectors <= 512) return launch_gradient<T, 256, 2>(a, factors, stream);
   if constexpr (sizeof(T) == 4) {
-    if (vectors > 768) return launch_gradient<T, 256, 1>(a, stream);
+    if (vectors > 768) return launch_gradient<T, 256, 1>(a, factors, stream);
   } else {
-    if (vectors > 1024 && vectors <= 1536) return launch_gradient<T, 256, 2>(a, stream);
+    if (vectors > 1024 && vectors <= 1536) return launch_gradient<T, 256, 2>(a, factors, stream);
   }
-  return launch_gradient<T, 512, 2>(a, stream);
+  return launch_gradient<T, 512, 2>(a, factors, stream);
 }
 
 template <class T>
@@ -863,76 +1079,16 @@ hipError_t launch_typed(const LogitsArgs& a, RowMode mode, hipStream_t stream) {
   }
 }
 
-// A pair's rows: sequence 2 i is [at[0], at[1]), sequence 2 i + 1 [at[1], at[2]).
-struct PairRows {
-  int64_t at[3];
-
-  __device__ __forceinline__ PairRows(const PairArgs& a, int64_t pair) {
-    for (int k = 0; k < 3; ++k) at[k] = std::min<int64_t>(std::max<int64_t>(a.offsets[2 * pair + k], 0), a.rows);
-  }
-};
-
-// The pair's loss, written by one thread, and the gradient of its preferred rows' log-probabilities
-// (the others' is the negative).  The sum runs over kPairThreads threads, four neighbouring rows
-// to each at a time and two such loads in flight, in a fixed order, in 64 bits; `logprobs4` gives four
-// rows' log-probabilities.
-constexpr int kPairThreads = 1024;
-typedef float f4_unaligned __attribute__((ext_vector_type(4), aligned(4)));
-typedef int32_t i4_unaligned __attribute__((ext_vector_type(4), aligned(4)));
-
-template <class Logprobs>
-__device__ __forceinline__ float pair_slope(const PairArgs& a, int64_t pair, const PairRows& rows, double (&sums)[kPairThreads / kWave],
-                                            Logprobs logprobs) {
-  double sum = 0.0;
-  auto add = [&](int64_t t, int32_t y, float lp, float ref) {
-    if (y < 0 || y >= a.cols) return;
-    const double v = static_cast<double>(lp) - ref;
-    sum += t < rows.at[1] ? v : -v;
-  };
-#pragma unroll 2
-  for (int64_t t = rows.at[0] + 4 * threadIdx.x; t < rows.at[2]; t += 4 * kPairThreads) {
-    if (t + 4 <= rows.at[2]) {
-      const i4_unaligned y = *reinterpret_cast<const i4_unaligned*>(a.targets + t);
-      f4_unaligned ref = {0.f, 0.f, 0.f, 0.f};
-      if (a.ref_logprobs) ref = *reinterpret_cast<const f4_unaligned*>(a.ref_logprobs + t);
-      const f4_unaligned lp = logprobs(t);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) add(t + k, y[k], lp[k], ref[k]);
-    } else {
-      for (int64_t u = t; u < rows.at[2]; ++u) add(u, a.targets[u], logprobs.one(u), a.ref_logprobs ? a.ref_logprobs[u] : 0.f);
-    }
-  }
-  for (int d = 1; d < kWave; d *= 2) sum += __shfl_xor(sum, d, kWave);
-  if (threadIdx.x % kWave == 0) sums[threadIdx.x / kWave] = sum;
-  __syncthreads();
-  double h = 0.0;
-  for (int w = 0; w < kPairThreads / kWave; ++w) h += sums[w];
-  h *= a.beta;
-  const double e = exp(-fabs(h)), rest = log1p(e), small = e / (1.0 + e);   // sigma(-|h|)
-  const double minus = rest + fmax(-h, 0.0), plus = rest + fmax(h, 0.0);    // -ln sigma(h), -ln sigma(-h)
-  if (threadIdx.x == 0) {
-    a.margins[pair] = static_cast<float>(h);
-    a.loss[pair] = static_cast<float>(h != h ? h : (1.0 - a.smoothing) * minus + a.smoothing * plus);
-  }
-  const double weight = a.weights ? a.weights[pair] : 1.f;
-  const double up = h >= 0 ? 1.0 / (1.0 + e) : small, down = h >= 0 ? small : 1.0 / (1.0 + e);
-  const double slope = h != h ? h : a.smoothing * up - (1.0 - a.smoothing) * down;
-  return weight == 0.0 ? 0.f : static_cast<float>(slope * a.beta * a.scale * weight);
-}
-
-// Log-probabilities by row, from memory or from LDS.
-struct RowLogprobs {
-  const float* p;
-  __device__ __forceinline__ f4_unaligned operator()(int64_t t) const { return *reinterpret_cast<const f4_unaligned*>(p + t); }
-  __device__ __forceinline__ float one(int64_t t) const { return p[t]; }
-};
-
 __global__ __launch_bounds__(kPairThreads)
 void pair_kernel(PairArgs a) {
-  __shared__ double sums[kPairThreads / kWave];
+  __shared__ PairSums shared;
   for (int64_t pair = blockIdx.x; pair < a.pairs; pair += gridDim.x) {
     const PairRows rows(a, pair);
-    const float g = pair_slope(a, pair, rows, sums, RowLogprobs{a.logprobs});
+    const float g = block_pair_slope(a, pair, rows, shared, [&](int64_t t, double& sum) {
+      FourRows r;
+      r.load(a, rows, t);
+      r.add(a, rows, t, sum);
+    });
     if (a.grad) {
       for (int64_t t = rows.at[0] + 4 * threadIdx.x; t < rows.at[2]; t += 4 * kPairThreads) {
         f4_unaligned v;
@@ -948,17 +1104,20 @@ void pair_kernel(PairArgs a) {
 }
 
 // The whole preference loss in one launch, for few logits: a block per pair takes its rows' sums,
-// the pair's loss and, reading the rows again out of the caches, their gradients.  Rows before
+// the pair's loss and, reading the rows again out of the caches, their gradients; what it needs of
+// a row again stays in LDS.  Rows before
 // the first pair and after the last go with those.  Every value is computed as by the kernels that
 // take one step each, to the same bits.
-constexpr int64_t kSmallRows = 4096;
+constexpr int64_t kSmallRows = 4 * kPairThreads;
 template <class T, int LANES, int HOLD, int U>   // as for short rows; U > 0: long rows, a wave for each
 __global__ __launch_bounds__(kPairThreads)
 void small_preference_kernel(LogitsArgs a, PairArgs p) {
   constexpr uint32_t kN = Vec<T>::kN;
-  constexpr int kGroups = kPairThreads / LANES;
-  __shared__ double sums[kPairThreads / kWave];
-  __shared__ float logprobs[kSmallRows], tops[kSmallRows], log_sums[kSmallRows];
+  constexpr int kGroups = kPairThreads / LANES, kAhead = U > 0 ? U : HOLD;
+  __shared__ PairSums shared;
+  __shared__ double shares[kSmallRows];          // l - ref, of rows that count
+  __shared__ float tops[kSmallRows], log_sums[kSmallRows], target_logits[kSmallRows];
+  __shared__ int32_t targets[kSmallRows];        // -1: no token, or no row of the pair
   const int64_t pair = blockIdx.x;
   const PairRows rows(p, pair);
   const int64_t from = pair == 0 ? 0 : rows.at[0], to = pair == p.pairs - 1 ? a.rows : rows.at[2];
@@ -969,9 +1128,11 @@ void small_preference_kernel(LogitsArgs a, PairArgs p) {
   for (int64_t row = from + group; row < to; row += kGroups) {
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
     const int32_t y = a.targets[row];
-    float lp = 0.f, log_sum = 0.f;
+    const float ref = p.ref_logprobs ? p.ref_logprobs[row] : 0.f;
+    const bool counts = y >= 0 && y < a.cols;
+    float lp = 0.f, log_sum = 0.f, target_logit = 0.f;
     Stat s{0.f, 0.f};
-    if (y >= 0 && y < a.cols) {
+    if (counts) {
       const uint32_t target = Vec<T>::raw(z + y);
       if constexpr (U == 0) {
         u4v h[HOLD];
@@ -980,49 +1141,75 @@ void small_preference_kernel(LogitsArgs a, PairArgs p) {
       } else {
         s = long_row_part<T, 1, U>(z, cols, lane);
       }
-      lp = row_logprob(s, Vec<T>::value(target), &log_sum);
+      target_logit = Vec<T>::value(target);
+      lp = row_logprob(s, target_logit, &log_sum);
     }
     if (lane == 0) {
       a.logprobs[row] = lp;
-      logprobs[row] = lp;
+      shares[row] = counts ? static_cast<double>(lp) - ref : 0.0;
       tops[row] = s.top;
       log_sums[row] = log_sum;
+      target_logits[row] = target_logit;
+      targets[row] = counts && row >= rows.at[0] && row < rows.at[2] ? y : -1;
     }
   }
   __syncthreads();
-  const float g = pair_slope(p, pair, rows, sums, RowLogprobs{logprobs});
+  // A row's last vector, which overlaps the one before it, is loaded before either is stored, and the
+  // first row's first vectors while the pair's loss is computed.
+  const uint32_t last = at.vectors - 1;
+  auto load = [&](int64_t row, u4v (&h)[kAhead], u4v& end) {
+    if (cols < kN || row >= to || targets[row] < 0) return;
+    const T* z = static_cast<const T*>(a.logits) + row * a.stride;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) h[i] = Vec<T>::template load<true>(z + at.start(std::min(i * LANES + lane, last)), 0, 0);
+    if (lane == last % LANES) end = Vec<T>::template load<true>(z + at.start(last), 0, 0);
+  };
+  u4v h[kAhead] = {}, end{};
+  if (a.dlogits) load(from + group, h, end);
+  const float g = block_pair_slope(p, pair, rows, shared, [&](int64_t t, double& sum) {
+    for (int64_t u = t; u < t + 4 && u < rows.at[2]; ++u) sum += u < rows.at[1] ? shares[u] : -shares[u];
+  });
   if (a.dlogits == nullptr) return;
   for (int64_t row = from + group; row < to; row += kGroups) {
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
     T* dz = static_cast<T*>(a.dlogits) + row * a.out_stride;
-    const int32_t y = a.targets[row];
-    const bool counts = y >= 0 && y < a.cols && row >= rows.at[0] && row < rows.at[2];
-    const RowGradient<T> grad = RowGradient<T>::of_stats(!counts ? 0.f : row < rows.at[1] ? g : -g, tops[row], log_sums[row]);
-    const uint32_t yv = static_cast<uint32_t>(y), target = grad.none ? 0 : Vec<T>::raw(z + y);
+    const int32_t y = targets[row];
+    const RowGradient<T> grad = RowGradient<T>::of_stats(y < 0 ? 0.f : row < rows.at[1] ? g : -g, tops[row], log_sums[row]);
+    const uint32_t yv = static_cast<uint32_t>(y);
+    const float target_logit = target_logits[row];
     if (cols < kN) {
-      u4v h[HOLD] = {};
-      if (!grad.none) at.load(z, h);
-      at.store_few(dz, grad, h[0], yv, Vec<T>::value(target));
+      if constexpr (U == 0) {
+        u4v few[HOLD] = {};
+        if (!grad.none) at.load(z, few);
+        at.store_few(dz, grad, few[0], yv, target_logit);
+      }
       continue;
     }
-    // The last vector, which overlaps the one before it, is loaded before either is stored.
-    const uint32_t last = at.vectors - 1;
-    u4v end{};
-    if (!grad.none && lane == last % LANES) end = Vec<T>::template load<true>(z + at.start(last), 0, 0);
-    for (uint32_t v = lane; v < at.vectors; v += LANES) {
-      u4v h = end;
-      if (!grad.none && v != last) h = Vec<T>::template load<true>(z + at.start(v), 0, 0);
-      Vec<T>::template store<true>(dz + at.start(v), 0, 0, grad.of_vector(h));
-      if (!grad.none && yv - at.start(v) < kN) dz[yv] = static_cast<T>(grad.of(Vec<T>::value(target), true));
+    for (uint32_t v0 = 0; v0 < at.vectors; v0 += kAhead * LANES) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const uint32_t v = v0 + i * LANES + lane;
+        if (v >= at.vectors) continue;
+        u4v x = h[i];
+        if (v0 > 0 && !grad.none) x = Vec<T>::template load<true>(z + at.start(v), 0, 0);
+        Vec<T>::template store<true>(dz + at.start(v), 0, 0, grad.of_vector(v == last ? end : x));
+        if (!grad.none && yv - at.start(v) < kN) dz[yv] = static_cast<T>(grad.of(target_logit, true));
+      }
     }
+    load(row + kGroups, h, end);
   }
 }
 
-// So many logits, and so many per pair, go through one launch, in which a pair has but one CU: 8 pairs of
-// 32 rows of 1,000 bf16 9.4 us instead of the 13.8 that three launches take (in a graph 9.0 and 9.3),
-// fp32 11.3 and 13.8 (10.9 and 9.2); of 64 rows of bf16 14.1 and 14.0 (13.7 and 9.5).  Whatever the
-// pairs' lengths, a CU that takes all rows is done in 0.12 ms.
-constexpr int64_t kSmallLogits = int64_t{1} << 19, kSmallPairLogits = int64_t{1} << 15;
+// So many logits, and so many per pair, go through one launch, in which a pair has but one CU, whose
+// exponentials bound it: 4 pairs of 24 rows of 1,000 fp32 10.0 us a call, two launches 10.5 (in a graph 10.0
+// and 7.8); 2 of 424 rows of 58 fp16 9.9 and 10.8; 16 of 32 rows of 1,000 fp32 13.5 and 11.0.  Whatever
+// the pairs' lengths, a CU that takes all rows is done in 0.12 ms.
+constexpr int64_t kSmallLogits = int64_t{1} << 19, kSmallPairLogits = 24576;
+// Few rows (on average, of a pair) and bytes take two launches, the second of which sums the pairs again
+// for every row: 566 rows of 3,902 bf16 in 55 pairs 11.9 us a call, three launches 14.2 (in a graph 10.3
+// and 12.0); 4,096 of 2,000 in 8 pairs 16.7 and 17.1; but 486 of 22,737 in 43 pairs 23.7 and 21.4, 4,096 of
+// 20,000 152 and 80.  A single pair among thousands that has all the rows costs 16 loads in turn.
+constexpr int64_t kFewRows = 4 * kPairThreads, kFewPairRows = 512, kFewBytes = int64_t{1} << 24;
 
 template <class T>
 hipError_t launch_small(const LogitsArgs& a, const PairArgs& p, hipStream_t stream) {
@@ -1050,6 +1237,20 @@ hipError_t launch_logits(const LogitsArgs& a, RowMode mode, int dtype, hipStream
     case PGC_F32: return launch_typed<float>(a, mode, stream);
     case PGC_BF16: return launch_typed<__bf16>(a, mode, stream);
     default: return launch_typed<_Float16>(a, mode, stream);
+  }
+}
+
+// Few rows need no launch between their log-probabilities and their gradient.
+bool preference_sums_in_gradient(int64_t rows, int64_t cols, int64_t pairs, int dtype) {
+  return pairs > 0 && pairs <= kFewRows && rows <= std::min(kFewRows, kFewPairRows * pairs) &&
+         rows * cols * (dtype == PGC_F32 ? 4 : 2) <= kFewBytes;
+}
+
+hipError_t launch_pair_gradient(const LogitsArgs& a, const PairArgs& p, int dtype, hipStream_t stream) {
+  switch (dtype) {
+    case PGC_F32: return launch_backward<float>(a, stream, PairFactors{p});
+    case PGC_BF16: return launch_backward<__bf16>(a, stream, PairFactors{p});
+    default: return launch_backward<_Float16>(a, stream, PairFactors{p});
   }
 }
 

@@ -300,10 +300,16 @@ int pgc_preference_loss(const pgc_logits* logits, const pgc_preference_args* a, 
     k.out_stride = a->dlogits_stride;
     return launched(pgc::launch_small_preference(k, p, logits->dtype, stream), "preference loss kernel");
   }
+  const bool sums_in_gradient = rows > 0 && a->dlogits && pgc::preference_sums_in_gradient(rows, logits->cols, pairs, logits->dtype);
   if (rows > 0) {
     k.stats = stats;
-    k.zero_grad = grad;
+    k.zero_grad = sums_in_gradient ? nullptr : grad;
     CHECK(launched(pgc::launch_logits(k, pgc::RowMode::kForward, logits->dtype, stream), "log-probability kernel"));
+  }
+  if (sums_in_gradient) {
+    k.dlogits = a->dlogits;
+    k.out_stride = a->dlogits_stride;
+    return launched(pgc::launch_pair_gradient(k, p, logits->dtype, stream), "pair gradient kernel");
   }
   if (pairs > 0) CHECK(launched(pgc::launch_pairs(p, stream), "pair kernel"));
   if (rows > 0 && a->dlogits) {

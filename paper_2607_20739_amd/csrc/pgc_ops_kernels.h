@@ -61,6 +61,11 @@ struct PairArgs {
 };
 hipError_t launch_pairs(const PairArgs& a, hipStream_t stream);
 
+// The same and the gradient in one launch, for few rows (a.stats as RowMode::kForward wrote them; a.grad and
+// p.grad are not used).
+bool preference_sums_in_gradient(int64_t rows, int64_t cols, int64_t pairs, int dtype);
+hipError_t launch_pair_gradient(const LogitsArgs& a, const PairArgs& p, int dtype, hipStream_t stream);
+
 // Forward, pairs and backward of few logits in one launch, without a workspace (a.dlogits null: no
 // gradient; p.logprobs and p.grad are not used).
 bool preference_is_small(int64_t rows, int64_t cols, int64_t pairs, int dtype);

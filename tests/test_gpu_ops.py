@@ -703,3 +703,52 @@ def test_every_operator_gives_a_row_the_same_logprobs(dtype):
         for a, b in zip(few, many):
             assert torch.equal(a, b[:len(a)])
         assert not many[3][24:].any()
+
+
+PREFERENCE_PATHS = [(3, [(3000, 40), (4096, 4096), (37, 1)]), (16, [(4000, 9), (300, 2)]), (30, [(4090, 70)]), (61, [(1000, 3)]),
+                    (120, [(4096, 33), (513, 1)]), (250, [(257, 1), (900, 200)]), (510, [(500, 2)]), (1000, [(700, 5)]),
+                    (2050, [(65, 1), (530, 64)]), (3000, [(400, 129)]), (4097, [(64, 33)]), (9001, [(21, 2)]), (20003, [(33, 1)])]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols,sizes", PREFERENCE_PATHS)
+def test_preference_loss_of_few_rows_and_of_many_have_the_same_bits(dtype, cols, sizes):
+    """One launch, two or three: pairs that are empty, of one row, and of all of them; rows of no pair,
+    rows without a token; more offsets than a wave has lanes; in place, at odd strides and addresses."""
+    for rows, pairs in sizes:
+        rng = np.random.default_rng(rows * 7 + pairs)
+        z, y = _case(dtype, rows, cols, rows + cols)
+        y[rng.random(rows) < 0.2] = -1
+        y = y.cuda()
+        ref = torch.from_numpy(rng.normal(size=rows).astype(np.float32)).cuda() - 3.0
+        weights = torch.from_numpy(rng.uniform(size=pairs).astype(np.float32)).cuda()
+        weights[pairs // 2:pairs // 2 + 1] *= float(pairs < 3)
+        spread = np.sort(rng.integers(0, rows + 1, 2 * pairs + 1))
+        one = np.full(2 * pairs + 1, rows)
+        one[:pairs] = 0
+        inner = np.clip(spread, rows // 3, rows - rows // 4)
+        for case, cuts in enumerate([spread, one, inner]):
+            _say("preference paths", dtype, rows, cols, pairs, case)
+            o = torch.from_numpy(cuts.astype(np.int32)).cuda()
+            kw = dict(beta=0.3, label_smoothing=0.1, scale=2.0, pair_weights=weights if case != 1 else None)
+            zg = _place(z, 3 * case, case)[1]
+            got = ops.preference_loss(zg, y, o, ref if case != 2 else None, **kw)
+            alone = ops.preference_loss(zg, y, o, ref if case != 2 else None, gradient=False, **kw)
+            more = 4097
+            zz = torch.cat([z.cuda(), z[:1].cuda().expand(more, cols)])
+            yy, rr = torch.cat([y, y[:1].expand(more)]), torch.cat([ref, ref[:1].expand(more)])
+            # The one that has all rows ends with them here, too.
+            want = ops.preference_loss(zz, yy, o, rr if case != 2 else None, **kw)
+            for i, (a, b) in enumerate(zip(got, want)):
+                assert torch.equal(a, b[:len(a)]), (case, i)
+            for a, b in zip(alone[:3], got[:3]):
+                assert torch.equal(a, b), case
+            assert not want[3][rows:].any()
+            ops.preference_loss(zg, y, o, ref if case != 2 else None, out=zg, **kw)
+            assert torch.equal(zg, got[3]), case
+        e = _Expected(z, y.cpu())
+        loss, margin, _, _ = O.preference(e.z, e.y, cuts, None, 0.3, 0.1, 2.0, weights.cpu().numpy())
+        err = 0.3 * np.concatenate([[0.0], np.cumsum(e.lp_tol + u * np.abs(e.lp))])
+        tol = err[cuts[2::2]] - err[cuts[:-1:2]] + 2 * u * np.abs(margin)
+        _close(got[1], margin, tol, "margins")
+        _close(got[0], loss, tol + 2 * u * np.abs(loss), "loss")
