@@ -9,7 +9,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
-#include <ATen/ops/empty.h>
+#include <ATen/ops/empty_cuda_dispatch.h>
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -62,7 +62,10 @@ struct Matrix {
   }
   void* data() const { return t.data_ptr(); }
   pgc_logits logits() const { return {data(), rows, cols, stride, dtype}; }
-  at::Tensor empty(at::IntArrayRef shape, at::ScalarType type) const { return at::empty(shape, t.options().dtype(type)); }
+  // Past the dispatcher, which takes 0.4 us more.
+  at::Tensor empty(at::IntArrayRef shape, at::ScalarType type) const {
+    return at::cuda::empty(shape, type, at::kStrided, t.device(), std::nullopt, std::nullopt);
+  }
 
   // Of this one's shape, type and GPU.
   int64_t like(const char* name, const at::Tensor& other) const {

@@ -93,7 +93,7 @@ def build(verbose=False):
           ["-L" + ROCM_LIB, "-Wl,-rpath," + ROCM_LIB, "-lrocprofiler-sdk-roctx"])
     torch_lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     _link("_ops_torch.so", BINDING_LIB, ["g++", binding, "-L" + PKG, "-lpgc", "-Wl,-rpath,$ORIGIN", "-L" + torch_lib,
-                                         "-lc10", "-ltorch_cpu", "-ltorch_python"])
+                                         "-lc10", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python"])
     if verbose:
         print("built", LIB)
         print("built", BINDING_LIB)
