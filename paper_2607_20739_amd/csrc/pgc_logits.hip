@@ -271,21 +271,20 @@ struct PairRows {
   }
 };
 
-// The gradient of the preferred rows' log-probabilities (the others' is the negative), in 64 bits, from
-// the pair's sum of l - ref, preferred rows less the others; kWrite: writes the loss and the margin, too.
-template <bool kWrite>
-__device__ __forceinline__ float pair_slope(const PairArgs& a, int64_t pair, double sum, bool writes) {
-  const double h = sum * a.beta;
-  const double e = exp(-fabs(h)), small = e / (1.0 + e);   // sigma(-|h|)
-  if (kWrite && writes) {
-    const double rest = log1p(e), minus = rest + fmax(-h, 0.0), plus = rest + fmax(h, 0.0);   // -ln sigma(h), -ln sigma(-h)
-    a.margins[pair] = static_cast<float>(h);
-    a.loss[pair] = static_cast<float>(h != h ? h : (1.0 - a.smoothing) * minus + a.smoothing * plus);
-  }
+// From the pair's sum of l - ref, preferred rows less the others, in 64 bits: the gradient of the
+// preferred rows' log-probabilities (the others' is the negative), and the loss and the margin.
+__device__ __forceinline__ float pair_slope(const PairArgs& a, int64_t pair, double sum) {
+  const double h = sum * a.beta, e = exp(-fabs(h)), large = 1.0 / (1.0 + e), small = e / (1.0 + e);   // sigma(|h|), sigma(-|h|)
   const double weight = a.weights ? a.weights[pair] : 1.f;
-  const double large = 1.0 / (1.0 + e), up = h >= 0 ? large : small, down = h >= 0 ? small : large;
+  const double up = h >= 0 ? large : small, down = h >= 0 ? small : large;
   const double slope = h != h ? h : a.smoothing * up - (1.0 - a.smoothing) * down;
   return weight == 0.0 ? 0.f : static_cast<float>(slope * a.beta * a.scale * weight);
+}
+__device__ __forceinline__ void write_pair(const PairArgs& a, int64_t pair, double sum) {
+  const double h = sum * a.beta, rest = log1p(exp(-fabs(h)));
+  const double minus = rest + fmax(-h, 0.0), plus = rest + fmax(h, 0.0);   // -ln sigma(h), -ln sigma(-h)
+  a.margins[pair] = static_cast<float>(h);
+  a.loss[pair] = static_cast<float>(h != h ? h : (1.0 - a.smoothing) * minus + a.smoothing * plus);
 }
 
 // A pair's sum runs in a fixed order, whoever adds it up: kPairWaves waves' lanes take four neighbouring
@@ -331,7 +330,8 @@ __device__ __forceinline__ double add_lanes(double sum) {
   return sum;
 }
 
-// By a block of kPairThreads; the first wave writes the loss and the margin, all threads get the slope.
+// By a block of kPairThreads, all of which get the slope.  One wave takes the 64-bit functions (all 16 take
+// 1 us longer), and the last writes the loss and the margin while the others go on.
 struct PairSums {
   double sums[kPairWaves];
   float slope;
@@ -344,13 +344,17 @@ __device__ __forceinline__ float block_pair_slope(const PairArgs& a, int64_t pai
   sum = add_lanes(sum);
   if (threadIdx.x % kWave == 0) shared.sums[threadIdx.x / kWave] = sum;
   __syncthreads();
-  if (threadIdx.x < kWave) {   // one wave: the 64-bit functions of all 16 take 1 us more
-    double h = 0.0;
-    for (int w = 0; w < kPairWaves; ++w) h += shared.sums[w];
-    const float slope = pair_slope<true>(a, pair, h, threadIdx.x == 0);
+  const bool first = threadIdx.x < kWave, last = threadIdx.x >= kPairThreads - kWave;
+  if (first || last) {
+    sum = 0.0;
+    for (int w = 0; w < kPairWaves; ++w) sum += shared.sums[w];
+  }
+  if (first) {
+    const float slope = pair_slope(a, pair, sum);
     if (threadIdx.x == 0) shared.slope = slope;
   }
   __syncthreads();
+  if (threadIdx.x == kPairThreads - kWave) write_pair(a, pair, sum);
   return shared.slope;
 }
 
@@ -407,7 +411,7 @@ struct PairFactors {
       }
       const int64_t pair = (n - 1) / 2;
       const PairRows rows(p, pair);
-      const float slope = pair_slope<false>(p, pair, wave_pair_sum(p, rows), false);
+      const float slope = pair_slope(p, pair, wave_pair_sum(p, rows));
       if (row >= r && row < rows.at[2]) g = row < rows.at[1] ? slope : -slope;
       r = std::max(r + 1, rows.at[2]);
     }
@@ -415,8 +419,8 @@ struct PairFactors {
   }
   // The pair's loss and margin.
   __device__ __forceinline__ void write(int64_t pair) const {
-    const PairRows rows(p, pair);
-    pair_slope<true>(p, pair, wave_pair_sum(p, rows), threadIdx.x % kWave == 0);
+    const double sum = wave_pair_sum(p, PairRows(p, pair));
+    if (threadIdx.x % kWave == 0) write_pair(p, pair, sum);
   }
 };
 
@@ -1128,9 +1132,11 @@ void small_preference_kernel(LogitsArgs a, PairArgs p) {
   uint32_t group = threadIdx.x / LANES;
   if constexpr (LANES == kWave) group = __builtin_amdgcn_readfirstlane(group);
   const ShortRow<T, LANES, HOLD> at(cols);
+  int32_t next_y = from + group < to ? a.targets[from + group] : -1;
   for (int64_t row = from + group; row < to; row += kGroups) {
     const T* z = static_cast<const T*>(a.logits) + row * a.stride;
-    const int32_t y = a.targets[row];
+    const int32_t y = next_y;
+    if (row + kGroups < to) next_y = a.targets[row + kGroups];   // on its way with this row
     const float ref = p.ref_logprobs ? p.ref_logprobs[row] : 0.f;
     const bool counts = y >= 0 && y < a.cols;
     float lp = 0.f, log_sum = 0.f, target_logit = 0.f;
@@ -1188,6 +1194,8 @@ void small_preference_kernel(LogitsArgs a, PairArgs p) {
       }
       continue;
     }
+    u4v next[kAhead] = {}, next_end{};
+    load(row + kGroups, next, next_end);
     for (uint32_t v0 = 0; v0 < at.vectors; v0 += kAhead * LANES) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) {
@@ -1199,7 +1207,9 @@ void small_preference_kernel(LogitsArgs a, PairArgs p) {
         if (!grad.none && yv - at.start(v) < kN) dz[yv] = static_cast<T>(grad.of(target_logit, true));
       }
     }
-    load(row + kGroups, h, end);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) h[i] = next[i];
+    end = next_end;
   }
 }
 
