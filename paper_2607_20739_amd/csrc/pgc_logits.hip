@@ -667,6 +667,12 @@ struct WaveRun {
     if (i < whole) Vec<T>::store(out, i * kWave, lane, d);
     else if (lane < part) Vec<T>::store(out, i * kWave, lane, d);
   }
+  // Of a row whose vectors are shared out, those before `held` one by one and the others by `group`s: whose
+  // has the target.
+  __device__ __forceinline__ uint32_t stored_by(uint32_t y, uint32_t held, uint32_t group, uint32_t parts) const {
+    const uint32_t i = ((y - odd) / kN - begin) / kWave;
+    return (i < held ? i : (i - held) / group) % parts;
+  }
   // The target's gradient, by the lane that stored its vector.
   __device__ __forceinline__ void store_target(T* dz, const RowGradient<T>& grad, uint32_t y, float target_logit) const {
     const uint32_t v = (y - odd) / kN - begin;    // of y = 0 in a shifted row: past any run
@@ -776,7 +782,7 @@ struct RowEnds {
 // A row's loss and gradient factor from the lanes' maxima and sums; one lane writes the loss.
 template <class T, int WAVES>
 __device__ __forceinline__ RowGradient<T> finish_policy_row(const LogitsArgs& a, int64_t row, const PolicyTurn<T>& turn, bool counts,
-                                                            Stat s, float target_logit, RowParts<WAVES>& parts, uint32_t tid) {
+                                                            Stat s, float target_logit, RowParts<WAVES>& parts, uint32_t tid, bool writes) {
   float lp = 0.f, loss = 0.f, g = 0.f, log_sum = 0.f;
   if (counts) {
     s = join_lanes<kWave>(s);
@@ -791,7 +797,7 @@ __device__ __forceinline__ RowGradient<T> finish_policy_row(const LogitsArgs& a,
     lp = row_logprob(s, target_logit, &log_sum);
     g = policy_slope(a, turn.row, lp, &loss);
   }
-  if (tid == 0) {
+  if (tid == 0 && writes) {
     a.logprobs[row] = lp;
     a.loss[row] = loss;
   }
@@ -805,7 +811,11 @@ __device__ __forceinline__ RowGradient<T> finish_policy_row(const LogitsArgs& a,
 // in LDS, where they are loaded without passing through registers; the rest of a row that is
 // longer still is read again.  8 waves of 16 + 9 vectors hold 102,400 16-bit values at two blocks
 // to a CU: rows of 131,072 bf16 take 741 us so, 805 held whole by one block of 16 waves.
-template <class T, int WAVES, int HOLD, int STAGE>
+//
+// kSplit, for few rows: as many blocks as blockIdx.z counts all take the row's sum, whose order stays the
+// same, and each the gradient of every so-manieth vector.  Not in place: a block would change what
+// another has yet to read.
+template <class T, int WAVES, int HOLD, int STAGE, bool kSplit>
 __global__ __launch_bounds__(Place<WAVES * kWave>::kThreads)
 void long_policy_kernel(LogitsArgs a) {
   constexpr int kN = Vec<T>::kN, LANES = WAVES * kWave;
@@ -818,6 +828,8 @@ void long_policy_kernel(LogitsArgs a) {
   const uint32_t tid = Place<LANES>::lane(), cols = static_cast<uint32_t>(a.cols);
   const uint32_t full = long_row_vectors<T>(cols), rem = cols - full * kN, wave = uniform(static_cast<int32_t>(tid / kWave));
   const uint32_t per = (full + LANES - 1) / LANES * kWave;
+  const uint32_t part = kSplit ? blockIdx.z : 0, parts_of_row = kSplit ? gridDim.z : 1;
+  auto mine_to_store = [&](uint32_t i) { return !kSplit || i % parts_of_row == part; };
   const T* z = static_cast<const T*>(a.logits) + row * a.stride;
   const WaveRun<T> run(z, full, wave * per, per);
   PolicyTurn<T> turn;
@@ -859,7 +871,7 @@ void long_policy_kernel(LogitsArgs a) {
     }
     if (tid < rem) add_value(s, Vec<T>::value(ends.tail));
   }
-  const RowGradient<T> grad = finish_policy_row<T, WAVES>(a, row, turn, counts, s, Vec<T>::value(target), parts, tid);
+  const RowGradient<T> grad = finish_policy_row<T, WAVES>(a, row, turn, counts, s, Vec<T>::value(target), parts, tid, part == 0);
   if (a.dlogits == nullptr) return;
   T* dz = static_cast<T*>(a.dlogits) + row * a.out_stride;
   const uint32_t y = static_cast<uint32_t>(turn.y);
@@ -870,23 +882,26 @@ void long_policy_kernel(LogitsArgs a) {
 #pragma unroll
     for (int k = 0; k < kMore; ++k) more[k] = run.load(i + k);
   };
-  if constexpr (STAGE > 0) load_more(HOLD + STAGE);
+  const uint32_t first_more = HOLD + STAGE + part * kMore;
+  if constexpr (STAGE > 0) load_more(first_more);
 #pragma unroll
   for (int i = 0; i < HOLD; ++i) {
+    if (!mine_to_store(i)) continue;
     asm("" : "+v"(held[i]));   // unpacked anew: twice the registers would go to its values
     run.store(dz, grad, i, held[i]);
   }
   if constexpr (STAGE > 0) {
 #pragma unroll 1
-    for (int i = 0; i < STAGE; ++i) run.store(dz, grad, HOLD + i, mine[i * kWave + run.lane]);
-    for (uint32_t i = HOLD + STAGE; run.any(i); i += kMore) {
+    for (int i = 0; i < STAGE; ++i)
+      if (mine_to_store(HOLD + i)) run.store(dz, grad, HOLD + i, mine[i * kWave + run.lane]);
+    for (uint32_t i = first_more; run.any(i); i += kMore * parts_of_row) {
 #pragma unroll
       for (int k = 0; k < kMore; ++k) run.store(dz, grad, i + k, more[k]);
-      load_more(i + kMore);
+      load_more(i + kMore * parts_of_row);
     }
   }
-  run.store_target(dz, grad, y, Vec<T>::value(target));
-  ends.store(dz, grad, full, run.odd, tid, rem, y);
+  if (!kSplit || run.stored_by(y, HOLD + STAGE, kMore, parts_of_row) == part) run.store_target(dz, grad, y, Vec<T>::value(target));
+  if (part == 0) ends.store(dz, grad, full, run.odd, tid, rem, y);
 }
 
 // kBackward of longer rows: every value by itself.  A group of LANES lanes takes LANES * U vectors of
@@ -1032,29 +1047,48 @@ hipError_t launch_forward(const LogitsArgs& a, hipStream_t stream) {
   return launch_rows<1024>(long_forward_kernel<T, 16, 4>, a, stream);
 }
 
+// Few long rows of a gradient that replaces no logits: four to eight blocks for each, up to one per CU.  16
+// rows of 65,536 bf16 9.0 us, by a block each 11.6; 64 10.5 and 12.4; 64 of 32,768 fp32 8.2 and 8.8; one of
+// 131,072 bf16 15.7 and 19.3.  Two blocks for each of 100 rows of 32,768 fp32 take 9.5, one 8.9; rows of up
+// to 7,168 vectors gain nothing.
+constexpr int64_t kCus = 256, kFewestParts = 4, kMostParts = 8;
+template <class T, int WAVES, int HOLD, int STAGE>
+hipError_t launch_long_policy(const LogitsArgs& a, hipStream_t stream) {
+  constexpr int LANES = WAVES * kWave;
+  if constexpr (HOLD == 16) {   // past 7,168 vectors
+    const int64_t parts = std::min(kCus / a.rows, kMostParts);
+    if (parts >= kFewestParts && a.dlogits && a.dlogits != a.logits) {
+      const dim3 grid(static_cast<uint32_t>(a.rows), 1, static_cast<uint32_t>(parts));
+      long_policy_kernel<T, WAVES, HOLD, STAGE, true><<<grid, LANES, 0, stream>>>(a);
+      return hipGetLastError();
+    }
+  }
+  return launch_rows<LANES>(long_policy_kernel<T, WAVES, HOLD, STAGE, false>, a, stream);
+}
+
 // Waves and vectors per lane by the row's vectors.
 template <class T>
 hipError_t launch_policy(const LogitsArgs& a, hipStream_t stream) {
   const int64_t vectors = (a.cols + Vec<T>::kN - 1) / Vec<T>::kN, full = a.cols / Vec<T>::kN;
   if (vectors <= kShortVectors) return launch_short<T, RowMode::kPolicy>(a, stream);
-  if (full <= 192) return launch_rows<64>(long_policy_kernel<T, 1, 3, 0>, a, stream);
-  if (full <= 256) return launch_rows<64>(long_policy_kernel<T, 1, 4, 0>, a, stream);
-  if (full <= 384) return launch_rows<64>(long_policy_kernel<T, 1, 6, 0>, a, stream);
-  if (full <= 512) return launch_rows<64>(long_policy_kernel<T, 1, 8, 0>, a, stream);
-  if (full <= 768) return launch_rows<256>(long_policy_kernel<T, 4, 3, 0>, a, stream);
-  if (full <= 1024) return launch_rows<256>(long_policy_kernel<T, 4, 4, 0>, a, stream);
-  if (full <= 1536) return launch_rows<256>(long_policy_kernel<T, 4, 6, 0>, a, stream);
-  if (full <= 2048) return launch_rows<256>(long_policy_kernel<T, 4, 8, 0>, a, stream);
-  if (full <= 3072) return launch_rows<512>(long_policy_kernel<T, 8, 6, 0>, a, stream);
-  if (full <= 4096) return launch_rows<512>(long_policy_kernel<T, 8, 8, 0>, a, stream);
-  if (full <= 5120) return launch_rows<512>(long_policy_kernel<T, 8, 10, 0>, a, stream);
-  if (full <= 6144) return launch_rows<512>(long_policy_kernel<T, 8, 12, 0>, a, stream);
-  if (full <= 7168) return launch_rows<512>(long_policy_kernel<T, 8, 14, 0>, a, stream);
-  if (full <= 8192) return launch_rows<512>(long_policy_kernel<T, 8, 16, 0>, a, stream);
+  if (full <= 192) return launch_long_policy<T, 1, 3, 0>(a, stream);
+  if (full <= 256) return launch_long_policy<T, 1, 4, 0>(a, stream);
+  if (full <= 384) return launch_long_policy<T, 1, 6, 0>(a, stream);
+  if (full <= 512) return launch_long_policy<T, 1, 8, 0>(a, stream);
+  if (full <= 768) return launch_long_policy<T, 4, 3, 0>(a, stream);
+  if (full <= 1024) return launch_long_policy<T, 4, 4, 0>(a, stream);
+  if (full <= 1536) return launch_long_policy<T, 4, 6, 0>(a, stream);
+  if (full <= 2048) return launch_long_policy<T, 4, 8, 0>(a, stream);
+  if (full <= 3072) return launch_long_policy<T, 8, 6, 0>(a, stream);
+  if (full <= 4096) return launch_long_policy<T, 8, 8, 0>(a, stream);
+  if (full <= 5120) return launch_long_policy<T, 8, 10, 0>(a, stream);
+  if (full <= 6144) return launch_long_policy<T, 8, 12, 0>(a, stream);
+  if (full <= 7168) return launch_long_policy<T, 8, 14, 0>(a, stream);
+  if (full <= 8192) return launch_long_policy<T, 8, 16, 0>(a, stream);
   // Past 20,480 vectors what 16 waves of one block hold more outweighs the second block: 2,048 rows of
   // 131,072 fp32 391 us, 433 by 8 waves; of 80,000 232 and 234; of 65,600 195 and 180.
-  if (full > 20480) return launch_rows<1024>(long_policy_kernel<T, 16, 16, 9>, a, stream);
-  return launch_rows<512>(long_policy_kernel<T, 8, 16, 9>, a, stream);
+  if (full > 20480) return launch_long_policy<T, 16, 16, 9>(a, stream);
+  return launch_long_policy<T, 8, 16, 9>(a, stream);
 }
 
 template <class T, class Factors = GivenFactors>

@@ -752,3 +752,31 @@ def test_preference_loss_of_few_rows_and_of_many_have_the_same_bits(dtype, cols,
         tol = err[cuts[2::2]] - err[cuts[:-1:2]] + 2 * u * np.abs(margin)
         _close(got[1], margin, tol, "margins")
         _close(got[0], loss, tol + 2 * u * np.abs(loss), "loss")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [28680, 32768, 57351, 65535, 65537, 82001, 131071, 163900, 262147])
+def test_policy_loss_of_few_rows_and_of_many_have_the_same_bits(dtype, cols):
+    """Rows that several blocks share, rows with a block each, and the gradient in place; targets in every
+    part of a row, at odd strides and addresses."""
+    many = 70
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    z = (2 * torch.randn(many, cols, generator=gen, device="cuda")).to(DTYPES[dtype])
+    y = torch.randint(0, cols, (many,), generator=gen, device="cuda").to(torch.int32)
+    y[:8] = torch.tensor([0, cols - 1, -1, 1, cols // 2, cols - 9, 7, 8])
+    old, adv = torch.full((many,), -11.0, device="cuda"), torch.linspace(-1, 1, many, device="cuda")
+    kw = dict(clip_low=0.2, clip_high=0.3)
+    want = ops.policy_loss(z, y, old, adv, ref_logprobs=old, kl=0.1, **kw)
+    for rows, pad, shift in [(1, 0, 0), (2, 1, 1), (31, 0, 3), (33, 5, 0), (50, 0, 0), (64, 3, 1), (65, 0, 0)]:
+        _say("policy few rows", dtype, cols, rows)
+        first = min(8, many - rows) if rows < 31 else 0
+        part = slice(first, first + rows)
+        _, zg = _place(z[part], pad, shift, fill=100.0)
+        buf, out = _place(torch.zeros(rows, cols, dtype=DTYPES[dtype]), pad, shift, fill=77.0)
+        got = ops.policy_loss(zg, y[part], old[part], adv[part], ref_logprobs=old[part], kl=0.1, out=out, **kw)
+        for a, b in zip(got, want):
+            assert torch.equal(a, b[part]), rows
+        out.fill_(77.0)
+        assert (buf == 77.0).all(), "values outside of the output were written"
+        ops.policy_loss(zg, y[part], old[part], adv[part], ref_logprobs=old[part], kl=0.1, out=zg, **kw)
+        assert torch.equal(zg, want[2][part]), rows
