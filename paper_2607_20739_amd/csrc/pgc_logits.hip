@@ -262,13 +262,23 @@ __device__ __forceinline__ void write_forward(const LogitsArgs& a, int64_t row, 
   if (a.zero_grad) a.zero_grad[row] = 0.f;
 }
 
+// A pair's sum runs in a fixed order, whoever adds it up: by chunks of kChunk rows from the pair's first on.
+// In a chunk kPairWaves waves' lanes take four neighbouring rows each, then the lanes of a wave are
+// added up, then the waves one after the other.  Chunk c belongs to lane c % 64; each lane adds up its
+// own, then the lanes.
+constexpr int kPairThreads = 1024, kPairWaves = kPairThreads / kWave, kChunk = 4 * kPairThreads;
+
 // A pair's rows: sequence 2 i is [at[0], at[1]), sequence 2 i + 1 [at[1], at[2]).
 struct PairRows {
   int64_t at[3];
 
   __device__ __forceinline__ PairRows(const PairArgs& a, int64_t pair) {
-    for (int k = 0; k < 3; ++k) at[k] = std::min<int64_t>(std::max<int64_t>(a.offsets[2 * pair + k], 0), a.rows);
+    for (int k = 0; k < 3; ++k) at[k] = bounded(a, a.offsets[2 * pair + k]);
   }
+  static __device__ __forceinline__ int64_t bounded(const PairArgs& a, int64_t offset) {
+    return std::min<int64_t>(std::max<int64_t>(offset, 0), a.rows);
+  }
+  __device__ __forceinline__ int64_t chunks() const { return (at[2] - at[0] + kChunk - 1) / kChunk; }
 };
 
 // From the pair's sum of l - ref, preferred rows less the others, in 64 bits: the gradient of the
@@ -287,9 +297,6 @@ __device__ __forceinline__ void write_pair(const PairArgs& a, int64_t pair, doub
   a.loss[pair] = static_cast<float>(h != h ? h : (1.0 - a.smoothing) * minus + a.smoothing * plus);
 }
 
-// A pair's sum runs in a fixed order, whoever adds it up: kPairWaves waves' lanes take four neighbouring
-// rows at a time, each adds up its own, then the lanes of a wave, then the waves one after the other.
-constexpr int kPairThreads = 1024, kPairWaves = kPairThreads / kWave;
 typedef float f4_unaligned __attribute__((ext_vector_type(4), aligned(4)));
 typedef int32_t i4_unaligned __attribute__((ext_vector_type(4), aligned(4)));
 
@@ -315,13 +322,15 @@ struct FourRows {
       }
     }
   }
-  __device__ __forceinline__ void add(const PairArgs& a, const PairRows& rows, int64_t t, double& sum) const {
+  __device__ __forceinline__ double sum(const PairArgs& a, const PairRows& rows, int64_t t) const {
+    double sum = 0.0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if (y[k] < 0 || y[k] >= a.cols) continue;
       const double v = static_cast<double>(lp[k]) - ref[k];
       sum += t + k < rows.at[1] ? v : -v;
     }
+    return sum;
   }
 };
 
@@ -331,34 +340,53 @@ __device__ __forceinline__ double add_lanes(double sum) {
 }
 
 // By a block of kPairThreads, all of which get the slope.  One wave takes the 64-bit functions (all 16 take
-// 1 us longer), and the last writes the loss and the margin while the others go on.
+// 1 us longer), and the last writes the loss and the margin while the others go on.  `part` gives a
+// thread's part of a chunk, from the row that it is given on.
+constexpr int kChunksAtOnce = 16;
 struct PairSums {
-  double sums[kPairWaves];
+  double sums[kChunksAtOnce][kPairWaves];
   float slope;
 };
-template <class Add>
-__device__ __forceinline__ float block_pair_slope(const PairArgs& a, int64_t pair, const PairRows& rows, PairSums& shared, Add add) {
+template <class Part>
+__device__ __forceinline__ float block_pair_slope(const PairArgs& a, int64_t pair, const PairRows& rows, PairSums& shared, Part part) {
+  const int64_t chunks = rows.chunks();
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const bool first = wave == 0, last = wave == kPairWaves - 1;
   double sum = 0.0;
-#pragma unroll 2
-  for (int64_t t = rows.at[0] + 4 * threadIdx.x; t < rows.at[2]; t += 4 * kPairThreads) add(t, sum);
-  sum = add_lanes(sum);
-  if (threadIdx.x % kWave == 0) shared.sums[threadIdx.x / kWave] = sum;
-  __syncthreads();
-  const bool first = threadIdx.x < kWave, last = threadIdx.x >= kPairThreads - kWave;
-  if (first || last) {
-    sum = 0.0;
-    for (int w = 0; w < kPairWaves; ++w) sum += shared.sums[w];
+  auto wave_sum = [&](int64_t c) { return add_lanes(part(rows.at[0] + c * kChunk + 4 * threadIdx.x)); };
+  auto chunk_sum = [&](int c) {
+    double total = 0.0;
+    for (int w = 0; w < kPairWaves; ++w) total += shared.sums[c][w];
+    return total;
+  };
+  if (chunks == 1) {   // the same without the lanes' last sum
+    const double v = wave_sum(0);
+    if (lane == 0) shared.sums[0][wave] = v;
+    __syncthreads();
+    if (first || last) sum = chunk_sum(0);
+  } else {
+    for (int64_t c0 = 0; c0 < chunks; c0 += kChunksAtOnce) {
+      if (c0 > 0) __syncthreads();   // before the sums of the next chunks
+      const int n = static_cast<int>(std::min<int64_t>(chunks - c0, kChunksAtOnce));
+      for (int c = 0; c < n; ++c) {
+        const double v = wave_sum(c0 + c);
+        if (lane == 0) shared.sums[c][wave] = v;
+      }
+      __syncthreads();
+      if ((first || last) && (c0 + lane % kChunksAtOnce) % kWave == lane && lane % kChunksAtOnce < n) sum += chunk_sum(lane % kChunksAtOnce);
+    }
+    if (first || last) sum = add_lanes(sum);
   }
   if (first) {
     const float slope = pair_slope(a, pair, sum);
-    if (threadIdx.x == 0) shared.slope = slope;
+    if (lane == 0) shared.slope = slope;
   }
   __syncthreads();
-  if (threadIdx.x == kPairThreads - kWave) write_pair(a, pair, sum);
+  if (last && lane == 0) write_pair(a, pair, sum);
   return shared.slope;
 }
 
-// By one wave, of at most 4 * kPairThreads rows; two waves' rows at a time are in flight.
+// By one wave, of one chunk; two waves' rows at a time are in flight.
 __device__ __forceinline__ double wave_pair_sum(const PairArgs& a, const PairRows& rows) {
   const uint32_t lane = threadIdx.x % kWave;
   double h = 0.0;
@@ -368,27 +396,28 @@ __device__ __forceinline__ double wave_pair_sum(const PairArgs& a, const PairRow
     FourRows r0, r1;
     r0.load(a, rows, t0);
     r1.load(a, rows, t1);
-    double sum0 = 0.0, sum1 = 0.0;
-    r0.add(a, rows, t0, sum0);
-    r1.add(a, rows, t1, sum1);
-    h += add_lanes(sum0);
-    h += add_lanes(sum1);
+    h += add_lanes(r0.sum(a, rows, t0));
+    h += add_lanes(r1.sum(a, rows, t1));
   }
   return h;
 }
 
-// How many of the offsets are at most `row`, by a wave: each step looks at 64 of them.
-__device__ __forceinline__ int64_t offsets_up_to(const PairArgs& a, int64_t row) {
+// How many of `count` keys, which do not decrease, are at most v, by a wave: each step looks at 64 of them.
+template <class Key>
+__device__ __forceinline__ int64_t keys_up_to(int64_t count, int64_t v, Key key) {
   const uint32_t lane = threadIdx.x % kWave;
-  int64_t from = 0, count = 2 * a.pairs + 1;
+  int64_t from = 0;
   while (true) {
     const int64_t step = (count + kWave - 1) / kWave, at = lane * step;
-    const uint64_t below = __ballot(at < count && a.offsets[from + (at < count ? at : 0)] <= row);
+    const uint64_t below = __ballot(at < count && key(from + (at < count ? at : 0)) <= v);
     const int64_t n = __popcll(below);
     if (step == 1 || n == 0) return from + n;
     from += (n - 1) * step;
     count = std::min(count - (n - 1) * step, step);
   }
+}
+__device__ __forceinline__ int64_t offsets_up_to(const PairArgs& a, int64_t row) {
+  return keys_up_to(2 * a.pairs + 1, row, [&](int64_t k) -> int64_t { return a.offsets[k]; });
 }
 
 // Where the gradient kernels take a row's factor from: memory, or the row's pair.  A wave calls with
@@ -1120,28 +1149,84 @@ hipError_t launch_typed(const LogitsArgs& a, RowMode mode, hipStream_t stream) {
   }
 }
 
+// The rows' part of the gradient of a pair, or of a chunk of it.
+__device__ __forceinline__ void write_rows(const PairArgs& a, const PairRows& rows, int64_t from, int64_t to, float g) {
+  for (int64_t t = from + 4 * threadIdx.x; t < to; t += kChunk) {
+    f4_unaligned v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = t + k < rows.at[1] ? g : -g;
+    if (t + 4 <= to) *reinterpret_cast<f4_unaligned*>(a.grad + t) = v;
+    else
+      for (int64_t u = t; u < to; ++u) a.grad[u] = v[u - t];
+  }
+}
+
 __global__ __launch_bounds__(kPairThreads)
 void pair_kernel(PairArgs a) {
   __shared__ PairSums shared;
   for (int64_t pair = blockIdx.x; pair < a.pairs; pair += gridDim.x) {
     const PairRows rows(a, pair);
-    const float g = block_pair_slope(a, pair, rows, shared, [&](int64_t t, double& sum) {
+    const float g = block_pair_slope(a, pair, rows, shared, [&](int64_t t) {
       FourRows r;
       r.load(a, rows, t);
-      r.add(a, rows, t, sum);
+      return r.sum(a, rows, t);
     });
-    if (a.grad) {
-      for (int64_t t = rows.at[0] + 4 * threadIdx.x; t < rows.at[2]; t += 4 * kPairThreads) {
-        f4_unaligned v;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = t + k < rows.at[1] ? g : -g;
-        if (t + 4 <= rows.at[2]) *reinterpret_cast<f4_unaligned*>(a.grad + t) = v;
-        else
-          for (int64_t u = t; u < rows.at[2]; ++u) a.grad[u] = v[u - t];
-      }
-    }
+    if (a.grad) write_rows(a, rows, rows.at[0], rows.at[2], g);
     __syncthreads();   // before the sums of the next pair
   }
+}
+
+// Long pairs, a block for each chunk: first the chunks' sums, then, in a second launch, each block adds up its
+// pair's.  Chunk c of pair i has the place first row / kChunk + i + c, so that all chunks have places in
+// [0, rows / kChunk + pairs), each its own.
+struct ChunkPlace {
+  int64_t pair, first;   // the pair's first place; pair -1: none
+
+  __device__ __forceinline__ ChunkPlace(const PairArgs& a, int64_t place) {
+    auto first_place = [&](int64_t i) { return PairRows::bounded(a, a.offsets[2 * i]) / kChunk + i; };
+    pair = keys_up_to(a.pairs, place, first_place) - 1;
+    first = pair < 0 ? 0 : first_place(pair);
+  }
+};
+
+__global__ __launch_bounds__(kPairThreads)
+void chunk_sum_kernel(PairArgs a) {
+  __shared__ double sums[kPairWaves];
+  const ChunkPlace at(a, blockIdx.x);
+  if (at.pair < 0) return;
+  const PairRows rows(a, at.pair);
+  const int64_t t = rows.at[0] + (blockIdx.x - at.first) * kChunk + 4 * threadIdx.x;
+  FourRows r;
+  r.load(a, rows, t);
+  double sum = add_lanes(r.sum(a, rows, t));
+  if (threadIdx.x % kWave == 0) sums[threadIdx.x / kWave] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    sum = 0.0;
+    for (int w = 0; w < kPairWaves; ++w) sum += sums[w];
+    a.chunk_sums[blockIdx.x] = sum;
+  }
+}
+
+__global__ __launch_bounds__(kPairThreads)
+void chunk_gradient_kernel(PairArgs a) {
+  __shared__ float slope;
+  const ChunkPlace at(a, blockIdx.x);
+  if (at.pair < 0) return;
+  const PairRows rows(a, at.pair);
+  const int64_t chunks = rows.chunks(), c = blockIdx.x - at.first;
+  if (c > 0 && c >= chunks) return;   // a pair's first place also without rows
+  double sum = 0.0;
+  if (threadIdx.x < kWave) {
+    for (int64_t k = threadIdx.x; k < chunks; k += kWave) sum += a.chunk_sums[at.first + k];
+    sum = add_lanes(sum);
+    const float g = pair_slope(a, at.pair, sum);
+    if (threadIdx.x == 0) slope = g;
+  }
+  __syncthreads();
+  const int64_t from = rows.at[0] + c * kChunk;
+  if (a.grad) write_rows(a, rows, from, std::min(rows.at[2], from + kChunk), slope);
+  if (c == 0 && threadIdx.x == 0) write_pair(a, at.pair, sum);
 }
 
 // The whole preference loss in one launch, for few logits: a block per pair takes its rows' sums,
@@ -1149,7 +1234,7 @@ void pair_kernel(PairArgs a) {
 // a row again stays in LDS.  Rows before
 // the first pair and after the last go with those.  Every value is computed as by the kernels that
 // take one step each, to the same bits.
-constexpr int64_t kSmallRows = 4 * kPairThreads;
+constexpr int64_t kSmallRows = kChunk;
 template <class T, int LANES, int HOLD, int U>   // as for short rows; U > 0: long rows, a wave for each
 __global__ __launch_bounds__(kPairThreads)
 void small_preference_kernel(LogitsArgs a, PairArgs p) {
@@ -1209,8 +1294,10 @@ void small_preference_kernel(LogitsArgs a, PairArgs p) {
   };
   u4v h[kAhead] = {}, end{};
   if (a.dlogits) load(from + group, h, end);
-  const float g = block_pair_slope(p, pair, rows, shared, [&](int64_t t, double& sum) {
+  const float g = block_pair_slope(p, pair, rows, shared, [&](int64_t t) {
+    double sum = 0.0;
     for (int64_t u = t; u < t + 4 && u < rows.at[2]; ++u) sum += u < rows.at[1] ? shares[u] : -shares[u];
+    return sum;
   });
   if (a.dlogits == nullptr) return;
   for (int64_t row = from + group; row < to; row += kGroups) {
@@ -1256,7 +1343,8 @@ constexpr int64_t kSmallLogits = int64_t{1} << 19, kSmallPairLogits = 24576;
 // for every row: 566 rows of 3,902 bf16 in 55 pairs 11.9 us a call, three launches 14.2 (in a graph 10.3
 // and 12.0); 4,096 of 2,000 in 8 pairs 16.7 and 17.1; but 486 of 22,737 in 43 pairs 23.7 and 21.4, 4,096 of
 // 20,000 152 and 80.  A single pair among thousands that has all the rows costs 16 loads in turn.
-constexpr int64_t kFewRows = 4 * kPairThreads, kFewPairRows = 512, kFewBytes = int64_t{1} << 24;
+constexpr int64_t kLongPairRows = 20480;
+constexpr int64_t kFewRows = kChunk, kFewPairRows = 512, kFewBytes = int64_t{1} << 24;
 
 template <class T>
 hipError_t launch_small(const LogitsArgs& a, const PairArgs& p, hipStream_t stream) {
@@ -1301,7 +1389,17 @@ hipError_t launch_pair_gradient(const LogitsArgs& a, const PairArgs& p, int dtyp
   }
 }
 
+int64_t pair_chunk_places(int64_t rows, int64_t pairs) { return rows / kChunk + pairs; }
+
 hipError_t launch_pairs(const PairArgs& a, hipStream_t stream) {
+  // Long pairs on average: 1,048,576 rows of 20 fp16 in one pair 36 us, by a block per pair 214; 170,950 of 58
+  // bf16 in 4 21 and 28; 104,502 of 12 fp32 in 10 15.8 and 13.8.
+  if (a.rows / kLongPairRows >= a.pairs) {
+    const uint32_t places = static_cast<uint32_t>(pair_chunk_places(a.rows, a.pairs));
+    chunk_sum_kernel<<<places, kPairThreads, 0, stream>>>(a);
+    chunk_gradient_kernel<<<places, kPairThreads, 0, stream>>>(a);
+    return hipGetLastError();
+  }
   pair_kernel<<<static_cast<int>(std::min(a.pairs, kGridX)), kPairThreads, 0, stream>>>(a);
   return hipGetLastError();
 }

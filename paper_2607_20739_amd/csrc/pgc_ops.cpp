@@ -229,7 +229,8 @@ int pgc_token_logprobs_backward(const pgc_logits* logits, const int32_t* targets
                   "log-probability gradient kernel");
 }
 
-// The rows' (M, ln S) pairs, then their gradients; nothing where one launch does it all.
+// The rows' (M, ln S) pairs, their gradients, then the sums of long pairs' chunks; nothing where one launch
+// does it all.
 int pgc_preference_workspace_bytes(const pgc_logits* logits, int64_t pairs, size_t* bytes) {
   if (logits == nullptr || bytes == nullptr) return fail(PGC_EINVAL, "null arguments");
   if (!known(logits->dtype)) return fail(PGC_EINVAL, "unknown dtype %d", logits->dtype);
@@ -237,7 +238,8 @@ int pgc_preference_workspace_bytes(const pgc_logits* logits, int64_t pairs, size
   CHECK(check_pairs(pairs));
   const size_t rows = static_cast<size_t>(logits->rows);
   const bool none = pgc::preference_is_small(logits->rows, logits->cols, pairs, logits->dtype);
-  *bytes = none ? 0 : align_up(8 * rows) + align_up(4 * rows);
+  const size_t sums = 8 * static_cast<size_t>(pgc::pair_chunk_places(logits->rows, pairs));
+  *bytes = none ? 0 : align_up(8 * rows) + align_up(4 * rows) + align_up(sums);
   return PGC_OK;
 }
 
@@ -289,6 +291,7 @@ int pgc_preference_loss(const pgc_logits* logits, const pgc_preference_args* a, 
   p.loss = a->loss;
   p.margins = a->margins;
   p.grad = a->dlogits ? grad : nullptr;
+  p.chunk_sums = reinterpret_cast<double*>(reinterpret_cast<char*>(grad) + align_up(4 * static_cast<size_t>(rows)));
   p.rows = rows;
   p.cols = logits->cols;
   p.pairs = pairs;

@@ -56,9 +56,11 @@ struct PairArgs {
   float* loss;
   float* margins;
   float* grad;                 // the rows' gradients, written for the rows of pairs; or null
+  double* chunk_sums;          // pair_chunk_places(rows, pairs) of them, as scratch memory
   int64_t rows, pairs, cols;
   double beta, smoothing, scale;
 };
+int64_t pair_chunk_places(int64_t rows, int64_t pairs);
 hipError_t launch_pairs(const PairArgs& a, hipStream_t stream);
 
 // The same and the gradient in one launch, for few rows (a.stats as RowMode::kForward wrote them; a.grad and

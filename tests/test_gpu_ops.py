@@ -780,3 +780,48 @@ def test_policy_loss_of_few_rows_and_of_many_have_the_same_bits(dtype, cols):
         assert (buf == 77.0).all(), "values outside of the output were written"
         ops.policy_loss(zg, y[part], old[part], adv[part], ref_logprobs=old[part], kl=0.1, out=zg, **kw)
         assert torch.equal(zg, want[2][part]), rows
+
+
+@pytest.mark.parametrize("dtype,rows,cols,cuts", [
+    ("f32", 70_001, 3, [5, 30_007, 60_001]), ("bf16", 40_000, 9, [0, 4096, 8192, 8192, 40_000]),
+    ("f16", 100_003, 4, [9_001, 9_001, 9_001, 13_097, 13_098, 50_000, 99_999]), ("f32", 600_000, 2, [1, 299_000, 599_998]),
+    ("bf16", 300_000, 5, [0, 1, 270_000, 280_000, 300_000]), ("f32", 16_384, 10, [4_095, 8_000, 12_290])])
+def test_preference_loss_of_long_pairs(dtype, rows, cols, cuts):
+    """A block for each 4,096 rows of a pair, or one for all of it: the same bits, and the oracle's values."""
+    _say("long pairs", dtype, rows, cols, cuts)
+    rng = np.random.default_rng(rows)
+    z, y = _case(dtype, rows, cols, rows + cols)
+    y[rng.random(rows) < 0.1] = -1
+    cuts = np.array(cuts, np.int32)
+    pairs = (len(cuts) - 1) // 2
+    e = _Expected(z, y)
+    ref = (e.lp + 0.01 * rng.normal(size=rows)).astype(np.float32)
+    zg, yg, rg = z.cuda(), y.cuda(), torch.from_numpy(ref).cuda()
+    kw = dict(beta=0.05, label_smoothing=0.1, scale=3.0)
+    got = ops.preference_loss(zg, yg, torch.from_numpy(cuts).cuda(), rg, **kw)
+    # Empty pairs behind them make the pairs short on average.
+    more = np.concatenate([cuts, np.full(400, cuts[-1], np.int32)])
+    want = ops.preference_loss(zg, yg, torch.from_numpy(more).cuda(), rg, **kw)
+    for i, (a, b) in enumerate(zip(got, want)):
+        assert torch.equal(a, b[:len(a)]), i
+    assert (want[0][pairs:] - np.log(2)).abs().max().item() < 1e-7
+    # The same pairs' rows elsewhere, and without the gradient.
+    put = 123
+    z2 = torch.cat([zg[-put:], zg, zg[:7]])
+    y2, r2 = torch.cat([yg[-put:], yg, yg[:7]]), torch.cat([rg[-put:], rg, rg[:7]])
+    moved = ops.preference_loss(z2, y2, torch.from_numpy(cuts + put).cuda(), r2, **kw)
+    for a, b in zip(got[:2], moved[:2]):
+        assert torch.equal(a, b)
+    assert torch.equal(moved[3][put:put + rows], got[3]) and not moved[3][:put].any()
+    only = ops.preference_loss(zg, yg, torch.from_numpy(cuts).cuda(), rg, gradient=False, **kw)
+    for a, b in zip(only[:3], got[:3]):
+        assert torch.equal(a, b)
+    loss, margin, _, g = O.preference(e.z, e.y, cuts, ref, 0.05, 0.1, 3.0)
+    err = 0.05 * np.concatenate([[0.0], np.cumsum(e.lp_tol + u * np.abs(e.lp))])
+    h_tol = err[cuts[2::2]] - err[cuts[:-1:2]]
+    _close(got[1], margin, h_tol + 2 * u * np.abs(margin), "margins")
+    _close(got[0], loss, h_tol + 2 * u * np.abs(loss), "loss")
+    g_tol = np.zeros(rows)
+    for i in range(pairs):
+        g_tol[cuts[2 * i]:cuts[2 * i + 2]] = 0.25 * 3.0 * 0.05 * h_tol[i]
+    _close(got[3], *e.gradient(g, dtype, g_tol + 2 * u * np.abs(g)), "gradient")
