@@ -1180,12 +1180,13 @@ void pair_kernel(PairArgs a) {
 // pair's.  Chunk c of pair i has the place first row / kChunk + i + c, so that all chunks have places in
 // [0, rows / kChunk + pairs), each its own.
 struct ChunkPlace {
-  int64_t pair, first;   // the pair's first place; pair -1: none
+  int64_t pair, first;   // the pair's first place; pair -1: none (also where offsets decrease)
 
   __device__ __forceinline__ ChunkPlace(const PairArgs& a, int64_t place) {
     auto first_place = [&](int64_t i) { return PairRows::bounded(a, a.offsets[2 * i]) / kChunk + i; };
     pair = keys_up_to(a.pairs, place, first_place) - 1;
     first = pair < 0 ? 0 : first_place(pair);
+    if (first > place) pair = -1;
   }
 };
 
@@ -1340,11 +1341,12 @@ void small_preference_kernel(LogitsArgs a, PairArgs p) {
 // the pairs' lengths, a CU that takes all rows is done in 0.12 ms.
 constexpr int64_t kSmallLogits = int64_t{1} << 19, kSmallPairLogits = 24576;
 // Few rows (on average, of a pair) and bytes take two launches, the second of which sums the pairs again
-// for every row: 566 rows of 3,902 bf16 in 55 pairs 11.9 us a call, three launches 14.2 (in a graph 10.3
-// and 12.0); 4,096 of 2,000 in 8 pairs 16.7 and 17.1; but 486 of 22,737 in 43 pairs 23.7 and 21.4, 4,096 of
-// 20,000 152 and 80.  A single pair among thousands that has all the rows costs 16 loads in turn.
+// for every row, or part of one: 566 rows of 3,902 bf16 in 55 pairs 11.9 us a call, three launches 14.2 (in a graph
+// 10.3 and 12.0); 1,000 in 10 pairs 12.6 and 14.7; 4,000 of 1,500 in 20 14.0 and 15.5; but 2,000 of 3,902 18.3 and
+// 17.4, 486 of 22,737 fp16 in 43 23.7 and 21.4, 4,096 of 20,000 152 and 80.  A single pair among thousands
+// that has all the rows costs 16 loads in turn.
 constexpr int64_t kLongPairRows = 20480;
-constexpr int64_t kFewRows = kChunk, kFewPairRows = 512, kFewBytes = int64_t{1} << 24;
+constexpr int64_t kFewRows = kChunk, kFewPairRows = 512, kFewBytes = int64_t{1} << 23, kFewBytesOfWaves = int64_t{1} << 24;
 
 template <class T>
 hipError_t launch_small(const LogitsArgs& a, const PairArgs& p, hipStream_t stream) {
@@ -1377,8 +1379,9 @@ hipError_t launch_logits(const LogitsArgs& a, RowMode mode, int dtype, hipStream
 
 // Few rows need no launch between their log-probabilities and their gradient.
 bool preference_sums_in_gradient(int64_t rows, int64_t cols, int64_t pairs, int dtype) {
+  const int64_t row_bytes = cols * (dtype == PGC_F32 ? 4 : 2);
   return pairs > 0 && pairs <= kFewRows && rows <= std::min(kFewRows, kFewPairRows * pairs) &&
-         rows * cols * (dtype == PGC_F32 ? 4 : 2) <= kFewBytes;
+         rows * row_bytes <= (row_bytes <= 4 * kWave * 16 ? kFewBytesOfWaves : kFewBytes);   // a wave or less to a row, or more
 }
 
 hipError_t launch_pair_gradient(const LogitsArgs& a, const PairArgs& p, int dtype, hipStream_t stream) {

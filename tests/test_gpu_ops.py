@@ -825,3 +825,20 @@ def test_preference_loss_of_long_pairs(dtype, rows, cols, cuts):
     for i in range(pairs):
         g_tol[cuts[2 * i]:cuts[2 * i + 2]] = 0.25 * 3.0 * 0.05 * h_tol[i]
     _close(got[3], *e.gradient(g, dtype, g_tol + 2 * u * np.abs(g)), "gradient")
+
+
+@pytest.mark.parametrize("rows,cols", [(90, 64), (3000, 300), (9000, 33), (90_000, 4)])
+def test_offsets_that_decrease_stay_within_the_rows(rows, cols):
+    """No results are promised for them, but nothing outside of the outputs is touched, in any path."""
+    _say("decreasing offsets", rows, cols)
+    z, y = _case("f32", rows, cols, rows)
+    zg, yg = z.cuda(), y.cuda()
+    for cuts in ([rows, rows // 2, 0], [rows - 1, 3, rows // 2, rows, 5], [rows // 2, 1, 0, -7, 1 << 30, 9, 2],
+                 [0, rows, 0, rows, 0], [-(1 << 31), (1 << 31) - 1, -(1 << 31)]):
+        buf, out = _place(torch.zeros(rows, cols), 3, 1, fill=77.0)
+        o = torch.tensor(cuts, dtype=torch.int32, device="cuda")
+        loss, margin, lp, _ = ops.preference_loss(zg, yg, o, out=out)
+        assert loss.isfinite().all() and margin.isfinite().all() or rows > 20480
+        assert torch.equal(lp, ops.token_logprobs(zg, yg)[0])
+        out.fill_(77.0)
+        assert (buf == 77.0).all()
