@@ -117,7 +117,9 @@ int pgc_token_logprobs_backward(const pgc_logits* logits, const int32_t* targets
  * Rows without a token count in no sum.  A sequence may be empty (its sum is 0).  Rows
  * of no pair, and of pairs whose gradient is 0 (w_i = 0), get gradient 0.
  * offsets must not decrease; values outside of [0, rows] are taken as the nearest bound.
- * h[i] is written to margins, l_t to logprobs.
+ * h[i] is written to margins, l_t to logprobs.  A token that cannot occur makes its
+ * pair's margin infinite: the loss is then the limit, with a term of weight 0 left out
+ * (0 for h = inf without smoothing).  Infinite sums on both sides make the pair NaN.
  */
 typedef struct pgc_preference_args {
   const int32_t* targets;       /* rows */

@@ -105,7 +105,8 @@ def preference(z, targets, offsets, ref=None, beta=0.1, smoothing=0.0, scale=1.0
         won, lost = slice(o[2 * i], o[2 * i + 1]), slice(o[2 * i + 1], o[2 * i + 2])
         h = beta * (each[won].sum() - each[lost].sum())
         margins[i] = h
-        loss[i] = (1 - smoothing) * _softplus(-h) + smoothing * _softplus(h)
+        # An infinite margin's loss is the limit: a term of weight 0 does not count.
+        loss[i] = sum(weight * _softplus(x) for weight, x in ((1 - smoothing, -h), (smoothing, h)) if weight)
         w = 1.0 if weights is None else float(weights[i])
         if w == 0:
             continue

@@ -294,7 +294,9 @@ __device__ __forceinline__ void write_pair(const PairArgs& a, int64_t pair, doub
   const double h = sum * a.beta, rest = log1p(exp(-fabs(h)));
   const double minus = rest + fmax(-h, 0.0), plus = rest + fmax(h, 0.0);   // -ln sigma(h), -ln sigma(-h)
   a.margins[pair] = static_cast<float>(h);
-  a.loss[pair] = static_cast<float>(h != h ? h : (1.0 - a.smoothing) * minus + a.smoothing * plus);
+  // A term of weight 0 is left out: an infinite margin makes one of them infinite.
+  const double loss = (a.smoothing == 1.0 ? 0.0 : (1.0 - a.smoothing) * minus) + (a.smoothing == 0.0 ? 0.0 : a.smoothing * plus);
+  a.loss[pair] = static_cast<float>(h != h ? h : loss);
 }
 
 typedef float f4_unaligned __attribute__((ext_vector_type(4), aligned(4)));

@@ -842,3 +842,36 @@ def test_offsets_that_decrease_stay_within_the_rows(rows, cols):
         assert torch.equal(lp, ops.token_logprobs(zg, yg)[0])
         out.fill_(77.0)
         assert (buf == 77.0).all()
+
+
+# Sizes that take one launch, two, three and four.
+LOSS_PATHS = [(40, 30), (1000, 100), (5001, 10), (50_001, 5)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", LOSS_PATHS)
+@pytest.mark.parametrize("smoothing", [0.0, 0.1, 1.0])
+def test_preference_loss_of_infinite_margins(dtype, rows, cols, smoothing):
+    """A token that cannot occur, in the second sequence (margin +inf) and in the first (-inf); or a row of
+    nothing but -inf.  Losses and gradients are the limits, no NaN."""
+    _say("infinite margins", dtype, rows, cols, smoothing)
+    z, y = _case(dtype, rows, cols, rows)
+    o = np.array([0, rows // 4, rows // 2, rows // 2 + 3, rows], np.int32)
+    for at, whole in [((o[1] + 1, o[2]), False), ((o[2] - 1, o[4] - 1), False), ((o[1], o[3] - 1), True)]:
+        z1, y1 = z.clone(), y.clone()
+        for t in at:
+            y1[t] = 1
+            z1[t, slice(None) if whole else 1] = -INF
+        e = _Expected(z1, y1)
+        kw = dict(beta=0.3, scale=1.7)
+        loss, margin, _, g = O.preference(e.z, e.y, o, None, 0.3, smoothing, 1.7)
+        assert np.isinf(margin).all() and not np.isnan(loss).any()
+        zg, yg, og = z1.cuda(), y1.cuda(), torch.from_numpy(o).cuda()
+        got = ops.preference_loss(zg, yg, og, label_smoothing=smoothing, **kw)
+        _close(got[1], margin, 0.0, "margins")
+        _close(got[0], loss, 0.0, "loss")
+        _close(got[2], e.lp, e.lp_tol, "logprobs")
+        _close(got[3], *e.gradient(g, dtype, 2 * u * np.abs(g)), "gradient")
+        only = ops.preference_loss(zg, yg, og, label_smoothing=smoothing, gradient=False, **kw)
+        for a, b in zip(only[:3], got[:3]):
+            assert torch.equal(a, b)

@@ -345,3 +345,13 @@ def test_the_binding_compiles_without_warnings():
         pytest.skip("g++ is not available")
     res = subprocess.run(["g++"] + B.binding_flags() + ["-fsyntax-only", B.BINDING], capture_output=True, text=True, timeout=300)
     assert res.returncode == 0 and "warning" not in res.stderr, res.stderr[-2000:]
+
+
+@pytest.mark.parametrize("smoothing,losses", [(0.0, [0.0, np.inf]), (0.1, [np.inf, np.inf]), (1.0, [np.inf, 0.0])])
+def test_oracle_losses_of_infinite_margins(smoothing, losses):
+    """-ln sigma(inf) = 0 and -ln sigma(-inf) = inf, each with its weight; weight 0 leaves a term out."""
+    z = np.array([[0.0, -np.inf], [0.0, -np.inf], [0.0, -np.inf], [0.0, -np.inf]])
+    loss, margins, _, grad = O.preference(z, [0, 1, 1, 0], [0, 1, 2, 3, 4], beta=0.5, smoothing=smoothing)
+    assert margins.tolist() == [np.inf, -np.inf] and loss.tolist() == losses
+    want = 0.5 * smoothing, -0.5 * (1 - smoothing)
+    assert grad.tolist() == [want[0], -want[0], want[1], -want[1]]
