@@ -154,7 +154,10 @@ int pgc_preference_loss(const pgc_logits* logits, const pgc_preference_args* arg
  *   dlogits = scale * d(sum_t w_t loss[t]) / dz
  * The gradient of the first term is -r a_t where r a_t <= b a_t and 0 where the bound
  * holds; a_t = 0 contributes 0 whatever r is.  A row without a token or with w_t = 0 has
- * loss, logprobs and gradient 0 and is not read.
+ * loss, logprobs and gradient 0 and is not read.  A target that cannot occur (l_t = -inf)
+ * has r = 0, and with kl > 0 and a finite ref_t the loss +inf, the limit; the gradient's
+ * factor is then -inf, so that no value of that row's gradient is finite (all are 0 where
+ * the whole row is -inf).
  */
 typedef struct pgc_policy_args {
   const int32_t* targets;       /* rows */

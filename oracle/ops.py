@@ -132,7 +132,7 @@ def policy(z, targets, old, advantages, ref=None, clip_low=0.2, clip_high=0.2, k
             slope = -ratio * a if ratio * a <= bound else 0.0
         if kl != 0:
             d = float(ref[t]) - lp[t]
-            loss[t] += kl * (np.expm1(d) - d)
+            loss[t] += kl * (np.expm1(d) - d if d < np.inf else d)   # the limit, not inf - inf
             slope -= kl * np.expm1(d)
         grad[t] = scale * slope * (1.0 if weights is None else float(weights[t]))
     return loss, np.where(on, lp, 0.0), grad

@@ -209,7 +209,7 @@ __device__ __forceinline__ float policy_slope(const LogitsArgs& a, const PolicyR
   }
   if (a.ref_logprobs) {
     const float d = r.ref_logprob - lp, e = expm1f(d);
-    l += a.kl * (e - d);
+    l += a.kl * (d == INFINITY ? d : e - d);   // a token that cannot occur: the limit, not inf - inf
     slope -= a.kl * e;
   }
   *loss = l;

@@ -875,3 +875,33 @@ def test_preference_loss_of_infinite_margins(dtype, rows, cols, smoothing):
         only = ops.preference_loss(zg, yg, og, label_smoothing=smoothing, gradient=False, **kw)
         for a, b in zip(only[:3], got[:3]):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [5, 40, 1001, 9001, 70001])
+def test_policy_loss_of_targets_that_cannot_occur(dtype, cols):
+    """Their KL term is +inf, the limit, and with it the loss; the other rows know nothing of it."""
+    _say("policy, banned targets", dtype, cols)
+    z, y = _case(dtype, 9, cols, cols)
+    y = torch.clamp(y, 0, cols - 1)
+    z[2, y[2]] = z[5, y[5]] = -INF
+    z[7] = -INF
+    e = _Expected(z, y)
+    old = np.where(np.isfinite(e.lp), e.lp - 0.1, -3.0).astype(np.float32)
+    adv = np.array([1, -1, 1, 1, 0.5, -1, 0, 1, 2], np.float32)
+    dev = [z.cuda(), y.cuda(), torch.from_numpy(old).cuda(), torch.from_numpy(adv).cuda()]
+    for kl in (0.0, 0.25):
+        loss, lp, g = O.policy(e.z, e.y, old, adv, old, kl=kl)
+        assert np.isposinf(loss[[2, 5, 7]]).all() == (kl > 0)
+        got = ops.policy_loss(*dev, ref_logprobs=dev[2], kl=kl)
+        # Ratios are exp(0.1) and the KL term's argument -0.1, both off by the log-probability's error.
+        l_err = np.where(np.isfinite(e.lp), e.lp_tol + 2 * u * (np.abs(np.nan_to_num(e.lp)) + np.abs(old)), 0.0)
+        tol = (1.2 * np.abs(adv) + kl) * (l_err + 16 * u)
+        _close(got[1], lp, e.lp_tol, "logprobs")
+        _close(got[0], loss, tol, "loss")
+        with np.errstate(invalid="ignore"):
+            want, g_tol = e.gradient(g, dtype, tol)
+        _close(got[2], want, np.nan_to_num(g_tol), "gradient")   # row 7, whose bound is inf * 0: zeros
+        if kl:
+            dz = _np(got[2])
+            assert not np.isfinite(dz[[2, 5]]).any() and not dz[7].any()

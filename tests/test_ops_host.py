@@ -355,3 +355,13 @@ def test_oracle_losses_of_infinite_margins(smoothing, losses):
     assert margins.tolist() == [np.inf, -np.inf] and loss.tolist() == losses
     want = 0.5 * smoothing, -0.5 * (1 - smoothing)
     assert grad.tolist() == [want[0], -want[0], want[1], -want[1]]
+
+
+def test_oracle_policy_loss_of_a_target_that_cannot_occur():
+    """kl (exp(d) - d - 1) at d = inf is inf; without the KL term the row has the ratio 0."""
+    z, y, one = np.array([[0.0, -np.inf, 1.0], [-np.inf] * 3]), [1, 0], np.ones(2)
+    loss, lp, grad = O.policy(z, y, -one, one, ref=-one, kl=0.1)
+    assert np.isneginf(lp).all() and np.isposinf(loss).all() and np.isneginf(grad).all()
+    for advantage, want in [(1.0, 0.0), (-1.0, 0.8)]:
+        loss, _, grad = O.policy(z, y, -one, advantage * one)
+        assert loss.tolist() == [want, want] and not grad.any()
