@@ -256,7 +256,7 @@ __device__ __forceinline__ float row_logprob(Stat s, float target_logit, float* 
 __device__ __forceinline__ void write_forward(const LogitsArgs& a, int64_t row, float lp, float top, float log_sum) {
   a.logprobs[row] = lp;
   if (a.stats) {
-    a.stats[2 * row] = top;
+    a.stats[2 * row] = log_sum != log_sum ? log_sum : top;   // fmaxf leaves NaN out
     a.stats[2 * row + 1] = log_sum;
   }
   if (a.zero_grad) a.zero_grad[row] = 0.f;

@@ -905,3 +905,17 @@ def test_policy_loss_of_targets_that_cannot_occur(dtype, cols):
         if kl:
             dz = _np(got[2])
             assert not np.isfinite(dz[[2, 5]]).any() and not dz[7].any()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [2, 10, 65, 513, 1001, 4097, 20000, 131072])
+def test_stats_of_broken_rows(dtype, cols):
+    """NaN or +inf makes both of a row's stats NaN; a row of nothing but -inf has (-inf, 0)."""
+    _say("stats of broken rows", dtype, cols)
+    z, y = _special_rows(dtype, cols)
+    e = _Expected(z, y)
+    _, stats = ops.token_logprobs(z.cuda(), y.cuda())
+    _close(stats[:, 0], e.top, 0.0, "maxima")
+    fine = np.isfinite(e.log_sum)
+    _close(stats[:, 1], e.log_sum, np.where(fine, e.sum_rel + 4 * u * np.abs(e.log_sum), 0.0), "log sums")
+    assert np.isnan(_np(stats)[[4, 5, 9]]).all() and _np(stats)[1].tolist() == [-INF, 0.0]
