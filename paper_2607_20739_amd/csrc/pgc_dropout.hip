@@ -14,6 +14,9 @@
 
 #include "pgc_ops_kernels.h"
 
+// A product and a sum are rounded apart wherever in a row a value lies.
+#pragma clang fp contract(off)
+
 namespace pgc {
 namespace {
 
@@ -119,6 +122,7 @@ __device__ __forceinline__ void store_first(char* p, u4v v, uint32_t bytes) {
 template <class T, bool kResidual>
 __device__ __forceinline__ void drop_value(const DropoutArgs& a, uint64_t key, const T* x, const T* res, T* out, uint32_t column) {
   float f = field(draw(key, column / 4), column % 4) >= a.threshold ? static_cast<float>(x[column]) * a.factor : 0.f;
+  asm("" : "+v"(f));   // rounded to 32 bits first, as in a vector: fp16's product and conversion would be fused
   if constexpr (kResidual) f += static_cast<float>(res[column]);
   out[column] = static_cast<T>(f);
 }

@@ -919,3 +919,42 @@ def test_stats_of_broken_rows(dtype, cols):
     fine = np.isfinite(e.log_sum)
     _close(stats[:, 1], e.log_sum, np.where(fine, e.sum_rel + 4 * u * np.abs(e.log_sum), 0.0), "log sums")
     assert np.isnan(_np(stats)[[4, 5, 9]]).all() and _np(stats)[1].tolist() == [-INF, 0.0]
+
+
+def _tied_products(dtype):
+    """(threshold, values): products x * factor that 32 bits round to the middle between two 16-bit numbers,
+    so that rounding once and twice differ; for types without such products any values."""
+    x = np.arange(1024, 2048)
+    for threshold in range(6000, 30000):
+        factor = np.float32(65536.0 / (65536 - threshold))
+        twice = (x.astype(np.float32) * factor).astype(np.float16)
+        ties = x[twice != (x * np.float64(factor)).astype(np.float16)]
+        if len(ties) > 1 or dtype != "f16":
+            return threshold, ties if dtype == "f16" else x
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,cols", [(65, 3), (65, 9), (65, 101), (33, 2049), (9, 4109), (9, 8193), (5, 16391), (3, 40001)])
+def test_dropout_gives_a_row_the_same_bits_wherever_it_lies(dtype, rows, cols):
+    """Values next to vectors are rounded as those in them: to 32 bits, then to the type.  In place, too."""
+    _say("dropout, same bits", dtype, rows, cols)
+    threshold, values = _tied_products(dtype)
+    rng = np.random.default_rng(cols)
+    x = torch.from_numpy(rng.choice(values, (rows, cols)).astype(np.float32) / 1024).to(DTYPES[dtype])
+    x *= torch.from_numpy(rng.choice([-1.0, 1.0], (rows, cols))).to(x.dtype)
+    r = torch.from_numpy(rng.normal(size=(rows, cols))).to(DTYPES[dtype])
+    keep = torch.from_numpy(O.keep_mask(threshold / 65536, 7, range(100, 100 + rows), cols))
+    scaled = torch.where(keep, x.float() * float(np.float32(65536.0 / (65536 - threshold))), 0.0)
+    p = threshold / 65536
+    for residual, want in [(None, scaled.to(x.dtype)), (r, (scaled + r.float()).to(x.dtype))]:
+        for pad, shift in [(0, 0), (0, 1), (1, 0), (6, 2), (8, 8), (13, 7), (63, 37), (64, 0)]:
+            xg = _place(x, pad, shift)[1]
+            rg = None if residual is None else _place(r, 2 * pad, 3 * shift)[1]
+            got = ops.dropout(xg, p, 7, residual=rg, first_row=100)
+            assert torch.equal(got.cpu(), want), (residual is None, pad, shift)
+            if rg is not None:
+                ops.dropout(xg, p, 7, residual=rg, first_row=100, out=rg)
+                assert torch.equal(rg.cpu(), want), ("out = residual", pad, shift)
+                rg.copy_(r)
+            ops.dropout(xg, p, 7, residual=rg, first_row=100, out=xg)
+            assert torch.equal(xg.cpu(), want), ("out = x", pad, shift)
