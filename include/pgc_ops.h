@@ -22,7 +22,8 @@
  *     nothing else is asked of addresses, strides and sizes.
  *   - Rows and columns number at most 2^31 - 1; a matrix may exceed 2^32 values.
  *   - An output may be the input of the same shape itself (same address and stride);
- *     apart from that an output must not overlap an input.
+ *     apart from that an output must not overlap an input.  Matrices of one stride
+ *     whose columns lie beside each other do not overlap.
  *   - Values are read as they are, computed with and summed in 32 bits (sequence
  *     sums in 64) and rounded once to the output's type, to nearest even.
  */

@@ -39,16 +39,16 @@ struct Span {
   const char* name;
   uintptr_t at = 0;
   size_t bytes = 0;
-  int64_t stride = 0;   // of a matrix, in bytes; 0: an array
+  int64_t stride = 0, row = 0;   // of a matrix: bytes from row to row and of a row; 0: an array
 };
 
 // A matrix's or an array's bytes, from its first value to its last.
 Span matrix(const char* name, const void* p, int64_t rows, int64_t cols, int64_t stride, int value) {
   const size_t last = rows > 0 ? static_cast<size_t>(rows - 1) * stride + cols : 0;
-  return {name, reinterpret_cast<uintptr_t>(p), last * value, stride * value};
+  return {name, reinterpret_cast<uintptr_t>(p), last * value, stride * value, cols * value};
 }
 Span array(const char* name, const void* p, int64_t count, int value) {
-  return {name, reinterpret_cast<uintptr_t>(p), static_cast<size_t>(count) * value, 0};
+  return {name, reinterpret_cast<uintptr_t>(p), static_cast<size_t>(count) * value};
 }
 
 int check_pointer(const Span& s, int align, bool required) {
@@ -57,12 +57,20 @@ int check_pointer(const Span& s, int align, bool required) {
   return PGC_OK;
 }
 
+// Whether two matrices are columns of one wider matrix that lie beside each other.
+bool side_by_side(const Span& a, const Span& b) {
+  if (a.stride == 0 || a.stride != b.stride) return false;
+  const uintptr_t stride = static_cast<uintptr_t>(a.stride);
+  const uintptr_t from_b = a.at >= b.at ? (a.at - b.at) % stride : (stride - (b.at - a.at) % stride) % stride;
+  return from_b >= static_cast<uintptr_t>(b.row) && from_b + a.row <= stride;
+}
+
 // An output may be an input itself where both are matrices of the same shape, else they
 // must lie apart.
 int check_apart(const Span& out, const Span& in, bool may_be_same) {
   if (out.at == 0 || in.at == 0 || out.bytes == 0 || in.bytes == 0) return PGC_OK;
   if (may_be_same && out.at == in.at && out.stride == in.stride) return PGC_OK;
-  if (out.at < in.at + in.bytes && in.at < out.at + out.bytes)
+  if (out.at < in.at + in.bytes && in.at < out.at + out.bytes && !side_by_side(out, in))
     return fail(PGC_EINVAL, "%s overlaps %s", out.name, in.name);
   return PGC_OK;
 }
@@ -261,7 +269,7 @@ int pgc_preference_loss(const pgc_logits* logits, const pgc_preference_args* a, 
   if (a->dlogits) CHECK(check_dlogits(logits, a->dlogits, a->dlogits_stride));
   size_t need = 0;
   CHECK(pgc_preference_workspace_bytes(logits, pairs, &need));
-  const Span ws = {"workspace", reinterpret_cast<uintptr_t>(workspace), need, 0};
+  const Span ws = {"workspace", reinterpret_cast<uintptr_t>(workspace), need};
   CHECK(check_pointer(ws, kAlign, true));
   if (workspace_bytes < need)
     return fail(PGC_EINVAL, "workspace too small: need %zu bytes", need);

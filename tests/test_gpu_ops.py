@@ -958,3 +958,28 @@ def test_dropout_gives_a_row_the_same_bits_wherever_it_lies(dtype, rows, cols):
                 rg.copy_(r)
             ops.dropout(xg, p, 7, residual=rg, first_row=100, out=xg)
             assert torch.equal(xg.cpu(), want), ("out = x", pad, shift)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [7, 100, 515, 4109, 9001])
+def test_columns_of_one_tensor_as_input_and_output(dtype, cols):
+    """Columns that lie beside the input's are no overlap: the same bits as with tensors of their own."""
+    _say("side by side", dtype, cols)
+    rows = 9
+    z, y = _case(dtype, rows, cols, 5)
+    zg, y = z.cuda(), y.cuda()
+    f = torch.linspace(-1, 1, rows, device="cuda")
+    lp, stats = ops.token_logprobs(zg, y)
+    o = torch.tensor([0, 4, rows], dtype=torch.int32, device="cuda")
+    calls = [lambda a, out: ops.dropout(a, 0.3, 5, out=out), lambda a, out: ops.token_logprobs_backward(a, y, stats, f, out=out),
+             lambda a, out: ops.policy_loss(a, y, lp, f, out=out)[2], lambda a, out: ops.preference_loss(a, y, o, lp, out=out)[3]]
+    for call in calls:
+        want = call(zg, None)
+        for a, b, width in [(0, cols, 2 * cols), (cols + 1, 0, 2 * cols + 1), (3, cols + 5, 2 * cols + 9)]:
+            both = torch.full((rows, width), 55.0, dtype=z.dtype, device="cuda")
+            left, right = both[:, a:a + cols], both[:, b:b + cols]
+            left.copy_(zg)
+            assert torch.equal(call(left, right), want) and torch.equal(left, zg)
+            left.fill_(55.0)
+            right.fill_(55.0)
+            assert (both == 55.0).all()

@@ -365,3 +365,13 @@ def test_oracle_policy_loss_of_a_target_that_cannot_occur():
     for advantage, want in [(1.0, 0.0), (-1.0, 0.8)]:
         loss, _, grad = O.policy(z, y, -one, advantage * one)
         assert loss.tolist() == [want, want] and not grad.any()
+
+
+@pytest.mark.parametrize("offset,apart", [(10, True), (12, True), (-12, True), (-10, True), (9, False), (13, False), (-13, False),
+                                          (-9, False), (22 + 12, True), (22 + 13, False), (5, False), (22, False), (-22, False)])
+def test_columns_beside_each_other_do_not_overlap(offset, apart):
+    """x has columns 0 to 9 of rows of 22 values, the output 10 columns further on (or ahead).  A pointer that is
+    refused last tells which refusal it was: that of overlap comes first."""
+    out = BASE + 2 * offset
+    args = _dropout_args(x_stride=22, out_stride=22, out=out, row_ids=out // 8 * 8)
+    _refused(ops.lib().pgc_dropout(ctypes.byref(args), None), "out overlaps row_ids" if apart else "out overlaps x")
