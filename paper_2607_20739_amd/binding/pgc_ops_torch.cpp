@@ -4,12 +4,14 @@
 // allocations take 4 to 9 us in Python.
 //
 // Functions take all arguments, by position; ops.py gives them their names and defaults.  Tensors
-// that do not fit raise ValueError, what the library refuses raises PGCError.
+// that do not fit raise ValueError, tensors with a tangent NotImplementedError, what the library
+// refuses raises PGCError.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty_cuda_dispatch.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -36,7 +38,11 @@ int dtype_of(const at::Tensor& t) {
 
 const at::Tensor& tensor(const char* name, PyObject* o) {
   TORCH_CHECK_VALUE(THPVariable_Check(o), name, " must be a tensor");
-  return THPVariable_Unpack(o);
+  const at::Tensor& t = THPVariable_Unpack(o);
+  // Otherwise the result would have no tangent, which counts as 0.
+  TORCH_CHECK_NOT_IMPLEMENTED(!t._fw_grad(0).defined() || !c10::AutogradState::get_tls_state().get_fw_grad_mode(),
+                              "forward-mode derivatives of the operators are not implemented, and ", name, " carries a tangent");
+  return t;
 }
 
 // Row stride of a matrix whose shape has been looked at.

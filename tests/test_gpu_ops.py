@@ -983,3 +983,31 @@ def test_columns_of_one_tensor_as_input_and_output(dtype, cols):
             left.fill_(55.0)
             right.fill_(55.0)
             assert (both == 55.0).all()
+
+
+def test_forward_mode_derivatives_are_refused():
+    """A result without a tangent would count as one whose tangent is 0."""
+    _say("forward mode")
+    import torch.autograd.forward_ad as fw
+    z, v = torch.randn(6, 40, device="cuda"), torch.randn(6, 40, device="cuda")
+    y = torch.zeros(6, dtype=torch.int32, device="cuda")
+    f = torch.zeros(6, device="cuda")
+    o = torch.tensor([0, 3, 6], dtype=torch.int32, device="cuda")
+    stats = ops.token_logprobs(z, y)[1]
+    with fw.dual_level():
+        for primal in (z, z.clone().requires_grad_()):
+            d = fw.make_dual(primal, v)
+            for call in (lambda: ops.dropout(d, 0.1, 1), lambda: ops.dropout(z, 0.1, 1, residual=d),
+                         lambda: ops.token_logprobs(d, y)):
+                with pytest.raises(NotImplementedError):
+                    call()
+        d, df = fw.make_dual(z, v), fw.make_dual(f, f + 1)
+        for call in (lambda: ops.dropout_backward(d, 0.1, 1), lambda: ops.token_logprobs_backward(d, y, stats, f),
+                     lambda: ops.token_logprobs_backward(z, y, stats, df), lambda: ops.preference_loss(d, y, o),
+                     lambda: ops.preference_loss(z, y, o, ref_logprobs=df), lambda: ops.policy_loss(d, y, f, f),
+                     lambda: ops.policy_loss(z, y, f, df)):
+            with pytest.raises(NotImplementedError, match="tangent"):
+                call()
+        primal = fw.unpack_dual(d).primal
+        assert torch.equal(ops.dropout(primal, 0.1, 1), ops.dropout(z, 0.1, 1))   # without its tangent
+    assert ops.dropout(z, 0.1, 1).shape == z.shape
