@@ -4,15 +4,17 @@
 // allocations take 4 to 9 us in Python.
 //
 // Functions take all arguments, by position; ops.py gives them their names and defaults.  Tensors
-// that do not fit raise ValueError, tensors with a tangent NotImplementedError, what the library
-// refuses raises PGCError.
+// that do not fit raise ValueError, tensors with a tangent and traces NotImplementedError, what the
+// library refuses raises PGCError.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/TracerMode.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty_cuda_dispatch.h>
 #include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
@@ -60,6 +62,10 @@ struct Matrix {
   int dtype;
 
   Matrix(const char* name, PyObject* o) : t(tensor(name, o)), dtype(dtype_of(t)) {
+    // A trace would take the result for a constant.
+    using Modes = c10::impl::TorchDispatchModeTLS;
+    TORCH_CHECK_NOT_IMPLEMENTED(!at::tracer::impl::is_dispatch_enabled() && !Modes::get_mode(c10::impl::TorchDispatchModeKey::PROXY),
+                                "the operators cannot be recorded in a trace");
     TORCH_CHECK_VALUE(t.dim() == 2 && dtype >= 0 && t.is_cuda() && t.layout() == at::kStrided,
                       name, " must be a 2-D float32, bfloat16 or float16 tensor on the GPU");
     rows = t.size(0);

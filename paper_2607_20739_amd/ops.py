@@ -5,7 +5,7 @@ that is a function of seed, row number and column; log-probabilities of given to
 preference loss of pairs of sequences; the clipped policy loss with a KL term.  The losses take
 logits and return the loss and the logits' gradient; `logits.backward(dlogits)` carries it on
 through a model.  dropout and token_logprobs take part in autograd where an input asks for it (backward;
-forward-mode derivatives are refused).
+forward-mode derivatives are refused, and so are traces by torch.jit.trace and make_fx).
 
 Tensors live on one GPU; matrices are 2-D float32, bfloat16 or float16 with adjacent columns and
 any row stride; tokens are int32 with -1 (or anything outside of [0, columns)) for "no token".

@@ -1011,3 +1011,23 @@ def test_forward_mode_derivatives_are_refused():
         primal = fw.unpack_dual(d).primal
         assert torch.equal(ops.dropout(primal, 0.1, 1), ops.dropout(z, 0.1, 1))   # without its tangent
     assert ops.dropout(z, 0.1, 1).shape == z.shape
+
+
+@pytest.mark.parametrize("requires_grad", [False, True])
+def test_traces_are_refused(requires_grad):
+    """torch.jit.trace and make_fx would record a result as a constant and give it for other inputs, too."""
+    _say("traces", requires_grad)
+    from torch.fx.experimental.proxy_tensor import make_fx
+    z = torch.randn(6, 40, device="cuda", requires_grad=requires_grad)
+    y = torch.zeros(6, dtype=torch.int32, device="cuda")
+    f = torch.zeros(6, device="cuda")
+    o = torch.tensor([0, 3, 6], dtype=torch.int32, device="cuda")
+    stats = ops.token_logprobs(z.detach(), y)[1]
+    for call in (lambda a: a + ops.dropout(a, 0.1, 1), lambda a: a + ops.dropout_backward(a, 0.1, 1),
+                 lambda a: a.sum() + ops.token_logprobs(a, y)[0], lambda a: a + ops.token_logprobs_backward(a, y, stats, f),
+                 lambda a: a.sum() + ops.preference_loss(a, y, o)[0], lambda a: a.sum() + ops.policy_loss(a, y, f, f)[0]):
+        with pytest.raises(NotImplementedError, match="trace"):
+            torch.jit.trace(call, (z,), check_trace=False)
+        with pytest.raises(NotImplementedError, match="trace"):
+            make_fx(call)(z.detach())
+    assert ops.dropout(z.detach(), 0.1, 1).shape == z.shape
