@@ -41,6 +41,7 @@ int dtype_of(const at::Tensor& t) {
 const at::Tensor& tensor(const char* name, PyObject* o) {
   TORCH_CHECK_VALUE(THPVariable_Check(o), name, " must be a tensor");
   const at::Tensor& t = THPVariable_Unpack(o);
+  TORCH_CHECK_VALUE(!t.is_neg(), name, " must not be a view that negates its values on reading (resolve_neg() writes them out)");
   // Otherwise the result would have no tangent, which counts as 0.
   TORCH_CHECK_NOT_IMPLEMENTED(!t._fw_grad(0).defined() || !c10::AutogradState::get_tls_state().get_fw_grad_mode(),
                               "forward-mode derivatives of the operators are not implemented, and ", name, " carries a tangent");

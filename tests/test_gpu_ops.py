@@ -1031,3 +1031,19 @@ def test_traces_are_refused(requires_grad):
         with pytest.raises(NotImplementedError, match="trace"):
             make_fx(call)(z.detach())
     assert ops.dropout(z.detach(), 0.1, 1).shape == z.shape
+
+
+def test_views_that_negate_are_refused():
+    """The imaginary part of a conjugate holds the values with the other sign, and a mark."""
+    _say("negated views")
+    z = torch.randn(6, 1, dtype=torch.complex64, device="cuda")
+    neg, real = z.conj().imag, z.real.contiguous()
+    y = torch.zeros(6, dtype=torch.int32, device="cuda")
+    f, minus = torch.ones(6, device="cuda"), torch._neg_view(torch.ones(6, device="cuda"))
+    assert neg.is_neg() and minus.is_neg()
+    for call in (lambda: ops.dropout(neg, 0.0, 1), lambda: ops.dropout(real, 0.0, 1, residual=neg),
+                 lambda: ops.dropout(real, 0.0, 1, out=neg), lambda: ops.token_logprobs(neg, y),
+                 lambda: ops.policy_loss(real, y, f, minus), lambda: ops.policy_loss(real, y, f, f, token_weights=minus)):
+        with pytest.raises(ValueError, match="resolve_neg"):
+            call()
+    assert torch.equal(ops.dropout(neg.resolve_neg(), 0.0, 1), -z.imag)
