@@ -11,6 +11,7 @@
 
 #include <ATen/TracerMode.h>
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty_cuda_dispatch.h>
 #include <c10/core/AutogradState.h>
 #include <c10/core/DeviceGuard.h>
@@ -102,18 +103,22 @@ struct Matrix {
   }
 };
 
-// The tensor that receives a result of a matrix's shape: `o`, or a new one for None.
+// The tensor that receives a result of a matrix's shape: `o`, or a new one for None.  One that asks
+// for a gradient would lose its own history unnoticed.  Only `over_logits` may: logits that a model
+// computed are replaced by their gradient, with which the model's backward pass starts.
 struct Output {
   at::Tensor t;
   int64_t stride;
 
-  Output(const Matrix& like, PyObject* o) {
+  Output(const Matrix& like, PyObject* o, bool over_logits) {
     if (o == Py_None) {
       t = like.empty({like.rows, like.cols}, like.t.scalar_type());
       stride = like.cols;
     } else {
       t = tensor("out", o);
       stride = like.like("out", t);
+      TORCH_CHECK_VALUE(!t.requires_grad() || !at::GradMode::is_enabled() || (over_logits && !t.is_leaf() && t.data_ptr() == like.data()),
+                        "out must not ask for a gradient (detach() it)");
       if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();   // autograd notices a saved tensor that this changes
     }
   }
@@ -189,7 +194,7 @@ PyObject* dropout_by(int (*entry)(const pgc_dropout_args*, void*), PyObject* con
   k.p = number(a[1]);
   k.seed = integer(a[2]);
   k.first_row = static_cast<int64_t>(integer(a[5]));
-  const Output out(x, a[6]);
+  const Output out(x, a[6], false);
   k.x = x.data();
   k.out = out.t.data_ptr();
   k.rows = x.rows;
@@ -237,7 +242,7 @@ PyObject* token_logprobs_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const int32_t* targets = x.ints("targets", a[1], x.rows);
   const float* stats = static_cast<float*>(x.array("stats", a[2], at::kFloat, {x.rows, 2}));
   const float* grad = x.floats("grad", a[3], x.rows);
-  const Output out(x, a[4]);
+  const Output out(x, a[4], true);
   const pgc_logits z = x.logits();
   launch(x, [&](void* stream) { return pgc_token_logprobs_backward(&z, targets, stats, grad, out.t.data_ptr(), out.stride, stream); });
   return THPVariable_Wrap(out.t);
@@ -277,7 +282,7 @@ PyObject* preference_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor logprobs = x.empty({x.rows}, at::kFloat);
   at::Tensor dlogits;
   if (flag(a[8])) {
-    const Output out(x, a[9]);
+    const Output out(x, a[9], true);
     dlogits = out.t;
     k.dlogits = dlogits.data_ptr();
     k.dlogits_stride = out.stride;
@@ -309,7 +314,7 @@ PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const at::Tensor loss = x.empty({x.rows}, at::kFloat), logprobs = x.empty({x.rows}, at::kFloat);
   at::Tensor dlogits;
   if (flag(a[10])) {
-    const Output out(x, a[11]);
+    const Output out(x, a[11], true);
     dlogits = out.t;
     k.dlogits = dlogits.data_ptr();
     k.dlogits_stride = out.stride;

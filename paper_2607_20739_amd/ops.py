@@ -7,6 +7,8 @@ logits and return the loss and the logits' gradient; `logits.backward(dlogits)` 
 through a model.  dropout and token_logprobs take part in autograd where an input asks for it (backward;
 forward-mode derivatives are refused, and so are traces by torch.jit.trace and make_fx).
 
+`out` must not ask for a gradient itself, unless it is the logits and a model's output.
+
 Tensors live on one GPU; matrices are 2-D float32, bfloat16 or float16 with adjacent columns and
 any row stride; tokens are int32 with -1 (or anything outside of [0, columns)) for "no token".
 Work is enqueued on torch's current stream of that GPU, outputs are new tensors of that stream.

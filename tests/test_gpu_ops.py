@@ -1047,3 +1047,35 @@ def test_views_that_negate_are_refused():
         with pytest.raises(ValueError, match="resolve_neg"):
             call()
     assert torch.equal(ops.dropout(neg.resolve_neg(), 0.0, 1), -z.imag)
+
+
+def test_outputs_that_ask_for_a_gradient_are_refused():
+    """Parameters and a graph's tensors are not overwritten unnoticed; logits may be replaced by their gradient."""
+    _say("out asks for a gradient")
+    z = torch.randn(6, 40, device="cuda")
+    y = torch.zeros(6, dtype=torch.int32, device="cuda")
+    f = torch.linspace(-1, 1, 6, device="cuda")
+    o = torch.tensor([0, 3, 6], dtype=torch.int32, device="cuda")
+    lp, stats = ops.token_logprobs(z, y)
+    calls = [lambda a, out: ops.dropout(a, 0.1, 1, out=out), lambda a, out: ops.dropout_backward(a, 0.1, 1, out=out),
+             lambda a, out: ops.token_logprobs_backward(a, y, stats, f, out=out),
+             lambda a, out: ops.preference_loss(a, y, o, lp + f, out=out)[3], lambda a, out: ops.policy_loss(a, y, lp, f, out=out)[2]]
+    leaf = torch.full((6, 40), 5.0, device="cuda", requires_grad=True)
+    inner = leaf + 0
+    for call in calls:
+        for out in (leaf, inner, inner[:, :]):
+            with pytest.raises(ValueError, match="out must not ask for a gradient"):
+                call(z, out)
+            with pytest.raises(ValueError):
+                call(leaf, leaf)
+        assert (leaf == 5.0).all() and (inner == 5.0).all()
+        want = call(z, None)
+        with torch.no_grad():
+            assert torch.equal(call(z, torch.zeros(6, 40, device="cuda", requires_grad=True)), want)
+    for call in calls[2:]:
+        w = z.clone().requires_grad_()
+        logits = w * 1
+        want = call(z, None)
+        assert call(logits, logits) is logits
+        logits.backward(logits.detach())
+        assert torch.equal(w.grad, want)
