@@ -4,7 +4,7 @@ Binding of include/pgc_ops.h (through binding/pgc_ops_torch.cpp), which states w
 that is a function of seed, row number and column; log-probabilities of given tokens; the
 preference loss of pairs of sequences; the clipped policy loss with a KL term.  The losses take
 logits and return the loss and the logits' gradient; `logits.backward(dlogits)` carries it on
-through a model.  dropout and token_logprobs take part in autograd where an input asks for it (backward;
+through a model, and a backward pass through the loss itself raises.  dropout and token_logprobs take part in autograd where an input asks for it (backward;
 forward-mode derivatives are refused, and so are traces by torch.jit.trace and make_fx).
 
 `out` must not ask for a gradient itself, unless it is the logits and a model's output.
@@ -160,8 +160,8 @@ def preference_loss(logits, targets, offsets, ref_logprobs=None, beta=0.1, label
     `out` receives it and may be the logits.  `workspace` (uint8, preference_workspace_bytes(logits,
     pairs)) is allocated where it is not given.
     """
-    return _native.preference_loss(logits, targets, offsets, ref_logprobs, beta, label_smoothing, scale, pair_weights,
-                                   gradient, out, workspace)
+    return _marked(logits, _native.preference_loss(logits, targets, offsets, ref_logprobs, beta, label_smoothing, scale,
+                                                   pair_weights, gradient, out, workspace))
 
 
 def policy_loss(logits, targets, old_logprobs, advantages, ref_logprobs=None, clip_low=0.2, clip_high=0.2, kl=0.0,
@@ -171,8 +171,15 @@ def policy_loss(logits, targets, old_logprobs, advantages, ref_logprobs=None, cl
     dlogits is the gradient of scale * sum(token_weights * loss), None with gradient=False.  `out`
     receives it and may be the logits.
     """
-    return _native.policy_loss(logits, targets, old_logprobs, advantages, ref_logprobs, clip_low, clip_high, kl, scale,
-                               token_weights, gradient, out)
+    return _marked(logits, _native.policy_loss(logits, targets, old_logprobs, advantages, ref_logprobs, clip_low, clip_high,
+                                               kl, scale, token_weights, gradient, out))
+
+
+def _marked(logits, results):
+    """A loss's results (dlogits last): part of a sum that is differentiated, they say so instead of missing in it."""
+    if torch.is_grad_enabled() and logits.requires_grad:
+        return (*_LossWithoutGraph.apply(logits, results[:-1]), results[-1])
+    return results
 
 
 # ---- autograd -------------------------------------------------------------------------------
@@ -221,3 +228,15 @@ class _TokenLogprobsGradient(torch.autograd.Function):
     @staticmethod
     def backward(ctx, _):
         raise RuntimeError("the gradient of token_logprobs is not differentiable")
+
+
+class _LossWithoutGraph(torch.autograd.Function):
+    """Values whose gradient has been computed already."""
+
+    @staticmethod
+    def forward(ctx, logits, values):
+        return values
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the losses' gradient is their result dlogits: call logits.backward(dlogits)")

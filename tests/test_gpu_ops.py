@@ -1079,3 +1079,30 @@ def test_outputs_that_ask_for_a_gradient_are_refused():
         assert call(logits, logits) is logits
         logits.backward(logits.detach())
         assert torch.equal(w.grad, want)
+
+
+def test_losses_in_a_differentiated_sum_raise():
+    """Without a graph they would be missing in the sum's gradient, without a word."""
+    _say("losses without a graph")
+    w = torch.randn(6, 40, device="cuda", requires_grad=True)
+    y = torch.zeros(6, dtype=torch.int32, device="cuda")
+    f = torch.linspace(-1, 1, 6, device="cuda")
+    o = torch.tensor([0, 3, 6], dtype=torch.int32, device="cuda")
+    for call in (lambda a, **kw: ops.preference_loss(a, y, o, f, **kw), lambda a, **kw: ops.policy_loss(a, y, f, f, **kw)):
+        z = w * 2
+        got = call(z)
+        for gradient in (True, False):
+            for value in call(z, gradient=gradient)[:-1]:
+                with pytest.raises(RuntimeError, match="dlogits"):
+                    ((w * w).sum() + value.sum()).backward(retain_graph=True)
+        assert w.grad is None
+        want = call(z.detach())
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+        assert not got[-1].requires_grad and call(z, gradient=False)[-1] is None
+        z.backward(got[-1])
+        assert torch.equal(w.grad, 2 * want[-1])
+        w.grad = None
+        with torch.no_grad():
+            assert not any(t.requires_grad for t in call(z))
+        assert not any(t.requires_grad for t in call(z.detach()))
