@@ -112,7 +112,9 @@ def dropout(x, p, seed, residual=None, row_ids=None, first_row=0, out=None):
     first_row + i.  Use another seed for each step and layer (pgc_splitmix64(seed, t)).
     `out` may be x or residual (not under autograd).
     """
-    if torch.is_grad_enabled() and (x.requires_grad or residual is not None and residual.requires_grad):
+    # What is no tensor is left to the binding, which refuses it.
+    if torch.is_grad_enabled() and (getattr(x, "requires_grad", False) or
+                                    residual is not None and getattr(residual, "requires_grad", False)):
         if out is not None:
             raise ValueError("out cannot be given where a gradient is asked for")
         return _Dropout.apply(x, residual, p, seed, row_ids, first_row)
@@ -129,7 +131,7 @@ def dropout_backward(dout, p, seed, row_ids=None, first_row=0, out=None):
 def token_logprobs(logits, targets):
     """(logprobs [rows], stats [rows, 2]): each row's log-probability of its target, and its maximum
     and the log of its sum of exp(z - maximum), which the backward pass takes."""
-    if torch.is_grad_enabled() and logits.requires_grad:
+    if torch.is_grad_enabled() and getattr(logits, "requires_grad", False):
         return _TokenLogprobs.apply(logits, targets)
     return _native.token_logprobs(logits, targets)
 

@@ -375,3 +375,13 @@ def test_columns_beside_each_other_do_not_overlap(offset, apart):
     out = BASE + 2 * offset
     args = _dropout_args(x_stride=22, out_stride=22, out=out, row_ids=out // 8 * 8)
     _refused(ops.lib().pgc_dropout(ctypes.byref(args), None), "out overlaps row_ids" if apart else "out overlaps x")
+
+
+@pytest.mark.parametrize("what", [None, 3.0, [[1.0, 2.0]], np.zeros((3, 4), np.float32)])
+def test_what_is_no_tensor_is_refused(what):
+    y, f = torch.zeros(3, dtype=torch.int32), torch.zeros(3)
+    for call, name in [(lambda: ops.dropout(what, 0.1, 1), "x"), (lambda: ops.dropout_backward(what, 0.1, 1), "x"),
+                       (lambda: ops.token_logprobs(what, y), "logits"), (lambda: ops.token_logprobs_backward(what, y, f, f), "logits"),
+                       (lambda: ops.preference_loss(what, y, y), "logits"), (lambda: ops.policy_loss(what, y, f, f), "logits")]:
+        with pytest.raises(ValueError, match=name + " must be a tensor"):
+            call()
