@@ -11,10 +11,12 @@ the host pass reports the feature as unknown, which is harmless and not shown;
 other warnings go to stderr) and linked
 into paper_2607_20739_amd/libpgc.so next to this file, linked against ROCm's
 roctx library for the per-step profiler ranges.  binding/pgc_ops_torch.cpp becomes
-paper_2607_20739_amd/_ops_torch.so, linked against that library and the installed torch.
+paper_2607_20739_amd/_ops_torch.so, linked against that library and the installed torch; where
+there is none, the library is built alone.
 """
 
 import concurrent.futures
+import importlib.util
 import os
 import shutil
 import subprocess
@@ -83,20 +85,35 @@ def _link(what, lib, cmd):
     os.replace(tmp, lib)
 
 
-def build(verbose=False):
-    """Compile and link libpgc.so and the torch binding; returns libpgc.so's path."""
-    import torch
-    os.makedirs(BUILD_DIR, exist_ok=True)
-    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as pool:
-        *objs, binding = pool.map(_compile, SOURCES + [BINDING])
+def _link_library(objs):
     _link("libpgc.so", LIB, [hipcc(), "--offload-arch=" + ARCH] + objs +
           ["-L" + ROCM_LIB, "-Wl,-rpath," + ROCM_LIB, "-lrocprofiler-sdk-roctx"])
+
+
+def _link_binding(obj):
+    import torch
     torch_lib = os.path.join(os.path.dirname(torch.__file__), "lib")
-    _link("_ops_torch.so", BINDING_LIB, ["g++", binding, "-L" + PKG, "-lpgc", "-Wl,-rpath,$ORIGIN", "-L" + torch_lib,
+    _link("_ops_torch.so", BINDING_LIB, ["g++", obj, "-L" + PKG, "-lpgc", "-Wl,-rpath,$ORIGIN", "-L" + torch_lib,
                                          "-lc10", "-ltorch_cpu", "-ltorch_hip", "-ltorch_python"])
+
+
+def build(verbose=False):
+    """Compile and link libpgc.so, then the torch binding; returns libpgc.so's path.
+
+    The library needs no torch: it is there also where the binding cannot be built, which raises.  Without
+    torch there is nothing to bind, and the binding is left out.
+    """
+    os.makedirs(BUILD_DIR, exist_ok=True)
+    bind = importlib.util.find_spec("torch") is not None
+    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as pool:
+        binding = pool.submit(_compile, BINDING) if bind else None
+        _link_library(list(pool.map(_compile, SOURCES)))
+        if verbose:
+            print("built", LIB)
+        if bind:
+            _link_binding(binding.result())
     if verbose:
-        print("built", LIB)
-        print("built", BINDING_LIB)
+        print("built " + BINDING_LIB if bind else "no torch: %s is left out" % BINDING_LIB)
     return LIB
 
 

@@ -8,6 +8,7 @@ import concurrent.futures
 import os
 import re
 import subprocess
+import sys
 
 import pytest
 
@@ -50,3 +51,45 @@ def test_inline_assembly_that_loads_registers_waits_for_them():
                 blocks += 1
                 assert "s_waitcnt" in block, (name, block[:120])
     assert blocks >= 2
+
+
+@pytest.fixture
+def recorded(monkeypatch, tmp_path):
+    """build() with its commands written down instead of run; those named in `failing` fail."""
+    ran, failing = [], set()
+
+    def run(what, cmd):
+        name = os.path.basename(what.split()[-1])
+        ran.append(name)
+        if name in failing:
+            raise RuntimeError(name + " failed")
+
+    monkeypatch.setattr(B, "_run", run)
+    monkeypatch.setattr(B, "hipcc", lambda: "hipcc")
+    monkeypatch.setattr(B, "BUILD_DIR", str(tmp_path))
+    monkeypatch.setattr(B.os, "replace", lambda a, b: None)
+    return ran, failing
+
+
+@pytest.mark.parametrize("failing", ["pgc_ops_torch.cpp", "_ops_torch.so"])
+def test_the_library_is_linked_where_the_binding_cannot_be_built(recorded, failing):
+    ran, fail = recorded
+    fail.add(failing)
+    with pytest.raises(RuntimeError, match=failing):
+        B.build()
+    assert "libpgc.so" in ran and set(B.SOURCES) <= set(ran)
+
+
+def test_the_library_builds_without_torch(recorded, monkeypatch):
+    ran, _ = recorded
+    monkeypatch.setattr(B.importlib.util, "find_spec", lambda name: None)
+    monkeypatch.setitem(sys.modules, "torch", None)      # importing it raises
+    assert B.build() == B.LIB
+    assert ran[-1] == "libpgc.so" and set(ran[:-1]) == set(B.SOURCES)
+
+
+def test_the_binding_is_linked_after_the_library(recorded):
+    ran, _ = recorded
+    assert B.build() == B.LIB
+    assert ran[-1] == "_ops_torch.so" and "libpgc.so" in ran
+    assert "pgc_ops_torch.cpp" in ran
