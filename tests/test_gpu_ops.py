@@ -1106,3 +1106,64 @@ def test_losses_in_a_differentiated_sum_raise():
         with torch.no_grad():
             assert not any(t.requires_grad for t in call(z))
         assert not any(t.requires_grad for t in call(z.detach()))
+
+
+# More rows than the grid's first dimensions hold: 2^20 blocks (x), 65,535 (y of the kernels whose x goes along a row).
+GRID_ROWS = (1 << 20) + 3
+
+
+def _ends(rows):
+    """The first rows, those around either limit and the last, as slices."""
+    return [slice(a, min(rows, a + 5)) for a in (0, 65_533, (1 << 20) - 2, rows - 5) if a < rows]
+
+
+@pytest.mark.parametrize("dtype,cols", [("bf16", 4112), ("f16", 1031), ("f32", 300)])
+def test_more_rows_than_one_grid_dimension(dtype, cols):
+    """A block, half of one or a quarter per row: rows around the limits have the bits that they have alone."""
+    rows = 8 * GRID_ROWS if cols == 300 else 4 * GRID_ROWS if cols == 1031 else GRID_ROWS
+    _say("grid", dtype, rows, cols)
+    z = torch.empty(rows, cols, dtype=DTYPES[dtype], device="cuda").fill_(0.25)
+    y = torch.full((rows,), -1, dtype=torch.int32, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    ends = _ends(rows)
+    for part in ends:
+        z[part].normal_(generator=gen)
+        y[part] = torch.randint(0, cols, (len(y[part]),), generator=gen, device="cuda").to(torch.int32)
+    alone = [z[part].clone() for part in ends]
+    f = torch.linspace(-1, 1, rows, device="cuda")
+    lp, stats = ops.token_logprobs(z, y)
+    want = [ops.token_logprobs(a, y[part]) for a, part in zip(alone, ends)]
+    for (l, s), part in zip(want, ends):
+        assert torch.equal(lp[part], l) and torch.equal(stats[part], s) and l.isfinite().all()
+    assert int((lp != 0).sum()) == int((y >= 0).sum())
+    out = ops.token_logprobs_backward(z, y, stats, f)
+    for a, (_, s), part in zip(alone, want, ends):
+        assert torch.equal(out[part], ops.token_logprobs_backward(a, y[part], s, f[part]))
+    loss, _, _ = ops.policy_loss(z, y, lp, f, out=out)
+    for a, (l, _), part in zip(alone, want, ends):
+        got = ops.policy_loss(a, y[part], l, f[part])
+        assert torch.equal(loss[part], got[0]) and torch.equal(out[part], got[2])
+    assert int((loss != 0).sum()) == int((y >= 0).sum())
+    ops.dropout(z, 0.3, 5, first_row=7, out=out)
+    for a, part in zip(alone, ends):
+        assert torch.equal(out[part], ops.dropout(a, 0.3, 5, first_row=7 + part.start))
+    # The untouched rows in between, by a second call over all but the first.
+    z, first = z[1:], out[1:]
+    assert torch.equal(ops.dropout(z, 0.3, 5, first_row=8), first)
+
+
+def test_more_short_rows_than_one_grid_dimension():
+    """256 rows to a block, one value each: 2^28 rows and some."""
+    rows = (1 << 28) + 77
+    _say("grid, short rows", rows)
+    z = torch.zeros(rows, 1, dtype=torch.bfloat16, device="cuda")
+    y = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    y[-80:-70] = -1
+    lp, stats = ops.token_logprobs(z + 2, y)
+    assert not lp.any() and int((stats[:, 0] == 2.0).sum()) == rows - 10 and not stats[-80:-70].any()
+    out = ops.dropout(z + 1, 0.5, 3)
+    want = ops.dropout(z[-300:] + 1, 0.5, 3, first_row=rows - 300)
+    assert torch.equal(out[-300:], want)
+    # Of so many fair draws the kept ones number half, to five standard deviations.
+    assert abs(int((out != 0).sum()) - rows / 2) < 5 * (rows / 4) ** 0.5
+    assert (out[: 1 << 20] == ops.dropout(z[: 1 << 20] + 1, 0.5, 3)).all()
