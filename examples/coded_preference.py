@@ -83,24 +83,41 @@ class Head:
 
 
 class Coded:
-    """The workers' rings and the master's decode on the library's placement and coefficients."""
+    """The workers' rings and the master's decode on the library's placement and coefficients.
 
-    def __init__(self, scheme, n, c, q, device):
-        self.n, self.c, self.scheme = n, c, scheme
+    With each_worker every worker evaluates its own copy of a partition and keeps a ring of its own.  Otherwise one
+    evaluation serves all holders of a partition, which gives the same words as long as its gradient does not depend on
+    who computes it.
+    """
+
+    def __init__(self, scheme, n, c, q, device, each_worker=False):
+        self.n, self.c, self.scheme, self.each_worker = n, c, scheme, each_worker
         self.ctx = P.pgc_init(scheme, n, c, 4)           # for its tables alone
         P.pgc_configure(self.ctx, "lsq", n, 4)
         self.placement = P.pgc_placement(self.ctx, n, c)
-        self.ring = torch.zeros(c, n, q, device=device)  # [slot][partition]
+        # [slot][worker], or, for all holders together, [slot][partition].
+        self.ring = torch.zeros(c, n, q, device=device)
         self.t = 0
 
+    def place(self, worker, slot):
+        """Where the worker's copy in that slot lies in the ring."""
+        return worker if self.each_worker else int(self.placement[worker][slot])
+
+    def word(self, worker):
+        return sum(self.ring[slot, self.place(worker, slot)] for slot in range(self.c))
+
     def step(self, evaluate, straggler_mask):
-        """One step: evaluate(partition) -> gradient; returns the decoded gradient."""
+        """One step: evaluate(worker, partition) -> gradient; returns the decoded gradient."""
         slots = range(self.c) if self.t == 0 else [(self.t - 1) % self.c]
         fresh = {}
         for slot in slots:
-            for k in {int(self.placement[i][slot]) for i in range(self.n)}:
-                if k not in fresh:                       # workers that hold it compute the same
-                    fresh[k] = evaluate(k)
+            for worker in range(self.n):
+                k = int(self.placement[worker][slot])
+                if self.each_worker:
+                    self.ring[slot, worker] = evaluate(worker, k)
+                    continue
+                if k not in fresh:
+                    fresh[k] = evaluate(worker, k)
                 # FR: a group's members share their copies; CR: the slot is one worker's own.
                 for s in range(self.c) if self.scheme == "FR" else [slot]:
                     self.ring[s, k] = fresh[k]
@@ -108,8 +125,7 @@ class Coded:
         ghat = torch.zeros_like(self.ring[0, 0])
         for j, weight in zip(survivors, d):
             if weight != 0:
-                word = sum(self.ring[s, int(self.placement[j][s])] for s in range(self.c))
-                ghat += float(weight) * word
+                ghat += float(weight) * self.word(j)
         self.t += 1
         return ghat * scale
 
@@ -118,8 +134,9 @@ class Coded:
 
 
 def train(scheme="FR", n=4, c=2, steps=40, policy_steps=20, pairs=6, longest=12, width=64, vocab=1000, lr=0.2, policy_lr=0.1, p=0.1,
-          mask_seed=3, device="cuda"):
-    """Both phases; returns {"preference": losses, "accuracy": of the pairs, "policy": losses, "w": parameters}."""
+          mask_seed=3, device="cuda", each_worker=False):
+    """Both phases; returns {"preference": losses, "accuracy": of the pairs, "policy": losses, "w": parameters,
+    "words": each worker's word of each step, where each evaluates its own}."""
     g = torch.Generator(device=device)
     g.manual_seed(1)
     teacher = torch.randn(width, vocab, generator=g, device=device)
@@ -127,22 +144,24 @@ def train(scheme="FR", n=4, c=2, steps=40, policy_steps=20, pairs=6, longest=12,
     head = Head(width, vocab, device)
     # The reference model's scores are fixed: the model before the first step.
     reference = [ops.token_logprobs(head.logits(head.w, part.x), part.targets)[0] for part in data]
-    out = {"preference": [], "policy": []}
+    out = {"preference": [], "policy": [], "words": []}
 
     def run(count, first, loss_of, rate, name):
-        coded = Coded(scheme, n, c, head.w.numel(), device)
+        coded = Coded(scheme, n, c, head.w.numel(), device, each_worker)
         try:
             for t in range(count):
                 mask = P.pgc_make_mask(mask_seed, first + t, P.PGC_POLICY_EXACT, n, c - 1)
                 values = []
 
-                def evaluate(k):
+                def evaluate(worker, k):
                     drop = (p, P.pgc_splitmix64(99, first + t), data[k].numbers)
                     value, grad = head.gradient(data[k], loss_of(k), drop)
                     values.append(value)
                     return grad
                 head.w -= rate * coded.step(evaluate, mask)
                 out[name].append(float(torch.stack(values).mean()))
+                if each_worker:
+                    out["words"].append([coded.word(j) for j in range(n)])
         finally:
             coded.close()
 
@@ -184,8 +203,9 @@ def main():
     ap.add_argument("--steps", type=int, default=40)
     ap.add_argument("--policy-steps", type=int, default=20)
     ap.add_argument("--vocab", type=int, default=1000)
+    ap.add_argument("--each-worker", action="store_true", help="every worker evaluates its own copy of a partition")
     args = ap.parse_args()
-    out = train(args.scheme, args.n, args.c, args.steps, args.policy_steps, vocab=args.vocab)
+    out = train(args.scheme, args.n, args.c, args.steps, args.policy_steps, vocab=args.vocab, each_worker=args.each_worker)
     print(json.dumps({"scheme": args.scheme, "n": args.n, "c": args.c, "preference_first": out["preference"][0],
                       "preference_last": out["preference"][-1], "pairs_ranked_right": out["accuracy"],
                       "policy_first": out["policy"][0], "policy_last": out["policy"][-1]}))
