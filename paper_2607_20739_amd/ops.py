@@ -162,8 +162,9 @@ def preference_loss(logits, targets, offsets, ref_logprobs=None, beta=0.1, label
     `out` receives it and may be the logits.  `workspace` (uint8, preference_workspace_bytes(logits,
     pairs)) is allocated where it is not given.
     """
-    return _marked(logits, _native.preference_loss(logits, targets, offsets, ref_logprobs, beta, label_smoothing, scale,
-                                                   pair_weights, gradient, out, workspace))
+    results = _native.preference_loss(logits, targets, offsets, ref_logprobs, beta, label_smoothing, scale, pair_weights,
+                                      gradient, out, workspace)
+    return _marked(logits, results) if logits.requires_grad else results
 
 
 def policy_loss(logits, targets, old_logprobs, advantages, ref_logprobs=None, clip_low=0.2, clip_high=0.2, kl=0.0,
@@ -173,13 +174,15 @@ def policy_loss(logits, targets, old_logprobs, advantages, ref_logprobs=None, cl
     dlogits is the gradient of scale * sum(token_weights * loss), None with gradient=False.  `out`
     receives it and may be the logits.
     """
-    return _marked(logits, _native.policy_loss(logits, targets, old_logprobs, advantages, ref_logprobs, clip_low, clip_high,
-                                               kl, scale, token_weights, gradient, out))
+    results = _native.policy_loss(logits, targets, old_logprobs, advantages, ref_logprobs, clip_low, clip_high, kl, scale,
+                                  token_weights, gradient, out)
+    return _marked(logits, results) if logits.requires_grad else results
 
 
 def _marked(logits, results):
-    """A loss's results (dlogits last): part of a sum that is differentiated, they say so instead of missing in it."""
-    if torch.is_grad_enabled() and logits.requires_grad:
+    """Results (dlogits last) for logits that ask for a gradient: in a sum that is differentiated, they raise instead of
+    missing in it."""
+    if torch.is_grad_enabled():
         return (*_LossWithoutGraph.apply(logits, results[:-1]), results[-1])
     return results
 
