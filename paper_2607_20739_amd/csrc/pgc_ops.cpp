@@ -361,7 +361,8 @@ int pgc_policy_loss(const pgc_logits* logits, const pgc_policy_args* a, void* hi
   pgc::LogitsArgs k = logits_args(logits, a->targets);
   k.old_logprobs = a->old_logprobs;
   k.advantages = a->advantages;
-  k.ref_logprobs = a->kl != 0.0 ? a->ref_logprobs : nullptr;
+  k.kl = static_cast<float>(a->kl);
+  k.ref_logprobs = k.kl != 0.f ? a->ref_logprobs : nullptr;   // of a factor that 32 bits round to 0, 0 * inf would stay
   k.weights = a->token_weights;
   k.loss = a->loss;
   k.logprobs = a->logprobs;
@@ -369,7 +370,6 @@ int pgc_policy_loss(const pgc_logits* logits, const pgc_policy_args* a, void* hi
   k.out_stride = a->dlogits_stride;
   k.clip_low = static_cast<float>(1.0 - a->clip_low);
   k.clip_high = static_cast<float>(1.0 + a->clip_high);
-  k.kl = static_cast<float>(a->kl);
   k.scale = static_cast<float>(a->scale);
   return launched(pgc::launch_logits(k, pgc::RowMode::kPolicy, logits->dtype, static_cast<hipStream_t>(hip_stream)),
                   "policy loss kernel");

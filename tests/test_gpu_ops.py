@@ -1167,3 +1167,19 @@ def test_more_short_rows_than_one_grid_dimension():
     # Of so many fair draws the kept ones number half, to five standard deviations.
     assert abs(int((out != 0).sum()) - rows / 2) < 5 * (rows / 4) ** 0.5
     assert (out[: 1 << 20] == ops.dropout(z[: 1 << 20] + 1, 0.5, 3)).all()
+
+
+def test_policy_loss_with_a_vanishing_kl_factor():
+    """Below what 32 bits hold it is no factor: the results are those without the KL term, also where that is infinite."""
+    _say("vanishing kl")
+    z, y = _case("f32", 9, 40, 3)
+    z, y = z.cuda(), y.clamp(0, 39).cuda()
+    z[3, y[3]] = -INF
+    old = torch.full((9,), -4.0, device="cuda")
+    far = old + 200.0                     # exp(ref - l) overflows
+    adv = torch.linspace(-1, 1, 9, device="cuda")
+    want = ops.policy_loss(z, y, old, adv)
+    assert want[0].isfinite().all() and want[2].isfinite().all()
+    for kl in (1e-60, -1e-60):
+        for a, b in zip(ops.policy_loss(z, y, old, adv, ref_logprobs=far, kl=kl), want):
+            assert torch.equal(a, b)
