@@ -145,6 +145,8 @@ def token_logprobs_backward(logits, targets, stats, grad, out=None):
 
 def preference_workspace_bytes(logits, pairs):
     """Bytes of the workspace that preference_loss needs for such logits and so many pairs."""
+    if not (torch.is_tensor(logits) and logits.dim() == 2 and logits.dtype in _DTYPES):
+        raise ValueError("logits must be a 2-D float32, bfloat16 or float16 tensor")
     rows, cols = logits.shape
     z, out = pgc_logits(None, rows, cols, cols, _DTYPES[logits.dtype]), _SIZE()
     status = lib().pgc_preference_workspace_bytes(ctypes.byref(z), pairs, ctypes.byref(out))

@@ -385,3 +385,9 @@ def test_what_is_no_tensor_is_refused(what):
                        (lambda: ops.preference_loss(what, y, y), "logits"), (lambda: ops.policy_loss(what, y, f, f), "logits")]:
         with pytest.raises(ValueError, match=name + " must be a tensor"):
             call()
+
+
+@pytest.mark.parametrize("logits", [None, torch.zeros(3, 4, dtype=torch.float64), torch.zeros(4), torch.zeros(2, 3, 4), np.zeros((3, 4))])
+def test_workspace_bytes_refuse_what_is_no_matrix_of_logits(logits):
+    with pytest.raises(ValueError, match="logits must be a 2-D"):
+        ops.preference_workspace_bytes(logits, 1)
