@@ -1337,16 +1337,22 @@ void small_preference_kernel(LogitsArgs a, PairArgs p) {
   }
 }
 
-// So many logits, and so many per pair, go through one launch, in which a pair has but one CU, whose
-// exponentials bound it: 4 pairs of 24 rows of 1,000 fp32 10.0 us a call, two launches 10.5 (in a graph 10.0
-// and 7.8); 2 of 424 rows of 58 fp16 9.9 and 10.8; 16 of 32 rows of 1,000 fp32 13.5 and 11.0.  Whatever
-// the pairs' lengths, a CU that takes all rows is done in 0.12 ms.
+// So many logits, and so many per pair, go through one launch, in which a pair has but one CU, whose exponentials
+// bound it.  The longest pair decides, and the host knows the average.  As calls, in 1 to 16 pairs of rows of 57 to
+// 2,000, two launches take 10 to 11 us, and one is faster up to 17,000 (short fp16 rows) to 48,000 (2,000 bf16) logits
+// per pair of equal lengths, up to 12,000 to 32,000 where lengths go from 1 to 3; the limit is the middle of these.
+// 4 pairs of 24 rows of 1,000 fp32 8.7 us and 10.9 in two (lengths from 1 to 3: 10.8 and 10.9), of 32 rows 10.8 and
+// 10.7, of 48 13.7 and 10.8; but 3 of 88 rows of 269 fp16, which take one, 11.8 and 10.9 (from 1 to 3: 15.3 and 10.8).
+// In a graph two win from 10,000 to 27,000 on (24 rows of 1,000 fp32 8.6 and 7.7).  More pairs than CUs take turns: 512
+// of 8 rows of 128 fp16 11.7, 1,000 of 4 rows of 100 fp32 17.8 (two launches 10.2), of 4 rows of 20 18.1 (20.7).
+// A pair that has all 524,288 logits takes 76 us (2,048 rows of 256 bf16) to 106 (4,096 of 128 fp32).
 constexpr int64_t kSmallLogits = int64_t{1} << 19, kSmallPairLogits = 24576;
 // Few rows (on average, of a pair) and bytes take two launches, the second of which sums the pairs again
 // for every row, or part of one: 566 rows of 3,902 bf16 in 55 pairs 11.9 us a call, three launches 14.2 (in a graph
 // 10.3 and 12.0); 1,000 in 10 pairs 12.6 and 14.7; 4,000 of 1,500 in 20 14.0 and 15.5; but 2,000 of 3,902 18.3 and
-// 17.4, 486 of 22,737 fp16 in 43 23.7 and 21.4, 4,096 of 20,000 152 and 80.  A single pair among thousands
-// that has all the rows costs 16 loads in turn.
+// 17.4, 486 of 22,737 fp16 in 43 23.7 and 21.4, 4,096 of 20,000 152 and 80.  A wave sums its rows' pairs in
+// turn, but of rows past the limit above it has few: 4,000 of 256 bf16 in 1,000 pairs 10.7 and 17.9 (lengths from 1 to 3:
+// 16.0 and 17.8), 4,000 of 200 in 4,000 23 and 45.  A single pair among thousands that has all the rows costs 16 loads in turn.
 constexpr int64_t kLongPairRows = 20480;
 constexpr int64_t kFewRows = kChunk, kFewPairRows = 512, kFewBytes = int64_t{1} << 23, kFewBytesOfWaves = int64_t{1} << 24;
 

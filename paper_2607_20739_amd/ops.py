@@ -27,6 +27,8 @@ PGC_F32, PGC_BF16, PGC_F16 = 0, 1, 2
 _P, _I32, _I64, _F64, _SIZE = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_double, ctypes.c_size_t
 
 
+# The C entry points' structures and signatures, for calls by address; calls on tensors go through the compiled module.
+
 class pgc_dropout_args(ctypes.Structure):
     _fields_ = [("x", _P), ("residual", _P), ("out", _P), ("row_ids", _P), ("rows", _I64), ("cols", _I64),
                 ("x_stride", _I64), ("residual_stride", _I64), ("out_stride", _I64), ("first_row", _I64),
