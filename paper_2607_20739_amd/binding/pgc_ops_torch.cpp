@@ -103,6 +103,9 @@ struct Matrix {
   }
 };
 
+// Whether a tensor that asks for a gradient is a parameter, or a view of one.
+bool of_a_leaf(const at::Tensor& t) { return t.is_leaf() || (t.is_view() && t._base().is_leaf()); }
+
 // The tensor that receives a result of a matrix's shape: `o`, or a new one for None.  One that asks
 // for a gradient would lose its own history unnoticed.  Only `over_logits` may: logits that a model
 // computed are replaced by their gradient, with which the model's backward pass starts.
@@ -117,7 +120,7 @@ struct Output {
     } else {
       t = tensor("out", o);
       stride = like.like("out", t);
-      TORCH_CHECK_VALUE(!t.requires_grad() || !at::GradMode::is_enabled() || (over_logits && !t.is_leaf() && t.data_ptr() == like.data()),
+      TORCH_CHECK_VALUE(!t.requires_grad() || !at::GradMode::is_enabled() || (over_logits && t.data_ptr() == like.data() && !of_a_leaf(t)),
                         "out must not ask for a gradient (detach() it)");
       if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();   // autograd notices a saved tensor that this changes
     }

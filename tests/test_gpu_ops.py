@@ -1183,3 +1183,24 @@ def test_policy_loss_with_a_vanishing_kl_factor():
     for kl in (1e-60, -1e-60):
         for a, b in zip(ops.policy_loss(z, y, old, adv, ref_logprobs=far, kl=kl), want):
             assert torch.equal(a, b)
+
+
+def test_views_of_parameters_are_not_replaced_by_a_gradient():
+    """A view of a parameter is no model's output, though it is no leaf itself; nor is its memory under another name."""
+    _say("views of parameters")
+    y = torch.zeros(6, dtype=torch.int32, device="cuda")
+    f = torch.linspace(-1, 1, 6, device="cuda")
+    o = torch.tensor([0, 3, 6], dtype=torch.int32, device="cuda")
+    leaf = torch.randn(6, 40, device="cuda", requires_grad=True)
+    was = leaf.detach().clone()
+    stats = ops.token_logprobs(was, y)[1]
+    for call in (lambda a, out: ops.token_logprobs_backward(a, y, stats, f, out=out),
+                 lambda a, out: ops.preference_loss(a, y, o, f, out=out), lambda a, out: ops.policy_loss(a, y, f, f, out=out)):
+        view = leaf[:, :]
+        for logits, out in [(view, view), (leaf.detach(), view), (leaf.detach(), leaf), (view, leaf)]:
+            with pytest.raises(ValueError, match="out must not ask for a gradient"):
+                call(logits, out)
+        assert torch.equal(leaf.detach(), was)
+        model = leaf * 2
+        part = model[:, :]                   # of a model's output, which may go
+        call(part, part)
