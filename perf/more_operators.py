@@ -1,0 +1,443 @@
+"""The calls that the operators of a training step's scores and update are measured on.
+
+A case is one pass through one operator: the scores of tokens under rows of logits (the given
+token's log-probability, the row's entropy, its most probable tokens) and their gradient; the norm of
+many gradients with the factor that clips it; an AdamW step over many tensors, whose states have
+32 bits or 8.
+
+`run` computes them in elementary torch operations in 32 bits, or, with `own` set, through the
+framework's entry points.
+"""
+
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+BYTES = {"f32": 4, "bf16": 2, "f16": 2}
+LOSS_SCALE = {"f32": 1.0, "bf16": 1.0, "f16": 4096.0}   # half precision has few small numbers
+BETA1, BETA2, EPS = 0.9, 0.999, 1e-8
+BLOCK = 256                              # values that share an 8-bit state's scale
+CHUNK = 1 << 27                          # values that the 64-bit evaluation widens at a time
+
+
+def listed():
+    return [
+        # A served answer's next token, with the alternatives that a client may ask for.
+        scores("scores_token", "bf16", rows=1, cols=131072, top=20, given=False),
+        # One decoding step of a batch of sequences, a vocabulary of odd size.
+        scores("scores_decode_odd", "f16", rows=48, cols=50021, top=5, banned=True),
+        # The repository's own classifier: every sample's class, with the runners-up.
+        scores("scores_classes", "f32", rows=1048576, cols=10, top=3),
+        # Scoring a large batch of sampled answers, a tenth of the tokens belonging to prompts.
+        scores("scores_large", "bf16", rows=8192, cols=131072, top=8, masked=0.1),
+        # A policy step with an entropy bonus: odd vocabulary in padded rows.
+        scores("scores_backward_odd", "f16", rows=2047, cols=50021, pad=27, masked=0.25, banned=True, backward=True),
+        # The entropy's gradient alone, over a large batch.
+        scores("scores_backward_large", "bf16", rows=16384, cols=32768, given=False, backward=True),
+        # The norm of the repository's own two-layer network's gradient.
+        grad_norm("norm_mlp", "f32", tensors=4, values=813 * 1024, width=1024),
+        # The norm of all the gradients of a large model.
+        grad_norm("norm_large", "bf16", tensors=290, values=1 << 29, width=4096),
+        # The update of that two-layer network.
+        adamw("adamw_mlp", 32, "f32", "f32", tensors=4, values=813 * 1024, width=1024, packed=True),
+        # A mixed-precision step: 32-bit weights with 16-bit copies, which the model computes with.
+        adamw("adamw_copies", 32, "f32", "bf16", tensors=148, values=124 << 20, width=1000, copies="bf16"),
+        # Adapters: many small 16-bit tensors of odd sizes, states in 8 bits.
+        adamw("adamw_8bit_adapters", 8, "f16", "f16", tensors=224, values=9 << 20, width=1001, packed=True),
+        # The states of a large model in 8 bits.
+        adamw("adamw_8bit_large", 8, "f32", "bf16", tensors=290, values=400 << 20, width=4096),
+    ]
+
+
+def scores(name, dtype, rows, cols, top=0, pad=0, masked=0.0, banned=False, given=True, backward=False):
+    return dict(name=name, op="scores", dtype=dtype, rows=rows, cols=cols, top=top, pad=pad, masked=masked, banned=banned,
+                given=given, backward=backward)
+
+
+def grad_norm(name, dtype, tensors, values, width):
+    return dict(name=name, op="norm", dtype=dtype, tensors=tensors, values=values, width=width)
+
+
+def adamw(name, bits, dtype, grad, tensors, values, width, copies="", packed=False):
+    """packed: the tensors lie one after the other in one vector, as coded gradients have them; otherwise each
+    starts at a multiple of 512 values, as an allocator places them."""
+    return dict(name=name, op="adamw", bits=bits, dtype=dtype, grad=grad, tensors=tensors, values=values, width=width,
+                copies=copies, packed=packed)
+
+
+def draw(rng):
+    """A case of the listed ones' ranges: values, columns, rows and tensors over their logarithms."""
+    def log_int(lo, hi):
+        return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+    op = rng.choice(["scores", "scores", "norm", "adamw", "adamw"])
+    dtype = rng.choice(["f32", "bf16", "f16"])
+    if op == "scores":
+        cols = log_int(10, 131072)
+        rows = max(1, min(log_int(1 << 10, 1 << 29) // cols, 1 << 20))
+        backward = rng.random() < 0.4
+        given = rng.random() < 0.6
+        case = scores("", dtype, rows, cols, top=0 if backward else rng.randint(0, 32), pad=rng.choice([0, 0, rng.randint(1, 64)]),
+                      masked=rng.choice([0.0, 0.1, 0.33]) if given else 0.0, banned=cols >= 1000 and rng.random() < 0.5,
+                      given=given, backward=backward)
+    else:
+        values = log_int(1 << 10, 1 << 28)
+        width = log_int(16, 8192)
+        tensors = min(log_int(1, 400), max(1, values // width))
+        if op == "norm":
+            case = grad_norm("", dtype, tensors, values, width)
+        else:
+            copies = rng.choice(["", "bf16", "f16"]) if dtype == "f32" else ""
+            grad = rng.choice(["f32", "bf16", "f16"]) if dtype == "f32" else dtype
+            case = adamw("", rng.choice([8, 32]), dtype, grad, tensors, values, width, copies, packed=rng.random() < 0.5)
+    del case["name"]
+    return case
+
+
+def sizes(case):
+    """The tensors' sizes: matrices of 1 to 3 shares of the values and vectors of `width` in turn."""
+    n, width = case["tensors"], case["width"]
+    vectors = n // 2
+    left = max(case["values"] - vectors * width, n)
+    weights = [1 + i % 3 for i in range(n - vectors)]
+    share = left / sum(weights)
+    matrices = [max(1, int(w * share)) for w in weights]
+    return [width if i % 2 else matrices[i // 2] for i in range(n)]
+
+
+def logits_of(case, gen, device):
+    """Rows of logits as a trained model gives them: a spread of a few units with the token that
+    follows ahead, reserved tokens at -inf, and rows that may be padded."""
+    rows, cols, dtype = case["rows"], case["cols"], DTYPES[case["dtype"]]
+    z = torch.randn(rows, cols + case["pad"], generator=gen, device=device, dtype=dtype)[:, :cols]
+    z.mul_(2.0)
+    y = torch.randint(0, cols, (rows,), generator=gen, device=device)
+    at = torch.arange(rows, device=device)
+    ahead = (z[at, y].float() + math.log(cols)).to(dtype)
+    if case["banned"]:
+        reserved = torch.rand(cols, generator=gen, device=device) < 0.01
+        z.masked_fill_(reserved, -math.inf)
+    z[at, y] = ahead
+    return z, y.to(torch.int32)
+
+
+def prepare(case, seed):
+    device = torch.device("cuda")
+    gen = torch.Generator(device=device)
+    gen.manual_seed(seed)
+    s = dict(case)
+    if case["op"] == "scores":
+        rows = case["rows"]
+        z, y = logits_of(case, gen, device)
+        y[torch.randperm(rows, generator=gen, device=device)[:int(case["masked"] * rows)]] = -1
+        s["logits"], s["targets"] = z, y if case["given"] else None
+        if case["backward"]:
+            x = z.float()
+            d = x - x.amax(1)[:, None]
+            total = torch.exp(d).sum(1)
+            log_sum = torch.log(total)
+            s["stats"] = torch.stack([x.amax(1), log_sum], 1)
+            s["entropy"] = log_sum - (torch.exp(d) * d.clamp(min=-1e4)).sum(1) / total
+            scale = LOSS_SCALE[case["dtype"]] / rows
+            noise = torch.rand(2, rows, generator=gen, device=device) * 2 - 1
+            s["grad_logprobs"] = noise[0] * scale if case["given"] else None
+            s["grad_entropy"] = (noise[1] - 2) * (0.01 * scale)
+        return s
+    counts = sizes(case)
+    if case["op"] == "norm":
+        s["grads"] = gradients(counts, DTYPES[case["dtype"]], gen, device)
+        s["max_norm"], s["scale"] = 1.0, 1.0 / LOSS_SCALE[case["dtype"]]
+        return s
+    # A model some hundred steps into its training, with gradients as the last steps had them.
+    starts = [0]
+    for n in counts:
+        starts.append(starts[-1] + (n if case["packed"] else -(-n // 512) * 512))
+
+    def laid_out(dtype, values=None):
+        """One vector for all tensors, and its parts."""
+        whole = torch.zeros(starts[-1], dtype=dtype, device=device)
+        parts = [whole[a:a + n] for a, n in zip(starts, counts)]
+        for part, x in zip(parts, values or ()):
+            part.copy_(x)
+        return whole, parts
+
+    s["all_params"], s["params"] = laid_out(DTYPES[case["dtype"]], [torch.randn(n, generator=gen, device=device).mul_(0.02) for n in counts])
+    s["grads"] = laid_out(DTYPES[case["grad"]], gradients(counts, DTYPES[case["grad"]], gen, device))[1]
+    s["all_copies"], s["copies"] = laid_out(DTYPES[case["copies"]]) if case["copies"] else (None, None)
+    m = [g.float().mul(0.1).add_(torch.randn(g.shape, generator=gen, device=device), alpha=1e-4) for g in s["grads"]]
+    v = [torch.rand(g.shape, generator=gen, device=device).add_(0.5).mul_(g.float().square_().add_(1e-8)) for g in s["grads"]]
+    if case["bits"] == 8:
+        coded = [(encode(a, 127), encode(b, 255)) for a, b in zip(m, v)]
+        s["m"], s["v"] = laid_out(torch.uint8, [a[0] for a, b in coded])[1], laid_out(torch.uint8, [b[0] for a, b in coded])[1]
+        s["scales"] = [torch.stack([a[1], b[1]], 1) for a, b in coded]
+        s["all_m"], s["m_values"] = laid_out(torch.bfloat16)     # which holds 8-bit states exactly
+        s["all_v"], s["v_values"] = laid_out(torch.bfloat16)
+    else:
+        s["all_m"], s["m"] = laid_out(torch.float32, m)
+        s["all_v"], s["v"] = laid_out(torch.float32, v)
+        s["scales"] = None
+    s["starts"] = starts
+    s["step"], s["lr"], s["decay"] = 200, 3e-4, [0.1 if i % 2 == 0 else 0.0 for i in range(len(counts))]
+    s["factor"] = torch.rand(1, generator=gen, device=device).mul_(0.5).add_(0.5)
+    return s
+
+
+def gradients(counts, dtype, gen, device):
+    """Tensors of unequal spread, as layers have them."""
+    return [torch.randn(n, generator=gen, device=device).mul_(1e-3 * (1 + i % 5)).to(dtype) for i, n in enumerate(counts)]
+
+
+def run(state):
+    return (run_own if own else run_plain)(state)
+
+
+def run_own(s):
+    from paper_2607_20739_amd import ops
+    if s["op"] == "scores":
+        if s["backward"]:
+            return ops.token_scores_backward(s["logits"], s["targets"], s["stats"], s["entropy"], s["grad_logprobs"],
+                                             s["grad_entropy"])
+        return ops.token_scores(s["logits"], s["targets"], s["top"])
+    if s["op"] == "norm":
+        return ops.grad_norm(s["grads"], max_norm=s["max_norm"], scale=s["scale"])
+    ops.adamw(s["params"], s["grads"], s["m"], s["v"], s["step"], s["lr"], betas=(BETA1, BETA2), eps=EPS,
+              weight_decay=s["decay"], scales=s["scales"], copies=s["copies"], factor=s["factor"])
+    if s["bits"] == 8:
+        ops.adamw_state_values(s["m"], s["v"], s["scales"], out=(s["m_values"], s["v_values"]))
+    return s["all_params"], s["all_copies"], s["all_m"], s["all_v"]
+
+
+# ---- the plain forms ------------------------------------------------------------------------
+
+def run_plain(s):
+    if s["op"] == "scores":
+        return plain_gradient(s) if s["backward"] else plain_scores(s)
+    if s["op"] == "norm":
+        # Squares of long lists are added up in 64 bits.
+        total = torch.stack([g.float().square().sum(dtype=torch.float64) for g in s["grads"]]).sum()
+        norm = total.sqrt() * s["scale"]
+        return norm.float().reshape(1), (s["scale"] * (s["max_norm"] / norm).clamp(max=1.0)).float().reshape(1)
+    _ = [plain_adamw(s, i) for i in range(len(s["params"]))]
+    return s["all_params"], s["all_copies"], s["all_m"], s["all_v"]
+
+
+def plain_scores(s):
+    z, k = s["logits"].float(), min(s["top"], s["cols"])
+    top = z.amax(1)
+    d = z - top[:, None]
+    e = torch.exp(d)
+    total = e.sum(1)
+    log_sum = torch.log(total)
+    entropy = log_sum - (e * torch.where(e == 0, 0.0, d)).sum(1) / total
+    # Values and columns as one number, which orders equal values by their columns.
+    bits = (z + 0.0).view(torch.int32)
+    order = torch.where(bits < 0, bits ^ 0x7FFFFFFF, bits).long() << 32
+    order = order + (0xFFFFFFFF - torch.arange(s["cols"], device=z.device))
+    tokens = 0xFFFFFFFF - (order.topk(k, 1).values & 0xFFFFFFFF)
+    values = z.gather(1, tokens)
+    top_logprobs = values - top[:, None] - log_sum[:, None]
+    tokens = torch.where(values == -math.inf, -1, tokens).to(torch.int32)
+    more = (0, s["top"] - k)
+    top_logprobs = torch.nn.functional.pad(top_logprobs, more, value=-math.inf)
+    tokens = torch.nn.functional.pad(tokens, more, value=-1)
+    stats = torch.stack([top, log_sum], 1)
+    if s["targets"] is None:
+        return None, entropy, top_logprobs, tokens, stats
+    on = s["targets"] >= 0
+    lp = z.gather(1, s["targets"].clamp(min=0).long()[:, None])[:, 0] - top - log_sum
+    return (torch.where(on, lp, 0.0), torch.where(on, entropy, 0.0), torch.where(on[:, None], top_logprobs, 0.0),
+            torch.where(on[:, None], tokens, -1), torch.where(on[:, None], stats, 0.0))
+
+
+def plain_gradient(s):
+    z, top, log_sum = s["logits"].float(), s["stats"][:, :1], s["stats"][:, 1:]
+    lp = z - top - log_sum
+    p = torch.exp(lp)
+    dz = -s["grad_entropy"][:, None] * p * (torch.where(p == 0, 0.0, lp) + s["entropy"][:, None])
+    if s["targets"] is not None:
+        on, g = s["targets"] >= 0, s["grad_logprobs"]
+        dz = dz - g[:, None] * p
+        dz.scatter_add_(1, s["targets"].clamp(min=0).long()[:, None], g[:, None])
+        dz = torch.where(on[:, None], dz, 0.0)
+    return dz.to(s["logits"].dtype)
+
+
+def plain_adamw(s, i):
+    p, t, decay = s["params"][i], s["step"], s["decay"][i]
+    g = s["grads"][i].float() * s["factor"]
+    if s["bits"] == 8:
+        m, v = decode(s["m"][i], s["scales"][i][:, 0], 127), decode(s["v"][i], s["scales"][i][:, 1], 255)
+    else:
+        m, v = s["m"][i], s["v"][i]
+    m = m * BETA1 + g * (1 - BETA1)
+    v = v * BETA2 + g * g * (1 - BETA2)
+    x = p.float()
+    denominator = torch.sqrt(v) * (1 / math.sqrt(1 - BETA2 ** t)) + EPS
+    x = x - (x * (s["lr"] * decay) + m / denominator * (s["lr"] / (1 - BETA1 ** t)))
+    p.copy_(x)
+    if s["copies"] is not None:
+        s["copies"][i].copy_(x)
+    if s["bits"] == 32:
+        s["m"][i].copy_(m)
+        s["v"][i].copy_(v)
+        return
+    code, scale = encode(m, 127)
+    s["m"][i].copy_(code)
+    s["scales"][i][:, 0] = scale
+    s["m_values"][i].copy_(decode(code, scale, 127))
+    code, scale = encode(v, 255)
+    s["v"][i].copy_(code)
+    s["scales"][i][:, 1] = scale
+    s["v_values"][i].copy_(decode(code, scale, 255))
+
+
+def encode(x, levels):
+    """Codes of 8 bits and the blocks' scales.  Values are rounded to 4 significant bits, the largest
+    of a block's is its scale, and a code counts how many such numbers lie between: 255 levels, or 127
+    beside a sign.  Below the last level a signed value becomes 0 where that is nearer, one without a
+    sign stays at it."""
+    n = x.numel()
+    bits = torch.nn.functional.pad(x, (0, -n % BLOCK)).view(torch.int32).view(-1, BLOCK)
+    size = bits & 0x7FFFFFFF
+    place = ((size + 0x7FFFF + (size >> 20 & 1)) >> 20).clamp(max=0x7F7)
+    scale = place.amax(1, keepdim=True).clamp(min=levels)
+    code = place - scale + levels
+    if levels == 127:
+        code = torch.where(code > -8, code.clamp(min=1), 0) * (size > 0)
+        code = torch.where((bits < 0) & (code > 0), code + 128, code)
+    else:
+        code = code.clamp(min=1) * (size > 0)
+    return code.to(torch.uint8).view(-1)[:n].contiguous(), (scale << 20).view(torch.float32)[:, 0]
+
+
+def decode(code, scale, levels):
+    n = code.numel()
+    code = torch.nn.functional.pad(code, (0, -n % BLOCK)).view(-1, BLOCK).int()
+    size = code & levels
+    place = ((scale.contiguous().view(torch.int32) >> 20)[:, None] - levels + size).clamp(min=0)
+    value = torch.where(size > 0, place << 20, 0).view(torch.float32)
+    value = torch.where(code > levels, -value, value)
+    return value.view(-1)[:n]
+
+
+# ---- the definitions in 64 bits -------------------------------------------------------------
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] == "scores":
+        return exact_gradient(s) if case["backward"] else exact_scores(s)
+    if case["op"] == "norm":
+        norm = s["scale"] * math.sqrt(math.fsum(float((g.double() ** 2).sum()) for g in s["grads"]))
+        factor = s["scale"] * min(1.0, s["max_norm"] / norm)
+        return torch.tensor([norm], dtype=torch.float64), torch.tensor([factor], dtype=torch.float64)
+    x_new, m_new, v_new = (torch.zeros_like(s["all_params"], dtype=torch.float64) for _ in range(3))
+    for i, (a, p) in enumerate(zip(s["starts"], s["params"])):
+        at = slice(a, a + p.numel())
+        g = s["grads"][i].double() * float(s["factor"])
+        m, v = s["m"][i], s["v"][i]
+        if case["bits"] == 8:
+            m, v = level_values(m, s["scales"][i][:, 0], True), level_values(v, s["scales"][i][:, 1], False)
+        m = BETA1 * m.double() + (1 - BETA1) * g
+        v = BETA2 * v.double() + (1 - BETA2) * g * g
+        m_hat, v_hat = m / (1 - BETA1 ** s["step"]), v / (1 - BETA2 ** s["step"])
+        x_new[at] = p.double() * (1 - s["lr"] * s["decay"][i]) - s["lr"] * m_hat / (v_hat.sqrt() + EPS)
+        m_new[at] = nearest_levels(m, True) if case["bits"] == 8 else m
+        v_new[at] = nearest_levels(v, False) if case["bits"] == 8 else v
+    return x_new, x_new if case["copies"] else None, m_new, v_new
+
+
+def blocks_of(x):
+    return torch.cat([x, x.new_zeros(-x.numel() % BLOCK)]).reshape(-1, BLOCK)
+
+
+def level(top, below):
+    """The number of 4 significant bits that lies so many places below `top`, which is one."""
+    mantissa, exponent = torch.frexp(top.double())
+    eighths = torch.round(mantissa * 16).long() - 8 + 8 * exponent.long() - below
+    return torch.ldexp((eighths % 8 + 8).double() / 16, torch.div(eighths, 8, rounding_mode="floor"))
+
+
+def level_values(code, scale, signed):
+    c = blocks_of(code).long()
+    size = c % 128 if signed else c
+    x = level(scale[:, None], (127 if signed else 255) - size) * (size > 0)
+    return (x * (1 - 2 * (c // 128)) if signed else x).reshape(-1)[:code.numel()]
+
+
+def nearest_levels(x, signed):
+    b = blocks_of(x)
+    mantissa, exponent = torch.frexp(b.abs())
+    r = torch.ldexp(torch.round(mantissa * 16) / 16, exponent)
+    top = r.amax(1, keepdim=True)
+    least = level(torch.where(top > 0, top, 1.0), 126 if signed else 254) * (top > 0)
+    small = torch.where(r >= least / 2, least, 0.0) if signed else torch.where(b > 0, least, 0.0)
+    return (torch.where(r >= least, r, small) * torch.sign(b)).reshape(-1)[:x.numel()]
+
+
+def blocks(s):
+    step = max(1, CHUNK // s["cols"])
+    return [(a, min(s["rows"], a + step)) for a in range(0, s["rows"], step)]
+
+
+def exact_scores(s):
+    rows, cols, device, k = s["rows"], s["cols"], s["logits"].device, s["top"]
+    f64 = dict(dtype=torch.float64, device=device)
+    stats, entropy, lp = torch.zeros(rows, 2, **f64), torch.zeros(rows, **f64), torch.zeros(rows, **f64)
+    top_lp = torch.full((rows, k), -math.inf, **f64)
+    tokens = torch.full((rows, k), -1, dtype=torch.int32, device=device)
+    for a, b in blocks(s):
+        x = s["logits"][a:b].double()
+        stats[a:b, 0] = x.max(1).values
+        x -= stats[a:b, :1]
+        stats[a:b, 1] = torch.log(torch.exp(x).sum(1))
+        x -= stats[a:b, 1:]
+        entropy[a:b] = -torch.nan_to_num(torch.exp(x) * x, nan=0.0).sum(1)
+        if s["targets"] is not None:
+            lp[a:b] = x[torch.arange(b - a, device=device), s["targets"][a:b].long().clamp(min=0)]
+        values, order = torch.sort(s["logits"][a:b].float(), dim=1, descending=True, stable=True)
+        n = min(k, cols)
+        tokens[a:b, :n] = torch.where(values[:, :n] > -math.inf, order[:, :n], -1).int()
+        top_lp[a:b, :n] = x.gather(1, order[:, :n])
+    if s["targets"] is None:
+        return None, entropy, top_lp, tokens, stats
+    off = s["targets"] < 0
+    lp[off], entropy[off], top_lp[off], stats[off] = 0.0, 0.0, 0.0, 0.0
+    tokens[off] = -1
+    return lp, entropy, top_lp, tokens, stats
+
+
+def exact_gradient(s):
+    out = torch.empty(s["rows"], s["cols"], dtype=torch.float64, device=s["logits"].device)
+    e, h = s["grad_entropy"].double(), s["entropy"].double()
+    for a, b in blocks(s):
+        ln_p = s["logits"][a:b].double() - s["stats"][a:b].double().sum(1, keepdim=True)
+        p = torch.exp(ln_p)
+        out[a:b] = -e[a:b, None] * torch.nan_to_num(p * (ln_p + h[a:b, None]), nan=0.0)
+        if s["targets"] is not None:
+            on = s["targets"][a:b] >= 0
+            g = s["grad_logprobs"][a:b].double()
+            out[a:b] -= g[:, None] * p
+            at = torch.arange(a, b, device=out.device)
+            out[at, s["targets"][a:b].long().clamp(min=0)] += g
+            out[a:b][~on] = 0.0
+    return out
+
+
+def work(case):
+    """Bytes that have to move, and operations: rows without a token are written, not read."""
+    if case["op"] == "scores":
+        b, rows, cols = BYTES[case["dtype"]], case["rows"], case["cols"]
+        read = b * cols * (rows - int(case["masked"] * rows))
+        if case["backward"]:
+            return {"bytes": read + b * rows * cols + 24 * rows, "flops": 6 * rows * cols}
+        return {"bytes": read + rows * (20 + 8 * case["top"]), "flops": 7 * rows * cols}
+    values = sum(sizes(case))
+    if case["op"] == "norm":
+        return {"bytes": BYTES[case["dtype"]] * values, "flops": 2 * values}
+    each = 2 * BYTES[case["dtype"]] + BYTES[case["grad"]] + (2 if case["copies"] else 0)
+    # 8-bit states: both read, written and, as the values that they stand for, written once more.
+    each += 16 if case["bits"] == 32 else 4 + 4
+    return {"bytes": each * values, "flops": 16 * values}
