@@ -2,7 +2,9 @@
  * pgc_ops.h -- C ABI of the operators that turn a language model's outputs into a
  * partition's loss and gradient, for coded gradient descent (pgc.h) on gfx950:
  * dropout, token log-probabilities, the preference loss of pairs of sequences and
- * the clipped policy loss, each forward and backward.
+ * the clipped policy loss, the scores of tokens (with the rows' entropies and most
+ * probable tokens), each forward and backward; and of those that turn a gradient into
+ * the next parameters: the norm of many gradients and an AdamW step over many tensors.
  *
  * Gradient coding combines copies of a partition's gradient that different workers
  * compute, so a partition's gradient must not depend on who computes it, nor with
@@ -177,6 +179,142 @@ typedef struct pgc_policy_args {
 } pgc_policy_args;
 
 int pgc_policy_loss(const pgc_logits* logits, const pgc_policy_args* args, void* hip_stream);
+
+/* ---- Scores of tokens ---------------------------------------------------------------
+ *
+ * With M_t, S_t and l_t of row t as for the token log-probabilities:
+ *   logprobs[t] = l_t,  stats[t] = (M_t, ln S_t)
+ *   entropy[t] = ln S_t - (1 / S_t) sum_j exp(z[t][j] - M_t) (z[t][j] - M_t)
+ *   top_tokens[t][i], top_logprobs[t][i]: the column of the row's i-th largest logit and
+ *     its log-probability, i = 0 .. top - 1; of equal logits the lower column comes first.
+ *
+ * Without targets every row is read and there are no logprobs.  With targets, a row whose
+ * target lies outside of [0, cols) is not read: its results are 0, its top_tokens -1.
+ * -inf marks a token that cannot occur: it adds nothing to the entropy and is none of the
+ * top ones; where fewer than `top` are left, the others are -1 with log-probability
+ * -inf.  A row of nothing but -inf has logprobs -inf, entropy 0 and stats (-inf, 0).  NaN or
+ * +inf in a row that is read makes the row's results NaN (its top_tokens -1), and no other's.
+ */
+enum { PGC_MAX_TOP = 64 };
+
+typedef struct pgc_scores_args {
+  const int32_t* targets;       /* rows, or NULL */
+  int64_t top;                  /* in [0, PGC_MAX_TOP] */
+  float* logprobs;              /* rows; NULL without targets */
+  float* entropy;               /* rows, or NULL */
+  float* stats;                 /* rows pairs, 8-byte aligned, or NULL */
+  float* top_logprobs;          /* rows x top */
+  int32_t* top_tokens;          /* rows x top */
+} pgc_scores_args;
+
+/* Bytes of device workspace that the call on such logits (their data is not looked at)
+ * needs: a multiple of 256, 0 for most.  Host only. */
+int pgc_token_scores_workspace_bytes(const pgc_logits* logits, int64_t top, size_t* bytes);
+
+/* workspace: at least that many bytes, 256-byte aligned, used until the stream has
+ * passed the call; may be NULL where none are needed. */
+int pgc_token_scores(const pgc_logits* logits, const pgc_scores_args* args, void* workspace,
+                     size_t workspace_bytes, void* hip_stream);
+
+/* dlogits[t][j] = g_t ([j = y_t] - p_j) - e_t p_j (ln p_j + H_t), p_j = exp(z[t][j] - M_t - ln S_t),
+ * in the type of the logits: g is the gradient of logprobs, e that of entropy, H the
+ * entropy.  A row without a token, or whose g and e are 0, gets zeros and is not read,
+ * whatever its logits hold; so does a row of nothing but -inf. */
+typedef struct pgc_scores_grad_args {
+  const int32_t* targets;       /* as given to pgc_token_scores */
+  const float* stats;           /* as pgc_token_scores wrote them */
+  const float* entropy;         /* rows, likewise; may be NULL without grad_entropy */
+  const float* grad_logprobs;   /* rows, or NULL for 0 (without targets: NULL) */
+  const float* grad_entropy;    /* rows, or NULL for 0 */
+  void* dlogits;                /* rows x cols in the logits' type */
+  int64_t dlogits_stride;
+} pgc_scores_grad_args;
+
+int pgc_token_scores_backward(const pgc_logits* logits, const pgc_scores_grad_args* args, void* hip_stream);
+
+/* ---- Norm of many gradients ---------------------------------------------------------
+ *
+ * norm = |scale| sqrt(sum of all squares),  factor = scale min(1, max_norm / norm)
+ *
+ * factor is what pgc_adamw multiplies the gradients by: `scale` takes the loss's scale
+ * back, the rest clips.  A norm of 0 has factor scale.  Where a value is NaN or infinite
+ * the norm is NaN or infinite and factor NaN, with which pgc_adamw changes nothing.  Sums
+ * run in 64 bits in an order that the tensors' sizes alone decide.
+ */
+typedef struct pgc_values {
+  const void* data;             /* `count` values one after the other */
+  int64_t count;
+  int32_t dtype;                /* enum pgc_dtype */
+} pgc_values;
+
+int pgc_grad_norm_workspace_bytes(const pgc_values* tensors, int64_t n, size_t* bytes);
+
+/* tensors: a host array of n.  max_norm: > 0, may be infinite.  norm, factor: one float each, or NULL. */
+int pgc_grad_norm(const pgc_values* tensors, int64_t n, double max_norm, double scale, float* norm,
+                  float* factor, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ---- AdamW step over many tensors ---------------------------------------------------
+ *
+ * For every value x of a tensor, its gradient g (times `factor`), its states m and v:
+ *   m' = beta1 m + (1 - beta1) g,  v' = beta2 v + (1 - beta2) g^2
+ *   x' = x - lr (weight_decay x + m' / (1 - beta1^step) / (sqrt(v' / (1 - beta2^step)) + eps))
+ * computed in 32 bits, x' rounded once to the parameter's type and, where there is a
+ * `copy`, once to the copy's.  m' and v' are kept in 32 bits or in 8; x' follows from them
+ * before they are rounded to 8.
+ *
+ * States in 8 bits: a tensor's values in blocks of 256 (the last may be shorter), one byte
+ * for each value of m and of v and two floats for each block: scales[2 b] for m, scales[2 b + 1]
+ * for v.  Values are rounded to 4 significant bits, to nearest even; i(x) numbers the
+ * non-negative floats of 4 significant bits upwards (the bits of x shifted right by 20).
+ *   v: the scale is the block's largest value A, the byte c of a value x is i(x) - i(A) + 255, of
+ *      a smaller one than c = 1 has, 1, and of 0, 0.
+ *   m: the low 7 bits c of the byte are i(|x|) - i(A) + 127, of a smaller one than c = 1 has, 1
+ *      where |x| rounds to at least half of that, else 0; the highest bit is the sign.
+ * (Where i(A) is less than 255, of m 127, the float with that number stands for A.)  So m
+ * keeps 127 numbers of either sign over 15.9 octaves, v 255 over 31.9, each within 1/16 of its
+ * value.  A block with a NaN, an infinity or a value of 2^128 (1 - 2^-5) and more has a scale
+ * that is not finite, and all its values are NaN.  Zeros stand for states of 0.
+ */
+typedef struct pgc_adamw_tensor {
+  void* param;                  /* `count` values, as are the others */
+  const void* grad;
+  void* copy;                   /* receives the new parameters, or NULL */
+  void* m;                      /* floats, or bytes */
+  void* v;
+  float* scales;                /* of 8-bit states, 8-byte aligned: 2 for each block; else NULL */
+  int64_t count;
+  double weight_decay;          /* finite, >= 0 */
+  int32_t param_dtype, grad_dtype, copy_dtype;   /* enum pgc_dtype */
+} pgc_adamw_tensor;
+
+typedef struct pgc_adamw_args {
+  double lr;                    /* finite, >= 0 */
+  double beta1, beta2;          /* in [0, 1) */
+  double eps;                   /* finite, > 0, also in 32 bits */
+  int64_t step;                 /* this step's number, from 1 on */
+  const float* lr_at;           /* one float on the device instead of lr, or NULL */
+  const int64_t* step_at;       /* one number on the device instead of step, or NULL */
+  const float* factor;          /* one float on the device, or NULL for 1; not finite: the call
+                                   changes nothing (copies included) */
+  int32_t state_bits;           /* 32 or 8 */
+} pgc_adamw_args;
+
+/* tensors: a host array of n, read before the call returns.  No two of all these arrays
+ * may overlap, but gradients each other. */
+int pgc_adamw(const pgc_adamw_tensor* tensors, int64_t n, const pgc_adamw_args* args, void* hip_stream);
+
+/* States in 8 bits as the numbers that they stand for, which float and bf16 hold exactly. */
+typedef struct pgc_adamw_state {
+  const void* m;
+  const void* v;
+  const float* scales;
+  void* m_values;               /* `count` each */
+  void* v_values;
+  int64_t count;
+  int32_t dtype;                /* of the values: PGC_F32 or PGC_BF16 */
+} pgc_adamw_state;
+
+int pgc_adamw_state_values(const pgc_adamw_state* tensors, int64_t n, void* hip_stream);
 
 #ifdef __cplusplus
 }

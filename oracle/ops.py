@@ -1,5 +1,6 @@
-"""Oracle of the language-model operators: dropout, token log-probabilities, the preference loss
-and the clipped policy loss with a KL term, with their gradients.
+"""Oracle of the language-model operators: dropout, token log-probabilities, the preference loss, the
+clipped policy loss with a KL term and the scores of tokens, with their gradients; the gradients' norm
+and the AdamW step with its states in 8 bits.
 
 TEST INFRASTRUCTURE ONLY (see the package docstring).  Plain numpy in 64 bits, from the formulas;
 shares nothing with the HIP library.  Inputs are arrays of any real type (taken to float64).
@@ -136,3 +137,133 @@ def policy(z, targets, old, advantages, ref=None, clip_low=0.2, clip_high=0.2, k
             slope -= kl * np.expm1(d)
         grad[t] = scale * slope * (1.0 if weights is None else float(weights[t]))
     return loss, np.where(on, lp, 0.0), grad
+
+
+# ---- scores of tokens -----------------------------------------------------------------------
+
+def read_rows(z, targets):
+    """Rows that are read: all without targets, else those with a token."""
+    return np.ones(len(z), dtype=bool) if targets is None else has_token(targets, np.shape(z)[1])
+
+
+def entropy(z, targets=None):
+    """-sum p ln p of each row; 0 of rows that are not read or hold nothing but -inf."""
+    z = np.asarray(z, dtype=np.float64)
+    top, log_sum = row_stats(z)
+    out = np.zeros(len(z))
+    for t in np.flatnonzero(read_rows(z, targets)):
+        if np.isnan(top[t]):
+            out[t] = np.nan
+        elif not np.isneginf(top[t]):
+            d = z[t][~np.isneginf(z[t])] - top[t]
+            out[t] = log_sum[t] - (np.exp(d) * d).sum() / np.exp(log_sum[t])
+    return out
+
+
+def top_tokens(z, top, targets=None):
+    """(log-probabilities, columns) [rows, top] of the largest logits, of equal ones the lower column."""
+    z = np.asarray(z, dtype=np.float64)
+    peak, log_sum = row_stats(z)
+    lp, tokens = np.zeros((len(z), top)), np.full((len(z), top), -1, dtype=np.int64)
+    for t in np.flatnonzero(read_rows(z, targets)):
+        lp[t] = np.nan if np.isnan(peak[t]) else -np.inf
+        if np.isnan(peak[t]) or np.isneginf(peak[t]):
+            continue
+        order = np.argsort(-z[t], kind="stable")[:top]
+        order = order[~np.isneginf(z[t, order])]
+        lp[t, :len(order)] = z[t, order] - peak[t] - log_sum[t]
+        tokens[t, :len(order)] = order
+    return lp, tokens
+
+
+def token_scores_backward(z, targets=None, grad_logprobs=None, grad_entropy=None):
+    """g (onehot - p) - e p (ln p + H); 0 for rows that are not read, whose g and e are 0, or where nothing
+    can occur."""
+    z = np.asarray(z, dtype=np.float64)
+    top, log_sum = row_stats(z)
+    h = entropy(z, targets)
+    out = np.zeros_like(z)
+    for t in np.flatnonzero(read_rows(z, targets)):
+        g = 0.0 if grad_logprobs is None else float(grad_logprobs[t])
+        e = 0.0 if grad_entropy is None else float(grad_entropy[t])
+        if (g == 0 and e == 0) or np.isneginf(top[t]):
+            continue
+        with np.errstate(invalid="ignore"):
+            ln_p = z[t] - top[t] - log_sum[t]
+            p = np.exp(ln_p)
+            out[t] = -g * p - e * p * np.where(np.isneginf(ln_p), 0.0, ln_p + h[t])
+        if targets is not None:
+            out[t, targets[t]] += g
+    return out
+
+
+# ---- from a gradient to the next parameters ---------------------------------------------------
+
+def grad_norm(grads, max_norm=np.inf, scale=1.0):
+    """(norm of all gradients times scale, the factor that clips them); factor NaN without a finite norm."""
+    norm = abs(scale) * np.sqrt(sum((np.asarray(g, dtype=np.float64) ** 2).sum() for g in grads))
+    if not np.isfinite(norm):
+        return norm, np.nan
+    return norm, scale * (max_norm / norm if norm > max_norm else 1.0)
+
+
+STATE_BLOCK = 256
+
+
+def _numbers(x):
+    """Numbers of the floats of 4 significant bits next to |x| (float32), ties to even."""
+    mantissa, exponent = np.frexp(np.abs(x).astype(np.float64))
+    # Below 2^-126 the spacing stays that of the smallest exponent.
+    step = np.ldexp(1.0, np.maximum(exponent, -125) - 4)
+    r = np.rint(np.abs(x).astype(np.float64) / step) * step
+    mantissa, exponent = np.frexp(r)
+    normal = (exponent + 126) * 8 + np.rint(mantissa * 16).astype(np.int64) - 8
+    return np.where(r == 0, 0, np.where(exponent >= -125, normal, np.rint(np.where(exponent >= -125, 0, r) / np.ldexp(1.0, -129)).astype(np.int64)))
+
+
+def _numbered(n):
+    """The float with number n."""
+    n = np.asarray(n, dtype=np.int64)
+    return np.where(n < 8, np.ldexp(n.astype(np.float64), -129), np.ldexp(1.0 + (n % 8) / 8.0, n // 8 - 127))
+
+
+def encode_states(x, signed):
+    """(bytes, one scale per block) of float32 states."""
+    x = np.asarray(x, dtype=np.float32)
+    codes, scales = np.zeros(len(x), dtype=np.uint8), np.zeros(-(-len(x) // STATE_BLOCK), dtype=np.float32)
+    levels = 127 if signed else 255
+    for b in range(len(scales)):
+        part = x[b * STATE_BLOCK:(b + 1) * STATE_BLOCK]
+        if not np.isfinite(part).all() or _numbers(part).max() >= 0x7F8:
+            scales[b] = np.nan
+            continue
+        number = _numbers(part)
+        most = max(number.max(), levels)
+        scales[b] = _numbered(most)
+        c = number - most + levels
+        c = np.where(c >= 1, c, np.where(c > -8, 1, 0) if signed else 1)
+        c = np.where(part == 0, 0, c)
+        codes[b * STATE_BLOCK:(b + 1) * STATE_BLOCK] = c + np.where((part < 0) & (c > 0), 128, 0)
+    return codes, scales
+
+
+def decode_states(codes, scales, signed):
+    """The numbers that the bytes stand for; NaN in blocks whose scale is not finite."""
+    codes, levels = np.asarray(codes, dtype=np.int64), 127 if signed else 255
+    scale = np.repeat(np.asarray(scales, dtype=np.float32), STATE_BLOCK)[:len(codes)]
+    c = codes % 128 if signed else codes
+    with np.errstate(invalid="ignore"):
+        number = np.where(np.isfinite(scale), _numbers(np.where(np.isfinite(scale), scale, 0)), 0) - levels + c
+    x = np.where(c == 0, 0.0, _numbered(np.maximum(number, 0)))
+    x = np.where(signed & (codes >= 128), -x, x)
+    return np.where(np.isfinite(scale), x, np.nan)
+
+
+def adamw(x, g, m, v, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, factor=1.0):
+    """(x', m', v') in 64 bits."""
+    x, g, m, v = (np.asarray(a, dtype=np.float64) for a in (x, g, m, v))
+    g = g * factor
+    m = beta1 * m + (1 - beta1) * g
+    v = beta2 * v + (1 - beta2) * g * g
+    m_hat, v_hat = m / (1 - beta1 ** step), v / (1 - beta2 ** step)
+    return x - lr * (weight_decay * x + m_hat / (np.sqrt(v_hat) + eps)), m, v

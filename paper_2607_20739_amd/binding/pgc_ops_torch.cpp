@@ -21,6 +21,9 @@
 #include <torch/csrc/utils/object_ptr.h>
 
 #include <initializer_list>
+#include <optional>
+#include <string>
+#include <vector>
 
 #include "pgc_ops.h"
 
@@ -49,6 +52,18 @@ const at::Tensor& tensor(const char* name, PyObject* o) {
   return t;
 }
 
+// A trace would take the results for constants.
+void refuse_traces() {
+  using Modes = c10::impl::TorchDispatchModeTLS;
+  TORCH_CHECK_NOT_IMPLEMENTED(!at::tracer::impl::is_dispatch_enabled() && !Modes::get_mode(c10::impl::TorchDispatchModeKey::PROXY),
+                              "the operators cannot be recorded in a trace");
+}
+
+// Past the dispatcher, which takes 0.4 us more.
+at::Tensor empty_on(const at::Device& device, at::IntArrayRef shape, at::ScalarType type) {
+  return at::cuda::empty(shape, type, at::kStrided, device, std::nullopt, std::nullopt);
+}
+
 // Row stride of a matrix whose shape has been looked at.
 int64_t row_stride(const char* name, const at::Tensor& t) {
   const int64_t rows = t.size(0), cols = t.size(1);
@@ -64,10 +79,7 @@ struct Matrix {
   int dtype;
 
   Matrix(const char* name, PyObject* o) : t(tensor(name, o)), dtype(dtype_of(t)) {
-    // A trace would take the result for a constant.
-    using Modes = c10::impl::TorchDispatchModeTLS;
-    TORCH_CHECK_NOT_IMPLEMENTED(!at::tracer::impl::is_dispatch_enabled() && !Modes::get_mode(c10::impl::TorchDispatchModeKey::PROXY),
-                                "the operators cannot be recorded in a trace");
+    refuse_traces();
     TORCH_CHECK_VALUE(t.dim() == 2 && dtype >= 0 && t.is_cuda() && t.layout() == at::kStrided,
                       name, " must be a 2-D float32, bfloat16 or float16 tensor on the GPU");
     rows = t.size(0);
@@ -76,10 +88,7 @@ struct Matrix {
   }
   void* data() const { return t.data_ptr(); }
   pgc_logits logits() const { return {data(), rows, cols, stride, dtype}; }
-  // Past the dispatcher, which takes 0.4 us more.
-  at::Tensor empty(at::IntArrayRef shape, at::ScalarType type) const {
-    return at::cuda::empty(shape, type, at::kStrided, t.device(), std::nullopt, std::nullopt);
-  }
+  at::Tensor empty(at::IntArrayRef shape, at::ScalarType type) const { return empty_on(t.device(), shape, type); }
 
   // Of this one's shape, type and GPU.
   int64_t like(const char* name, const at::Tensor& other) const {
@@ -140,6 +149,17 @@ uint64_t integer(PyObject* o) {
   return v;
 }
 
+// A whole number, not rounded or wrapped.
+int64_t whole(const char* name, PyObject* o) {
+  THPObjectPtr index(PyNumber_Index(o));
+  if (!index) throw python_error();
+  int over = 0;
+  const long long v = PyLong_AsLongLongAndOverflow(index.get(), &over);
+  if (v == -1 && PyErr_Occurred()) throw python_error();
+  TORCH_CHECK_VALUE(over == 0, name, " has more than 64 bits");
+  return v;
+}
+
 bool flag(PyObject* o) {
   const int v = PyObject_IsTrue(o);
   if (v < 0) throw python_error();
@@ -153,10 +173,9 @@ void check(int status) {
   throw python_error();
 }
 
-// Calls an entry point on torch's current stream of the GPU that `like` is on.
+// Calls an entry point on torch's current stream of a GPU.
 template <class Call>
-void launch(const Matrix& like, Call call) {
-  const c10::Device device = like.t.device();
+void launch(const c10::Device device, Call call) {
   THPObjectPtr index(PyLong_FromLong(device.index()));
   THPObjectPtr stream(index ? PyObject_CallOneArg(g_raw_stream, index.get()) : nullptr);
   if (!stream) throw python_error();
@@ -168,6 +187,12 @@ void launch(const Matrix& like, Call call) {
   status = call(handle);
   Py_END_ALLOW_THREADS
   check(status);
+}
+
+// ... of the GPU that `like` is on.
+template <class Call>
+void launch(const Matrix& like, Call call) {
+  launch(like.t.device(), call);
 }
 
 PyObject* tuple(std::initializer_list<at::Tensor> tensors) {
@@ -329,6 +354,263 @@ PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// logits, targets, top
+PyObject* token_scores(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  expect(n, 3);
+  const Matrix x("logits", a[0]);
+  const pgc_logits z = x.logits();
+  pgc_scores_args k{};
+  k.targets = x.ints("targets", a[1], x.rows);
+  k.top = whole("top", a[2]);
+  size_t bytes = 0;
+  check(pgc_token_scores_workspace_bytes(&z, k.top, &bytes));
+  at::Tensor workspace, logprobs;
+  if (bytes > 0) workspace = x.empty({static_cast<int64_t>(bytes)}, at::kByte);
+  // Without targets a NULL would be taken for none: an empty list of rows has no address.
+  const bool given = a[1] != Py_None;
+  if (given) logprobs = x.empty({x.rows}, at::kFloat);
+  const at::Tensor entropy = x.empty({x.rows}, at::kFloat), stats = x.empty({x.rows, 2}, at::kFloat);
+  const at::Tensor top_logprobs = x.empty({x.rows, k.top}, at::kFloat), top_tokens = x.empty({x.rows, k.top}, at::kInt);
+  if (given && x.rows > 0) k.logprobs = static_cast<float*>(logprobs.data_ptr());
+  k.entropy = static_cast<float*>(entropy.data_ptr());
+  k.stats = static_cast<float*>(stats.data_ptr());
+  k.top_logprobs = static_cast<float*>(top_logprobs.data_ptr());
+  k.top_tokens = static_cast<int32_t*>(top_tokens.data_ptr());
+  launch(x, [&](void* stream) { return pgc_token_scores(&z, &k, workspace.defined() ? workspace.data_ptr() : nullptr, bytes, stream); });
+  return tuple({logprobs, entropy, top_logprobs, top_tokens, stats});
+  END_HANDLE_TH_ERRORS
+}
+
+// logits, targets, stats, entropy, grad_logprobs, grad_entropy, out
+PyObject* token_scores_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  expect(n, 7);
+  const Matrix x("logits", a[0]);
+  const pgc_logits z = x.logits();
+  pgc_scores_grad_args k{};
+  k.targets = x.ints("targets", a[1], x.rows);
+  k.stats = static_cast<float*>(x.array("stats", a[2], at::kFloat, {x.rows, 2}));
+  k.entropy = x.floats("entropy", a[3], x.rows);
+  k.grad_logprobs = x.floats("grad_logprobs", a[4], x.rows);
+  k.grad_entropy = x.floats("grad_entropy", a[5], x.rows);
+  const Output out(x, a[6], true);
+  k.dlogits = out.t.data_ptr();
+  k.dlogits_stride = out.stride;
+  launch(x, [&](void* stream) { return pgc_token_scores_backward(&z, &k, stream); });
+  return THPVariable_Wrap(out.t);
+  END_HANDLE_TH_ERRORS
+}
+
+// A list of tensors: a Python sequence and its items, which it keeps alive.
+class List {
+ public:
+  List(const char* name, PyObject* o) : name_(name) {
+    TORCH_CHECK_VALUE(!THPVariable_Check(o) && PySequence_Check(o), name, " must be a list of tensors");
+    items_ = THPObjectPtr(PySequence_Fast(o, "a list of tensors"));
+    if (!items_) throw python_error();
+  }
+  int64_t size() const { return PySequence_Fast_GET_SIZE(items_.get()); }
+  PyObject* item(int64_t i) const { return PySequence_Fast_GET_ITEM(items_.get(), i); }
+  const at::Tensor& operator[](int64_t i) const { return tensor(name_, item(i)); }
+  const char* name() const { return name_; }
+  void expect_size(int64_t n) const { TORCH_CHECK_VALUE(size() == n, name_, " must have as many tensors as the first list: ", n); }
+
+ private:
+  const char* name_;
+  mutable THPObjectPtr items_;
+};
+
+// A GPU tensor whose values lie one after the other in memory, in some order of its dimensions.
+const at::Tensor& dense(const char* name, const at::Tensor& t) {
+  TORCH_CHECK_VALUE(t.is_cuda() && t.layout() == at::kStrided, name, " must be tensors on the GPU");
+  TORCH_CHECK_VALUE(t.is_non_overlapping_and_dense(), name, " must be tensors without gaps between their values");
+  return t;
+}
+// ... that has its values in the same places as another.
+const at::Tensor& beside(const char* name, const at::Tensor& t, const at::Tensor& like) {
+  TORCH_CHECK_VALUE(t.device() == like.device() && t.layout() == at::kStrided && t.sizes() == like.sizes() &&
+                        (t.strides() == like.strides() || (t.is_contiguous() && like.is_contiguous())),
+                    name, " must have the shape, strides and device of the tensor that they belong to");
+  return t;
+}
+int floating(const char* name, const at::Tensor& t) {
+  const int dtype = dtype_of(t);
+  TORCH_CHECK_VALUE(dtype >= 0, name, " must be float32, bfloat16 or float16 tensors");
+  return dtype;
+}
+void of_type(const char* name, const at::Tensor& t, at::ScalarType type) {
+  TORCH_CHECK_VALUE(t.scalar_type() == type, name, " must be ", type, " tensors");
+}
+
+// The call changes the tensor: autograd notices a saved one by its version.
+void written(const at::Tensor& t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+void no_gradient(const char* name, const at::Tensor& t) {
+  TORCH_CHECK_VALUE(!t.requires_grad() || !at::GradMode::is_enabled(), name, " must not ask for a gradient (detach() them)");
+}
+
+// One value on the GPU; null for None.
+void* single(const char* name, PyObject* o, at::ScalarType type, const std::optional<at::Device>& device) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = tensor(name, o);
+  TORCH_CHECK_VALUE(t.scalar_type() == type && t.numel() == 1 && t.is_cuda() && (!device || t.device() == *device),
+                    name, " must be a ", type, " tensor of one value on the GPU of the others");
+  return t.data_ptr();
+}
+
+// grads, max_norm, scale
+PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  expect(n, 3);
+  refuse_traces();
+  const List grads("grads", a[0]);
+  TORCH_CHECK_VALUE(grads.size() > 0, "grads must hold a tensor");
+  const at::Device device = dense("grads", grads[0]).device();
+  std::vector<pgc_values> values(grads.size());
+  for (int64_t i = 0; i < grads.size(); ++i) {
+    const at::Tensor& t = dense("grads", grads[i]);
+    TORCH_CHECK_VALUE(t.device() == device, "grads must be on one GPU");
+    values[i] = {t.data_ptr(), t.numel(), floating("grads", t)};
+  }
+  const double max_norm = number(a[1]), scale = number(a[2]);
+  size_t bytes = 0;
+  check(pgc_grad_norm_workspace_bytes(values.data(), grads.size(), &bytes));
+  at::Tensor workspace;
+  if (bytes > 0) workspace = empty_on(device, {static_cast<int64_t>(bytes)}, at::kByte);
+  const at::Tensor norm = empty_on(device, {1}, at::kFloat), factor = empty_on(device, {1}, at::kFloat);
+  launch(device, [&](void* stream) {
+    return pgc_grad_norm(values.data(), grads.size(), max_norm, scale, static_cast<float*>(norm.data_ptr()),
+                         static_cast<float*>(factor.data_ptr()), workspace.defined() ? workspace.data_ptr() : nullptr, bytes, stream);
+  });
+  return tuple({norm, factor});
+  END_HANDLE_TH_ERRORS
+}
+
+// params, grads, moments, variances, step, lr, beta1, beta2, eps, weight_decay, scales, copies, factor
+PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  expect(n, 13);
+  refuse_traces();
+  const List params("params", a[0]), grads("grads", a[1]), moments("moments", a[2]), variances("variances", a[3]);
+  const int64_t count = params.size();
+  grads.expect_size(count);
+  moments.expect_size(count);
+  variances.expect_size(count);
+  std::optional<List> scales, copies, decays;
+  if (a[10] != Py_None) {
+    scales.emplace("scales", a[10]);
+    scales->expect_size(count);
+  }
+  if (a[11] != Py_None) {
+    copies.emplace("copies", a[11]);
+    copies->expect_size(count);
+  }
+  double decay = 0.0;
+  if (PySequence_Check(a[9]) && !THPVariable_Check(a[9])) {
+    decays.emplace("weight_decay", a[9]);
+    decays->expect_size(count);
+  } else {
+    decay = number(a[9]);
+  }
+  std::optional<at::Device> device;
+  std::vector<pgc_adamw_tensor> tensors(count);
+  for (int64_t i = 0; i < count; ++i) {
+    const at::Tensor& p = dense("params", params[i]);
+    if (!device) device = p.device();
+    TORCH_CHECK_VALUE(p.device() == *device, "params must be on one GPU");
+    TORCH_CHECK_VALUE(p.is_leaf() || !p.requires_grad() || !at::GradMode::is_enabled(),
+                      "params that were computed cannot be changed where a gradient is asked for (detach() them)");
+    const at::Tensor &g = beside("grads", grads[i], p), &m = beside("moments", moments[i], p), &v = beside("variances", variances[i], p);
+    of_type("moments", m, scales ? at::kByte : at::kFloat);
+    of_type("variances", v, scales ? at::kByte : at::kFloat);
+    no_gradient("moments", m);
+    no_gradient("variances", v);
+    pgc_adamw_tensor& t = tensors[i];
+    t.param = p.data_ptr();
+    t.grad = g.data_ptr();
+    t.m = m.data_ptr();
+    t.v = v.data_ptr();
+    t.count = p.numel();
+    t.param_dtype = floating("params", p);
+    t.grad_dtype = floating("grads", g);
+    if (scales) {
+      const at::Tensor& s = (*scales)[i];
+      const int64_t blocks = (t.count + 255) / 256;
+      TORCH_CHECK_VALUE(s.device() == *device && s.scalar_type() == at::kFloat && s.sizes() == at::IntArrayRef({blocks, 2}) && s.is_contiguous(),
+                        "scales must be contiguous float32 tensors of shape [blocks of 256 values, 2]");
+      no_gradient("scales", s);
+      t.scales = static_cast<float*>(s.data_ptr());
+    }
+    if (copies) {
+      const at::Tensor& c = beside("copies", (*copies)[i], p);
+      no_gradient("copies", c);
+      t.copy = c.data_ptr();
+      t.copy_dtype = floating("copies", c);
+    }
+    t.weight_decay = decays ? number(decays->item(i)) : decay;
+  }
+  pgc_adamw_args k{};
+  if (THPVariable_Check(a[4])) k.step_at = static_cast<int64_t*>(single("step", a[4], at::kLong, device));
+  else k.step = whole("step", a[4]);
+  if (THPVariable_Check(a[5])) k.lr_at = static_cast<float*>(single("lr", a[5], at::kFloat, device));
+  else k.lr = number(a[5]);
+  k.beta1 = number(a[6]);
+  k.beta2 = number(a[7]);
+  k.eps = number(a[8]);
+  k.factor = static_cast<float*>(single("factor", a[12], at::kFloat, device));
+  k.state_bits = scales ? 8 : 32;
+  if (!device) {    // no tensor to launch anything for: the arguments alone are looked at
+    check(pgc_adamw(nullptr, 0, &k, nullptr));
+    Py_RETURN_NONE;
+  }
+  launch(*device, [&](void* stream) { return pgc_adamw(tensors.data(), count, &k, stream); });
+  for (int64_t i = 0; i < count; ++i) {
+    written(params[i]);
+    written(moments[i]);
+    written(variances[i]);
+    if (scales) written((*scales)[i]);
+    if (copies) written((*copies)[i]);
+  }
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
+// moments, variances, scales, moment values, variance values
+PyObject* adamw_state_values(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  expect(n, 5);
+  refuse_traces();
+  const List moments("moments", a[0]), variances("variances", a[1]), scales("scales", a[2]), ms("out", a[3]), vs("out", a[4]);
+  const int64_t count = moments.size();
+  for (const List* l : {&variances, &scales, &ms, &vs}) l->expect_size(count);
+  if (count == 0) Py_RETURN_NONE;
+  std::vector<pgc_adamw_state> tensors(count);
+  const at::Device device = dense("moments", moments[0]).device();
+  for (int64_t i = 0; i < count; ++i) {
+    const at::Tensor &m = dense("moments", moments[i]), &v = beside("variances", variances[i], m), &s = scales[i];
+    const at::Tensor &mv = beside("out", ms[i], m), &vv = beside("out", vs[i], m);
+    TORCH_CHECK_VALUE(m.device() == device, "moments must be on one GPU");
+    of_type("moments", m, at::kByte);
+    of_type("variances", v, at::kByte);
+    TORCH_CHECK_VALUE(s.device() == device && s.scalar_type() == at::kFloat && s.sizes() == at::IntArrayRef({(m.numel() + 255) / 256, 2}) && s.is_contiguous(),
+                      "scales must be contiguous float32 tensors of shape [blocks of 256 values, 2]");
+    TORCH_CHECK_VALUE((mv.scalar_type() == at::kFloat || mv.scalar_type() == at::kBFloat16) && vv.scalar_type() == mv.scalar_type(),
+                      "out must be float32 or bfloat16 tensors");
+    no_gradient("out", mv);
+    no_gradient("out", vv);
+    tensors[i] = {m.data_ptr(), v.data_ptr(), static_cast<float*>(s.data_ptr()), mv.data_ptr(), vv.data_ptr(), m.numel(), dtype_of(mv)};
+  }
+  launch(device, [&](void* stream) { return pgc_adamw_state_values(tensors.data(), count, stream); });
+  for (int64_t i = 0; i < count; ++i) {
+    written(ms[i]);
+    written(vs[i]);
+  }
+  Py_RETURN_NONE;
+  END_HANDLE_TH_ERRORS
+}
+
 template <class F>
 constexpr PyMethodDef method(const char* name, F f) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr};
@@ -345,7 +627,8 @@ PyMODINIT_FUNC PyInit__ops_torch(void) {
   static PyMethodDef methods[] = {
       method("dropout", dropout), method("dropout_backward", dropout_backward), method("token_logprobs", token_logprobs),
       method("token_logprobs_backward", token_logprobs_backward), method("preference_loss", preference_loss),
-      method("policy_loss", policy_loss), {nullptr, nullptr, 0, nullptr}};
+      method("policy_loss", policy_loss), method("token_scores", token_scores), method("token_scores_backward", token_scores_backward),
+      method("grad_norm", grad_norm), method("adamw", adamw), method("adamw_state_values", adamw_state_values), {nullptr, nullptr, 0, nullptr}};
   static PyModuleDef module = {PyModuleDef_HEAD_INIT, "_ops_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
   if (g_raw_stream == nullptr) g_raw_stream = imported("torch._C", "_cuda_getCurrentRawStream");
   if (g_error == nullptr && g_raw_stream) g_error = imported("paper_2607_20739_amd._lib", "PGCError");

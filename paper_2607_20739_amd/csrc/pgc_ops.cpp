@@ -2,9 +2,12 @@
 // and launches.
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <new>
+#include <vector>
 
 #include "pgc_ops.h"
 #include "pgc_ops_kernels.h"
@@ -135,14 +138,14 @@ int dropout(const pgc_dropout_args* a, void* stream) {
 }
 
 // The logits and their targets, with the columns' lower bound.
-int check_logits(const pgc_logits* z, const int32_t* targets) {
+int check_logits(const pgc_logits* z, const int32_t* targets, bool targets_required = true) {
   if (!known(z->dtype)) return fail(PGC_EINVAL, "unknown dtype %d", z->dtype);
   CHECK(check_extents(z->rows, z->cols));
   if (z->cols < 1) return fail(PGC_EINVAL, "logits need at least one column");
   CHECK(check_stride("logits", z->stride, z->cols));
   const int b = value_bytes(z->dtype);
   CHECK(check_pointer(matrix("logits", z->data, z->rows, z->cols, z->stride, b), b, true));
-  return check_pointer(array("targets", targets, z->rows, 4), 4, true);
+  return check_pointer(array("targets", targets, z->rows, 4), 4, targets_required);
 }
 
 // An array of `count` floats that is read or written.
@@ -179,6 +182,265 @@ pgc::LogitsArgs logits_args(const pgc_logits* z, const int32_t* targets) {
 }
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+
+// ---- many tensors ---------------------------------------------------------------------------
+
+// So many values need fewer blocks than a grid may have, and more memory than a GPU has.
+constexpr int64_t kMostCount = int64_t{1} << 38, kMostInList = int64_t{1} << 20;
+
+int check_list(const void* tensors, int64_t n) {
+  if (n < 0 || n > kMostInList) return fail(PGC_EINVAL, "the number of tensors must lie in [0, 2^20]");
+  return tensors == nullptr && n > 0 ? fail(PGC_EINVAL, "tensors is NULL") : PGC_OK;
+}
+
+// A tensor's values, and how many there are so far.
+int check_count(int64_t count, int64_t* values) {
+  if (count < 0 || count > kMostCount - *values) return fail(PGC_EINVAL, "counts must not be negative, nor exceed 2^38 together");
+  *values += count;
+  return PGC_OK;
+}
+
+// All of many arrays; `written` ones overlap no other.
+struct Range {
+  uintptr_t from, to;
+  const char* name;
+  bool written;
+};
+
+class Ranges {
+ public:
+  // One kind of array of all tensors after the other: their addresses mostly rise, so that each kind is in order
+  // already, and kinds are merged.
+  void begin_kind() { kinds_.push_back(all_.size()); }
+  void add(const char* name, const void* p, size_t bytes, bool written) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+    if (at != 0 && bytes > 0) all_.push_back({at, at + bytes, name, written});
+  }
+  int check() {
+    auto before = [](const Range& a, const Range& b) { return a.from < b.from; };
+    kinds_.push_back(all_.size());
+    for (size_t k = 0; k + 1 < kinds_.size(); ++k) {
+      const auto a = all_.begin() + kinds_[k], b = all_.begin() + kinds_[k + 1];
+      if (!std::is_sorted(a, b, before)) std::sort(a, b, before);
+      std::inplace_merge(all_.begin(), a, b, before);
+    }
+    // Of the ranges so far: the one that ends last, and that of the written ones.
+    Range last{0, 0, "", false}, written = last;
+    for (const Range& r : all_) {
+      if (r.from < written.to) return fail(PGC_EINVAL, "%s overlaps %s", written.name, r.name);
+      if (r.written && r.from < last.to) return fail(PGC_EINVAL, "%s overlaps %s", r.name, last.name);
+      if (r.to > last.to) last = r;
+      if (r.written) written = r;
+    }
+    return PGC_OK;
+  }
+
+ private:
+  std::vector<Range> all_;
+  std::vector<size_t> kinds_{0};
+};
+
+// Deals tensors out to launches of at most `most`, each with the first block of its own: calls
+// put(args, slot, index) for a tensor with values, launch(args, blocks) for each full or last one.
+template <class Args, class Count, class Put, class Launch>
+int deal(Args& args, int64_t n, int most, int64_t chunk, Count count, Put put, Launch launch) {
+  int64_t blocks = 0;
+  args.tensors = 0;
+  args.chunk = static_cast<int32_t>(chunk);
+  for (int64_t i = 0; i < n; ++i) {
+    if (count(i) == 0) continue;
+    put(args, args.tensors, i);
+    args.first[args.tensors++] = static_cast<int32_t>(blocks);
+    blocks += (count(i) + chunk - 1) / chunk;
+    if (args.tensors < most) continue;
+    CHECK(launch(args, blocks));
+    args.tensors = 0;
+    blocks = 0;
+  }
+  return args.tensors > 0 ? launch(args, blocks) : PGC_OK;
+}
+
+int adamw(const pgc_adamw_tensor* tensors, int64_t n, const pgc_adamw_args* a, hipStream_t stream) {
+  CHECK(check_list(tensors, n));
+  const bool small = a->state_bits == 8;
+  if (!small && a->state_bits != 32) return fail(PGC_EINVAL, "state_bits must be 32 or 8");
+  if (!(a->lr >= 0.0) || !finite32(a->lr)) return fail(PGC_EINVAL, "lr must be finite and not negative");
+  if (!(a->beta1 >= 0.0 && a->beta1 < 1.0) || !(a->beta2 >= 0.0 && a->beta2 < 1.0) || static_cast<float>(a->beta1) == 1.f ||
+      static_cast<float>(a->beta2) == 1.f)
+    return fail(PGC_EINVAL, "beta1 and beta2 must lie in [0, 1)");
+  if (!(static_cast<float>(a->eps) > 0.f) || !finite32(a->eps)) return fail(PGC_EINVAL, "eps must be positive and finite");
+  if (a->step_at == nullptr && a->step < 1) return fail(PGC_EINVAL, "step must be at least 1");
+  CHECK(check_floats("lr_at", a->lr_at, 1, false));
+  CHECK(check_pointer(array("step_at", a->step_at, 1, 8), 8, false));
+  CHECK(check_floats("factor", a->factor, 1, false));
+  Ranges ranges;
+  ranges.add("lr_at", a->lr_at, 4, false);
+  ranges.add("step_at", a->step_at, 8, false);
+  ranges.add("factor", a->factor, 4, false);
+  int64_t values = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    const pgc_adamw_tensor& t = tensors[i];
+    CHECK(check_count(t.count, &values));
+    if (!known(t.param_dtype)) return fail(PGC_EINVAL, "unknown param dtype %d", t.param_dtype);
+    if (!known(t.grad_dtype)) return fail(PGC_EINVAL, "unknown grad dtype %d", t.grad_dtype);
+    if (t.copy && !known(t.copy_dtype)) return fail(PGC_EINVAL, "unknown copy dtype %d", t.copy_dtype);
+    if (!(t.weight_decay >= 0.0) || !finite32(t.weight_decay) || !finite32(t.weight_decay * a->lr))
+      return fail(PGC_EINVAL, "weight_decay must be finite and not negative");
+    const int pb = value_bytes(t.param_dtype), gb = value_bytes(t.grad_dtype), cb = value_bytes(t.copy_dtype), sb = small ? 1 : 4;
+    CHECK(check_pointer(array("param", t.param, t.count, pb), pb, true));
+    CHECK(check_pointer(array("grad", t.grad, t.count, gb), gb, true));
+    CHECK(check_pointer(array("copy", t.copy, t.count, cb), cb, false));
+    CHECK(check_pointer(array("m", t.m, t.count, sb), sb, true));
+    CHECK(check_pointer(array("v", t.v, t.count, sb), sb, true));
+    CHECK(check_pointer(array("scales", t.scales, small ? t.count : 0, 8), 8, true));
+  }
+  auto each = [&](const char* name, bool written, auto address, auto bytes) {
+    ranges.begin_kind();
+    for (int64_t i = 0; i < n; ++i) ranges.add(name, address(tensors[i]), bytes(tensors[i]), written);
+  };
+  using Tensor = const pgc_adamw_tensor&;
+  const size_t sb = small ? 1 : 4;
+  each("param", true, [](Tensor t) { return t.param; }, [](Tensor t) -> size_t { return t.count * value_bytes(t.param_dtype); });
+  each("grad", false, [](Tensor t) { return t.grad; }, [](Tensor t) -> size_t { return t.count * value_bytes(t.grad_dtype); });
+  each("copy", true, [](Tensor t) { return t.copy; }, [](Tensor t) -> size_t { return t.count * value_bytes(t.copy_dtype); });
+  each("m", true, [](Tensor t) { return t.m; }, [=](Tensor t) -> size_t { return t.count * sb; });
+  each("v", true, [](Tensor t) { return t.v; }, [=](Tensor t) -> size_t { return t.count * sb; });
+  if (small) each("scales", true, [](Tensor t) { return t.scales; }, [](Tensor t) -> size_t { return (t.count + 255) / 256 * 8; });
+  CHECK(ranges.check());
+
+  pgc::AdamwArgs k{};
+  k.beta1 = static_cast<float>(a->beta1);
+  k.rest1 = static_cast<float>(1.0 - a->beta1);
+  k.beta2 = static_cast<float>(a->beta2);
+  k.rest2 = static_cast<float>(1.0 - a->beta2);
+  k.eps = static_cast<float>(a->eps);
+  k.lr = a->lr;
+  k.log_beta1 = std::log(a->beta1);
+  k.log_beta2 = std::log(a->beta2);
+  k.step = a->step;
+  k.rate = static_cast<float>(a->lr / -std::expm1(a->step * k.log_beta1));
+  k.spread = static_cast<float>(1.0 / std::sqrt(-std::expm1(a->step * k.log_beta2)));
+  k.lr_at = a->lr_at;
+  k.step_at = a->step_at;
+  k.factor = a->factor;
+  return deal(k, n, pgc::kMostTensors, pgc::adamw_chunk(values), [&](int64_t i) { return tensors[i].count; },
+              [&](pgc::AdamwArgs& args, int at, int64_t i) {
+                const pgc_adamw_tensor& t = tensors[i];
+                args.tensor[at] = {t.param, t.grad, t.copy, t.m, t.v, t.scales, t.count,
+                                   static_cast<float>(a->lr_at ? t.weight_decay : t.weight_decay * a->lr),
+                                   static_cast<int8_t>(t.param_dtype), static_cast<int8_t>(t.grad_dtype), static_cast<int8_t>(t.copy_dtype)};
+              },
+              [&](const pgc::AdamwArgs& args, int64_t blocks) {
+                return launched(pgc::launch_adamw(args, blocks, a->state_bits, stream), "AdamW kernel");
+              });
+}
+
+int state_values(const pgc_adamw_state* tensors, int64_t n, hipStream_t stream) {
+  CHECK(check_list(tensors, n));
+  Ranges ranges;
+  int64_t values = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    const pgc_adamw_state& t = tensors[i];
+    CHECK(check_count(t.count, &values));
+    if (t.dtype != PGC_F32 && t.dtype != PGC_BF16) return fail(PGC_EINVAL, "the values must be float or bf16");
+    const int b = value_bytes(t.dtype);
+    CHECK(check_pointer(array("m", t.m, t.count, 1), 1, true));
+    CHECK(check_pointer(array("v", t.v, t.count, 1), 1, true));
+    CHECK(check_pointer(array("scales", t.scales, t.count, 8), 8, true));
+    CHECK(check_pointer(array("m_values", t.m_values, t.count, b), b, true));
+    CHECK(check_pointer(array("v_values", t.v_values, t.count, b), b, true));
+  }
+  auto each = [&](const char* name, bool written, auto address, auto bytes) {
+    ranges.begin_kind();
+    for (int64_t i = 0; i < n; ++i) ranges.add(name, address(tensors[i]), bytes(tensors[i]), written);
+  };
+  using Tensor = const pgc_adamw_state&;
+  each("m", false, [](Tensor t) { return t.m; }, [](Tensor t) -> size_t { return t.count; });
+  each("v", false, [](Tensor t) { return t.v; }, [](Tensor t) -> size_t { return t.count; });
+  each("scales", false, [](Tensor t) { return t.scales; }, [](Tensor t) -> size_t { return (t.count + 255) / 256 * 8; });
+  each("m_values", true, [](Tensor t) { return t.m_values; }, [](Tensor t) -> size_t { return t.count * value_bytes(t.dtype); });
+  each("v_values", true, [](Tensor t) { return t.v_values; }, [](Tensor t) -> size_t { return t.count * value_bytes(t.dtype); });
+  CHECK(ranges.check());
+  pgc::StateArgs k{};
+  return deal(k, n, pgc::kMostTensors, pgc::adamw_chunk(values), [&](int64_t i) { return tensors[i].count; },
+              [&](pgc::StateArgs& args, int at, int64_t i) {
+                const pgc_adamw_state& t = tensors[i];
+                args.m[at] = t.m;
+                args.v[at] = t.v;
+                args.scales[at] = t.scales;
+                args.m_values[at] = t.m_values;
+                args.v_values[at] = t.v_values;
+                args.count[at] = t.count;
+                args.dtype[at] = static_cast<int8_t>(t.dtype);
+              },
+              [&](const pgc::StateArgs& args, int64_t blocks) {
+                return launched(pgc::launch_state_values(args, blocks, stream), "state kernel");
+              });
+}
+
+// The blocks of the norm's sums, and their chunk.
+int norm_blocks(const pgc_values* tensors, int64_t n, int64_t* blocks, int64_t* chunk) {
+  CHECK(check_list(tensors, n));
+  int64_t values = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    CHECK(check_count(tensors[i].count, &values));
+    if (!known(tensors[i].dtype)) return fail(PGC_EINVAL, "unknown dtype %d", tensors[i].dtype);
+  }
+  *chunk = pgc::norm_chunk(values);
+  *blocks = 0;
+  for (int64_t i = 0; i < n; ++i) *blocks += (tensors[i].count + *chunk - 1) / *chunk;
+  return PGC_OK;
+}
+
+int grad_norm(const pgc_values* tensors, int64_t n, double max_norm, double scale, float* norm, float* factor,
+              void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  int64_t blocks = 0, chunk = 0;
+  CHECK(norm_blocks(tensors, n, &blocks, &chunk));
+  if (!(max_norm > 0.0)) return fail(PGC_EINVAL, "max_norm must be positive");
+  if (!finite32(scale)) return fail(PGC_EINVAL, "scale must be finite");
+  CHECK(check_floats("norm", norm, 1, false));
+  CHECK(check_floats("factor", factor, 1, false));
+  const size_t need = align_up(8 * static_cast<size_t>(blocks));
+  CHECK(check_pointer({"workspace", reinterpret_cast<uintptr_t>(workspace), need}, kAlign, true));
+  if (workspace_bytes < need) return fail(PGC_EINVAL, "workspace too small: need %zu bytes", need);
+  Ranges ranges;
+  ranges.add("norm", norm, 4, true);
+  ranges.begin_kind();
+  ranges.add("factor", factor, 4, true);
+  ranges.begin_kind();
+  ranges.add("workspace", workspace, need, true);
+  ranges.begin_kind();
+  for (int64_t i = 0; i < n; ++i) {
+    const int b = value_bytes(tensors[i].dtype);
+    CHECK(check_pointer(array("gradient", tensors[i].data, tensors[i].count, b), b, true));
+    ranges.add("gradient", tensors[i].data, tensors[i].count * static_cast<size_t>(b), false);
+  }
+  CHECK(ranges.check());
+  double* sums = static_cast<double*>(workspace);
+  pgc::NormArgs k{};
+  CHECK(deal(k, n, pgc::kMostValues, chunk, [&](int64_t i) { return tensors[i].count; },
+             [&](pgc::NormArgs& args, int at, int64_t i) {
+               args.data[at] = tensors[i].data;
+               args.count[at] = tensors[i].count;
+               args.dtype[at] = static_cast<int8_t>(tensors[i].dtype);
+             },
+             [&](pgc::NormArgs& args, int64_t blocks_now) {
+               args.sums = sums;
+               sums += blocks_now;
+               return launched(pgc::launch_norm_sums(args, blocks_now, stream), "norm kernel");
+             }));
+  return launched(pgc::launch_norm_end({static_cast<double*>(workspace), blocks, max_norm, scale, norm, factor}, stream), "norm kernel");
+}
+
+// Lists take host memory: without it a call fails like any other.
+template <class Call>
+int with_memory(Call call) {
+  try {
+    return call();
+  } catch (const std::bad_alloc&) {
+    return fail(PGC_EINVAL, "too many tensors for the host's memory");
+  }
+}
 
 }  // namespace
 
@@ -373,6 +635,110 @@ int pgc_policy_loss(const pgc_logits* logits, const pgc_policy_args* a, void* hi
   k.scale = static_cast<float>(a->scale);
   return launched(pgc::launch_logits(k, pgc::RowMode::kPolicy, logits->dtype, static_cast<hipStream_t>(hip_stream)),
                   "policy loss kernel");
+}
+
+int pgc_token_scores_workspace_bytes(const pgc_logits* logits, int64_t top, size_t* bytes) {
+  if (logits == nullptr || bytes == nullptr) return fail(PGC_EINVAL, "null arguments");
+  if (!known(logits->dtype)) return fail(PGC_EINVAL, "unknown dtype %d", logits->dtype);
+  CHECK(check_extents(logits->rows, logits->cols));
+  if (top < 0 || top > PGC_MAX_TOP) return fail(PGC_EINVAL, "top must lie in [0, %d]", PGC_MAX_TOP);
+  *bytes = align_up(pgc::scores_workspace_bytes(logits->rows, logits->cols, top, logits->dtype));
+  return PGC_OK;
+}
+
+int pgc_token_scores(const pgc_logits* logits, const pgc_scores_args* a, void* workspace, size_t workspace_bytes,
+                     void* hip_stream) {
+  if (logits == nullptr || a == nullptr) return fail(PGC_EINVAL, "null arguments");
+  const int64_t rows = logits->rows;
+  CHECK(check_logits(logits, a->targets, false));
+  if (a->top < 0 || a->top > PGC_MAX_TOP) return fail(PGC_EINVAL, "top must lie in [0, %d]", PGC_MAX_TOP);
+  if (a->targets == nullptr && a->logprobs != nullptr) return fail(PGC_EINVAL, "logprobs need targets");
+  CHECK(check_floats("logprobs", a->logprobs, rows, a->targets != nullptr));
+  CHECK(check_floats("entropy", a->entropy, rows, false));
+  CHECK(check_pointer(array("stats", a->stats, rows, 8), 8, false));
+  const Span top_logprobs = array("top_logprobs", a->top_logprobs, rows * a->top, 4);
+  const Span top_tokens = array("top_tokens", a->top_tokens, rows * a->top, 4);
+  CHECK(check_pointer(top_logprobs, 4, true));
+  CHECK(check_pointer(top_tokens, 4, true));
+  size_t need = 0;
+  CHECK(pgc_token_scores_workspace_bytes(logits, a->top, &need));
+  const Span ws = {"workspace", reinterpret_cast<uintptr_t>(workspace), need};
+  CHECK(check_pointer(ws, kAlign, true));
+  if (workspace_bytes < need) return fail(PGC_EINVAL, "workspace too small: need %zu bytes", need);
+  const Span outs[] = {array("logprobs", a->logprobs, rows, 4), array("entropy", a->entropy, rows, 4),
+                       array("stats", a->stats, rows, 8), top_logprobs, top_tokens, ws};
+  const Span ins[] = {matrix("logits", logits->data, rows, logits->cols, logits->stride, value_bytes(logits->dtype)),
+                      array("targets", a->targets, rows, 4)};
+  CHECK(check_all_apart(outs, 6, ins, 2));
+  if (rows == 0) return PGC_OK;
+  pgc::ScoresArgs k{};
+  k.logits = logits->data;
+  k.targets = a->targets;
+  k.rows = rows;
+  k.cols = logits->cols;
+  k.stride = logits->stride;
+  k.top = static_cast<int32_t>(a->top);
+  k.logprobs = a->logprobs;
+  k.entropy = a->entropy;
+  k.stats = a->stats;
+  k.top_logprobs = a->top_logprobs;
+  k.top_tokens = a->top_tokens;
+  return launched(pgc::launch_scores(k, logits->dtype, workspace, static_cast<hipStream_t>(hip_stream)), "scores kernel");
+}
+
+int pgc_token_scores_backward(const pgc_logits* logits, const pgc_scores_grad_args* a, void* hip_stream) {
+  if (logits == nullptr || a == nullptr) return fail(PGC_EINVAL, "null arguments");
+  const int64_t rows = logits->rows;
+  CHECK(check_logits(logits, a->targets, false));
+  if (a->targets == nullptr && a->grad_logprobs != nullptr) return fail(PGC_EINVAL, "grad_logprobs needs targets");
+  CHECK(check_pointer(array("stats", a->stats, rows, 8), 8, true));
+  CHECK(check_floats("entropy", a->entropy, rows, a->grad_entropy != nullptr));
+  CHECK(check_floats("grad_logprobs", a->grad_logprobs, rows, false));
+  CHECK(check_floats("grad_entropy", a->grad_entropy, rows, false));
+  if (rows > 0 && a->grad_logprobs == nullptr && a->grad_entropy == nullptr) return fail(PGC_EINVAL, "neither of the gradients is given");
+  CHECK(check_dlogits(logits, a->dlogits, a->dlogits_stride));
+  const Span outs[] = {matrix("dlogits", a->dlogits, rows, logits->cols, a->dlogits_stride, value_bytes(logits->dtype))};
+  const Span ins[] = {array("targets", a->targets, rows, 4), array("stats", a->stats, rows, 8), array("entropy", a->entropy, rows, 4),
+                      array("grad_logprobs", a->grad_logprobs, rows, 4), array("grad_entropy", a->grad_entropy, rows, 4)};
+  CHECK(check_all_apart(outs, 1, ins, 5));
+  if (rows == 0) return PGC_OK;
+  pgc::ScoresArgs k{};
+  k.logits = logits->data;
+  k.targets = a->targets;
+  k.rows = rows;
+  k.cols = logits->cols;
+  k.stride = logits->stride;
+  k.out_stride = a->dlogits_stride;
+  k.stats = const_cast<float*>(a->stats);
+  k.entropy = const_cast<float*>(a->entropy);
+  k.grad_logprobs = a->grad_logprobs;
+  k.grad_entropy = a->grad_entropy;
+  k.dlogits = a->dlogits;
+  return launched(pgc::launch_scores_gradient(k, logits->dtype, static_cast<hipStream_t>(hip_stream)), "scores gradient kernel");
+}
+
+int pgc_grad_norm_workspace_bytes(const pgc_values* tensors, int64_t n, size_t* bytes) {
+  if (bytes == nullptr) return fail(PGC_EINVAL, "null arguments");
+  int64_t blocks = 0, chunk = 0;
+  CHECK(norm_blocks(tensors, n, &blocks, &chunk));
+  *bytes = align_up(8 * static_cast<size_t>(blocks));
+  return PGC_OK;
+}
+
+int pgc_grad_norm(const pgc_values* tensors, int64_t n, double max_norm, double scale, float* norm, float* factor,
+                  void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return with_memory([&] {
+    return grad_norm(tensors, n, max_norm, scale, norm, factor, workspace, workspace_bytes, static_cast<hipStream_t>(hip_stream));
+  });
+}
+
+int pgc_adamw(const pgc_adamw_tensor* tensors, int64_t n, const pgc_adamw_args* args, void* hip_stream) {
+  if (args == nullptr) return fail(PGC_EINVAL, "null arguments");
+  return with_memory([&] { return adamw(tensors, n, args, static_cast<hipStream_t>(hip_stream)); });
+}
+
+int pgc_adamw_state_values(const pgc_adamw_state* tensors, int64_t n, void* hip_stream) {
+  return with_memory([&] { return state_values(tensors, n, static_cast<hipStream_t>(hip_stream)); });
 }
 
 }  // extern "C"

@@ -73,4 +73,86 @@ hipError_t launch_pair_gradient(const LogitsArgs& a, const PairArgs& p, int dtyp
 bool preference_is_small(int64_t rows, int64_t cols, int64_t pairs, int dtype);
 hipError_t launch_small_preference(const LogitsArgs& a, const PairArgs& p, int dtype, hipStream_t stream);
 
+// Scores of tokens and their gradient (a.dlogits).
+struct ScoresArgs {
+  const void* logits;
+  const int32_t* targets;  // or null: every row is read
+  int64_t rows, cols, stride, out_stride;
+  int32_t top;
+  float* logprobs;         // null without targets
+  float* entropy;          // or null; of the gradient: read
+  float* stats;            // or null; of the gradient: read
+  float* top_logprobs;
+  int32_t* top_tokens;
+  const float* grad_logprobs;   // or null
+  const float* grad_entropy;    // or null
+  void* dlogits;
+};
+hipError_t launch_scores(const ScoresArgs& a, int dtype, void* workspace, hipStream_t stream);
+size_t scores_workspace_bytes(int64_t rows, int64_t cols, int64_t top, int dtype);
+hipError_t launch_scores_gradient(const ScoresArgs& a, int dtype, hipStream_t stream);
+
+// Many tensors go to a kernel by value, as many at a time as its arguments hold.
+constexpr int kMostTensors = 48, kMostValues = 64;
+
+struct NormArgs {
+  const void* data[kMostValues];
+  int64_t count[kMostValues];
+  int32_t first[kMostValues];   // the tensor's first block
+  int8_t dtype[kMostValues];
+  int32_t tensors, chunk;       // chunk: values of a block
+  double* sums;                 // a block's each
+};
+struct NormEnd {
+  const double* sums;
+  int64_t count;
+  double max_norm, scale;
+  float* norm;                  // or null
+  float* factor;                // or null
+};
+int32_t norm_chunk(int64_t values);
+hipError_t launch_norm_sums(const NormArgs& a, int64_t blocks, hipStream_t stream);
+hipError_t launch_norm_end(const NormEnd& a, hipStream_t stream);
+
+struct AdamwTensor {
+  void* param;
+  const void* grad;
+  void* copy;              // or null
+  void* m;
+  void* v;
+  float* scales;           // of 8-bit states
+  int64_t count;
+  float decay;             // weight_decay; times lr where that is on the host
+  int8_t param_dtype, grad_dtype, copy_dtype;
+};
+struct AdamwArgs {
+  AdamwTensor tensor[kMostTensors];
+  int32_t first[kMostTensors];   // the tensor's first block
+  int32_t tensors, chunk;        // chunk: values of a block, a multiple of 4,096
+  float beta1, rest1, beta2, rest2, eps;   // rest = 1 - beta
+  float rate;                    // lr / (1 - beta1^step)
+  float spread;                  // 1 / sqrt(1 - beta2^step)
+  // Where lr or step are on the device, these three are computed there.
+  double lr, log_beta1, log_beta2;
+  int64_t step;
+  const float* lr_at;
+  const int64_t* step_at;
+  const float* factor;
+};
+int32_t adamw_chunk(int64_t values);
+hipError_t launch_adamw(const AdamwArgs& a, int64_t blocks, int state_bits, hipStream_t stream);
+
+struct StateArgs {
+  const void* m[kMostTensors];
+  const void* v[kMostTensors];
+  const float* scales[kMostTensors];
+  void* m_values[kMostTensors];
+  void* v_values[kMostTensors];
+  int64_t count[kMostTensors];
+  int32_t first[kMostTensors];
+  int8_t dtype[kMostTensors];
+  int32_t tensors, chunk;
+};
+hipError_t launch_state_values(const StateArgs& a, int64_t blocks, hipStream_t stream);
+
 }  // namespace pgc

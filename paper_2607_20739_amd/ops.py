@@ -1,10 +1,13 @@
-"""Operators that turn a language model's outputs into a partition's loss and gradient.
+"""Operators that turn a language model's outputs into a partition's loss and gradient, and a gradient
+into the next parameters.
 
 Binding of include/pgc_ops.h (through binding/pgc_ops_torch.cpp), which states what each operator computes: dropout with a mask
 that is a function of seed, row number and column; log-probabilities of given tokens; the
-preference loss of pairs of sequences; the clipped policy loss with a KL term.  The losses take
+preference loss of pairs of sequences; the clipped policy loss with a KL term; the scores of tokens
+(log-probabilities, entropies, most probable tokens); the norm of many gradients; an AdamW step over
+many tensors with states in 32 bits or 8.  The losses take
 logits and return the loss and the logits' gradient; `logits.backward(dlogits)` carries it on
-through a model, and a backward pass through the loss itself raises.  dropout and token_logprobs take part in autograd where an input asks for it (backward;
+through a model, and a backward pass through the loss itself raises.  dropout, token_logprobs and token_scores take part in autograd where an input asks for it (backward;
 forward-mode derivatives are refused, and so are traces by torch.jit.trace and make_fx).
 
 `out` must not ask for a gradient itself, unless it is the logits and a model's output.
@@ -51,6 +54,34 @@ class pgc_policy_args(ctypes.Structure):
                 ("loss", _P), ("logprobs", _P), ("dlogits", _P), ("dlogits_stride", _I64)]
 
 
+class pgc_scores_args(ctypes.Structure):
+    _fields_ = [("targets", _P), ("top", _I64), ("logprobs", _P), ("entropy", _P), ("stats", _P), ("top_logprobs", _P),
+                ("top_tokens", _P)]
+
+
+class pgc_scores_grad_args(ctypes.Structure):
+    _fields_ = [("targets", _P), ("stats", _P), ("entropy", _P), ("grad_logprobs", _P), ("grad_entropy", _P),
+                ("dlogits", _P), ("dlogits_stride", _I64)]
+
+
+class pgc_values(ctypes.Structure):
+    _fields_ = [("data", _P), ("count", _I64), ("dtype", _I32)]
+
+
+class pgc_adamw_tensor(ctypes.Structure):
+    _fields_ = [("param", _P), ("grad", _P), ("copy", _P), ("m", _P), ("v", _P), ("scales", _P), ("count", _I64),
+                ("weight_decay", _F64), ("param_dtype", _I32), ("grad_dtype", _I32), ("copy_dtype", _I32)]
+
+
+class pgc_adamw_args(ctypes.Structure):
+    _fields_ = [("lr", _F64), ("beta1", _F64), ("beta2", _F64), ("eps", _F64), ("step", _I64), ("lr_at", _P), ("step_at", _P),
+                ("factor", _P), ("state_bits", _I32)]
+
+
+class pgc_adamw_state(ctypes.Structure):
+    _fields_ = [("m", _P), ("v", _P), ("scales", _P), ("m_values", _P), ("v_values", _P), ("count", _I64), ("dtype", _I32)]
+
+
 _SIGNATURES = {
     "pgc_ops_last_error": (ctypes.c_char_p, []),
     "pgc_dropout": (ctypes.c_int, [ctypes.POINTER(pgc_dropout_args), _P]),
@@ -61,6 +92,13 @@ _SIGNATURES = {
     "pgc_preference_loss": (ctypes.c_int, [ctypes.POINTER(pgc_logits), ctypes.POINTER(pgc_preference_args),
                                            _P, _SIZE, _P]),
     "pgc_policy_loss": (ctypes.c_int, [ctypes.POINTER(pgc_logits), ctypes.POINTER(pgc_policy_args), _P]),
+    "pgc_token_scores_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(pgc_logits), _I64, ctypes.POINTER(_SIZE)]),
+    "pgc_token_scores": (ctypes.c_int, [ctypes.POINTER(pgc_logits), ctypes.POINTER(pgc_scores_args), _P, _SIZE, _P]),
+    "pgc_token_scores_backward": (ctypes.c_int, [ctypes.POINTER(pgc_logits), ctypes.POINTER(pgc_scores_grad_args), _P]),
+    "pgc_grad_norm_workspace_bytes": (ctypes.c_int, [ctypes.POINTER(pgc_values), _I64, ctypes.POINTER(_SIZE)]),
+    "pgc_grad_norm": (ctypes.c_int, [ctypes.POINTER(pgc_values), _I64, _F64, _F64, _P, _P, _P, _SIZE, _P]),
+    "pgc_adamw": (ctypes.c_int, [ctypes.POINTER(pgc_adamw_tensor), _I64, ctypes.POINTER(pgc_adamw_args), _P]),
+    "pgc_adamw_state_values": (ctypes.c_int, [ctypes.POINTER(pgc_adamw_state), _I64, _P]),
 }
 
 _DTYPES = {torch.float32: PGC_F32, torch.bfloat16: PGC_BF16, torch.float16: PGC_F16}
@@ -96,7 +134,7 @@ class _Native:
             raise RuntimeError("the compiled binding of the operators is not built (%s); run "
                                "`python -m paper_2607_20739_amd.build`" % e) from e
         for f in ("dropout", "dropout_backward", "token_logprobs", "token_logprobs_backward", "preference_loss",
-                  "policy_loss"):
+                  "policy_loss", "token_scores", "token_scores_backward", "grad_norm", "adamw", "adamw_state_values"):
             setattr(self, f, getattr(_ops_torch, f))
         return self.__dict__[name]
 
@@ -141,6 +179,75 @@ def token_logprobs(logits, targets):
 def token_logprobs_backward(logits, targets, stats, grad, out=None):
     """Gradient of the logits from the gradient of the log-probabilities.  `out` may be the logits."""
     return _native.token_logprobs_backward(logits, targets, stats, grad, out)
+
+
+# ---- scores of tokens -------------------------------------------------------------------------
+
+def token_scores(logits, targets=None, top=0):
+    """(logprobs [rows], entropy [rows], top_logprobs [rows, top], top_tokens [rows, top], stats [rows, 2]).
+
+    Each row's log-probability of its target, the entropy of its softmax and its `top` (up to 64) most
+    probable tokens, the most probable first, of equal ones the lower.  Without targets logprobs is None
+    and every row is scored; with them, rows without a token get zeros, and -1 for top_tokens.  Places
+    that are left where fewer than `top` tokens can occur hold -1 and -inf.  logprobs and entropy take
+    part in autograd, the others carry no gradient.  stats are those of token_logprobs.
+    """
+    if torch.is_grad_enabled() and getattr(logits, "requires_grad", False):
+        return _TokenScores.apply(logits, targets, top)
+    return _native.token_scores(logits, targets, top)
+
+
+def token_scores_backward(logits, targets, stats, entropy, grad_logprobs=None, grad_entropy=None, out=None):
+    """Gradient of the logits from those of token_scores' logprobs and entropy, one of which may be None.
+    `out` may be the logits."""
+    return _native.token_scores_backward(logits, targets, stats, entropy, grad_logprobs, grad_entropy, out)
+
+
+# ---- from a gradient to the next parameters -----------------------------------------------------
+
+def grad_norm(grads, max_norm=float("inf"), scale=1.0):
+    """(norm [1], factor [1]): the norm of all gradients times `scale`, and what adamw has to multiply them
+    by for a norm of at most max_norm: scale * min(1, max_norm / norm).
+
+    Use the inverse of a loss's scale for `scale`.  factor is NaN where a gradient is not finite.
+    """
+    return _native.grad_norm(grads, max_norm, scale)
+
+
+def adamw_states(params, bits=32):
+    """(moments, variances, scales): zeros for adamw, in 32 bits (scales None) or in 8."""
+    if bits not in (8, 32):
+        raise ValueError("bits must be 32 or 8")
+    dtype = torch.float32 if bits == 32 else torch.uint8
+    moments, variances = ([torch.zeros_like(p, dtype=dtype, requires_grad=False) for p in params] for _ in range(2))
+    if bits == 32:
+        return moments, variances, None
+    return moments, variances, [torch.zeros((p.numel() + 255) // 256, 2, device=p.device) for p in params]
+
+
+def adamw(params, grads, moments, variances, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, scales=None,
+          copies=None, factor=None):
+    """One AdamW step, in place, over lists of tensors (float32, bfloat16 or float16) of one GPU.
+
+    moments, variances and scales: as adamw_states made them; with scales the states have 8 bits.  step: this
+    step's number, from 1 on; step and lr may be GPU tensors of one int64 and one float32, which a captured
+    graph reads anew.  weight_decay: a number, or one for each tensor.  copies: 16-bit tensors, say, that
+    receive the new parameters.  factor: a float32 GPU tensor that the gradients are multiplied by, as
+    grad_norm returns it; where it is not finite, nothing changes.  Tensors may have gaps nowhere, and
+    those that belong together have the same strides.  Parameters may ask for a gradient; the step is
+    not part of a graph.
+    """
+    beta1, beta2 = betas
+    _native.adamw(params, grads, moments, variances, step, lr, beta1, beta2, eps, weight_decay, scales, copies, factor)
+
+
+def adamw_state_values(moments, variances, scales, dtype=torch.float32, out=None):
+    """(moments, variances): states in 8 bits as the numbers that they stand for, which float32 and bfloat16 hold
+    exactly.  out: a pair of lists that receive them."""
+    if out is None:
+        out = tuple([torch.empty_like(t, dtype=dtype) for t in some] for some in (moments, variances))
+    _native.adamw_state_values(moments, variances, scales, *out)
+    return out
 
 
 # ---- losses ---------------------------------------------------------------------------------
@@ -237,6 +344,39 @@ class _TokenLogprobsGradient(torch.autograd.Function):
     @staticmethod
     def backward(ctx, _):
         raise RuntimeError("the gradient of token_logprobs is not differentiable")
+
+
+class _TokenScores(torch.autograd.Function):
+    """Of the results only the log-probabilities and the entropy carry a gradient."""
+
+    @staticmethod
+    def forward(ctx, logits, targets, top):
+        results = _native.token_scores(logits, targets, top)
+        _, entropy, top_logprobs, top_tokens, stats = results
+        ctx.save_for_backward(logits, targets, stats, entropy)
+        ctx.mark_non_differentiable(top_logprobs, top_tokens, stats)
+        ctx.set_materialize_grads(False)
+        return results
+
+    @staticmethod
+    def backward(ctx, grad_logprobs, grad_entropy, *_):
+        if grad_logprobs is None and grad_entropy is None:
+            return None, None, None
+        logits, targets, stats, entropy = ctx.saved_tensors
+        grads = [g if g is None else g.contiguous() for g in (grad_logprobs, grad_entropy)]
+        return _TokenScoresGradient.apply(logits, targets, stats, entropy, *grads), None, None
+
+
+class _TokenScoresGradient(torch.autograd.Function):
+    """A gradient that has none itself: a graph of it can be made, but not gone back through."""
+
+    @staticmethod
+    def forward(ctx, logits, targets, stats, entropy, grad_logprobs, grad_entropy):
+        return token_scores_backward(logits, targets, stats, entropy, grad_logprobs, grad_entropy)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("the gradient of token_scores is not differentiable")
 
 
 class _LossWithoutGraph(torch.autograd.Function):
