@@ -1,5 +1,5 @@
-// Token log-probabilities, their gradient, the policy loss and the preference loss
-// (include/pgc_ops.h), for gfx950.
+// Token log-probabilities, their gradient and that of the scores, the policy loss and the preference
+// loss (include/pgc_ops.h), for gfx950.
 //
 // All of it is one exponential and a handful of additions per logit, so memory bounds it: a row
 // should come in once and its gradient leave once, with enough loads in flight throughout.  Sums of
@@ -145,6 +145,33 @@ struct RowGradient {
     return target ? v + g : v;
   }
   // Gradient of a vector, as if the target were in none.
+  __device__ __forceinline__ u4v of_vector(u4v z) const {
+    constexpr uint32_t kN = Vec<T>::kN;
+    if (none) return u4v{0, 0, 0, 0};
+    auto f = Vec<T>::floats(z);
+#pragma unroll
+    for (uint32_t k = 0; k < kN; ++k) f[k] = of(f[k], false);
+    return Vec<T>::packed(f);
+  }
+};
+
+// The gradient of the scores: g (onehot(y) - p) - e p (ln p + H), from the row's stats and entropy H.  With d = z - top the
+// factor of p is a + b d, b = -e and a = -g - e (H - ln sum).
+// p is taken 2^8 times larger and the factor as much smaller, so that factors of up to 2^8 lose nothing that 32 bits hold.
+template <class T>
+struct ScoresGradient {
+  float g, a, b, top, log2_inverse;
+  bool none;   // zeros, as above
+
+  __device__ __forceinline__ ScoresGradient(float g_, float e, float top_, float log_sum, float entropy)
+      : g(g_), a((e == 0.f ? -g_ : -g_ - e * (entropy - log_sum)) * 0x1p-8f), b(-e * 0x1p-8f), top(top_), log2_inverse(8.f - log_sum * kLog2E),
+        none((g_ == 0.f && e == 0.f) || (top_ == -INFINITY && log_sum == 0.f)) {}
+
+  __device__ __forceinline__ float of(float z, bool target) const {
+    const float d = z - top, p = exp2_fast(__builtin_fmaf(d, kLog2E, log2_inverse));
+    const float v = p * __builtin_fmaf(b, fmaxf(d, -200.f), a);   // at -inf, where p is 0, the factor has to be finite
+    return target ? v + g : v;
+  }
   __device__ __forceinline__ u4v of_vector(u4v z) const {
     constexpr uint32_t kN = Vec<T>::kN;
     if (none) return u4v{0, 0, 0, 0};
@@ -334,10 +361,24 @@ __device__ __forceinline__ int64_t offsets_up_to(const PairArgs& a, int64_t row)
 // Where the gradient kernels take a row's factor from: memory, or the row's pair.  A wave calls with
 // the rows [first, end) that its lanes have, and each lane's own.
 struct GivenFactors {
-  static constexpr bool kPairs = false;
+  static constexpr bool kPairs = false, kScores = false;
+};
+// Of the scores: those of the log-probability and of the entropy, either of which may be missing.  Without targets
+// every row counts.
+struct ScoresFactors {
+  static constexpr bool kPairs = false, kScores = true;
+  const float* grad_logprobs;
+  const float* grad_entropy;
+  const float* entropy;
+
+  template <class T>
+  __device__ __forceinline__ ScoresGradient<T> gradient(const LogitsArgs& a, int64_t row, bool counts) const {
+    const float g = counts && grad_logprobs ? grad_logprobs[row] : 0.f, e = counts && grad_entropy ? grad_entropy[row] : 0.f;
+    return ScoresGradient<T>(g, e, a.stats[2 * row], a.stats[2 * row + 1], e == 0.f ? 0.f : entropy[row]);
+  }
 };
 struct PairFactors {
-  static constexpr bool kPairs = true;
+  static constexpr bool kPairs = true, kScores = false;
   PairArgs p;
 
   __device__ __forceinline__ float operator()(int64_t first, int64_t end, int64_t row) const {
@@ -365,33 +406,19 @@ struct PairFactors {
 };
 
 int64_t pairs_of(const GivenFactors&) { return 0; }
+int64_t pairs_of(const ScoresFactors&) { return 0; }
 int64_t pairs_of(const PairFactors& f) { return f.p.pairs; }
 
-// A short row as one of LANES lanes sees it: its vectors are lane, lane + LANES, ..., HOLD of them.
-// The row's last vector ends with the row and may overlap the one before it (both have the same
-// gradient; in the sums only one counts the values that both hold).
+// ... with what becomes of the vectors.
 template <class T, int LANES, int HOLD>
-struct ShortRow {
-  static constexpr uint32_t kN = Vec<T>::kN;
-  uint32_t lane, cols, vectors, overlap;
+struct ShortRow : ShortVectors<T, LANES, HOLD> {
+  using ShortVectors<T, LANES, HOLD>::ShortVectors;
+  using ShortVectors<T, LANES, HOLD>::kN;
+  using ShortVectors<T, LANES, HOLD>::vectors;
+  using ShortVectors<T, LANES, HOLD>::overlap;
+  using ShortVectors<T, LANES, HOLD>::number;
+  using ShortVectors<T, LANES, HOLD>::skipped;
 
-  __device__ __forceinline__ explicit ShortRow(uint32_t cols_)
-      : lane(Place<LANES>::lane()), cols(cols_), vectors((cols_ + kN - 1) / kN), overlap(vectors * kN - cols_) {}
-  __device__ __forceinline__ uint32_t number(int i) const { return i * LANES + lane; }
-  // First column of vector v, and how many of its values others have.
-  __device__ __forceinline__ uint32_t start(uint32_t v) const { return v + 1 < vectors ? v * kN : cols - kN; }
-  __device__ __forceinline__ uint32_t skipped(uint32_t v) const { return v + 1 < vectors ? 0 : v < vectors ? overlap : kN; }
-
-  __device__ __forceinline__ void load(const T* z, u4v (&h)[HOLD]) const {
-    if (cols >= kN) {
-#pragma unroll
-      for (int i = 0; i < HOLD; ++i) h[i] = Vec<T>::template load<true>(z + start(number(i)), 0, 0);
-    } else {                // fewer values than a vector: at its end
-      T v[kN];
-      for (uint32_t k = 0; k < kN; ++k) v[k] = z[k < overlap ? 0 : k - overlap];
-      __builtin_memcpy(&h[0], v, sizeof(v));
-    }
-  }
   __device__ __forceinline__ Stat stat(const u4v (&h)[HOLD]) const {
     Stat s{-INFINITY, 0.f};
 #pragma unroll
@@ -407,7 +434,8 @@ struct ShortRow {
     return join_lanes<LANES>(s);
   }
   // The gradient of a row of fewer values than a vector.
-  __device__ __forceinline__ void store_few(T* dz, const RowGradient<T>& grad, u4v z, uint32_t y, float target_logit) const {
+  template <class Gradient>
+  __device__ __forceinline__ void store_few(T* dz, const Gradient& grad, u4v z, uint32_t y, float target_logit) const {
     T v[kN];
     const u4v d = grad.of_vector(z);
     __builtin_memcpy(v, &d, sizeof(v));
@@ -419,6 +447,69 @@ struct ShortRow {
 // How many waves have a row of `rows` short ones.
 template <int LANES>
 __host__ __device__ __forceinline__ int64_t short_row_waves(int64_t rows) { return (rows + kWave / LANES - 1) / (kWave / LANES); }
+
+// A short row's gradient, from the registers to memory: through LDS, to as many lanes as the wave's rows have vectors.
+template <class T, int LANES, int HOLD>
+__device__ __forceinline__ void store_turned(const LogitsArgs& a, const ShortRow<T, LANES, HOLD>& at, const u4v* mine, int64_t first) {
+  constexpr uint32_t kRows = kWave / LANES;
+  const uint32_t vectors = at.vectors;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // lanes of one wave: LDS keeps their order
+  __builtin_amdgcn_wave_barrier();
+  const uint32_t inverse = 65536 / vectors + 1;   // n / vectors = n * inverse >> 16 for n up to 256, vectors up to 128
+#pragma unroll
+  for (int i = 0; i < HOLD; ++i) {
+    const uint32_t n = i * kWave + threadIdx.x % kWave, r = n * inverse >> 16, v = n - r * vectors;
+    if (r < kRows && first + r < a.rows) Vec<T>::store(static_cast<T*>(a.dlogits) + (first + r) * a.out_stride + at.start(v), 0, 0, mine[n]);
+  }
+}
+
+// The scores' gradient of a short row, by all lanes of a wave at once.
+template <class T, int LANES, int HOLD>
+__device__ __forceinline__ void store_short_scores(const LogitsArgs& a, const ScoresFactors& factors, const ShortRow<T, LANES, HOLD>& at,
+                                                   u4v* turned, int64_t row, int64_t first, bool there, int32_t y) {
+  constexpr uint32_t kN = Vec<T>::kN;
+  const bool has_target = y >= 0 && y < a.cols;
+  if (HOLD == 1 && !there) return;
+  const T* z = static_cast<const T*>(a.logits) + row * a.stride;
+  T* dz = static_cast<T*>(a.dlogits) + row * a.out_stride;
+  u4v h[HOLD] = {};
+  float target_logit = 0.f;
+  ScoresGradient<T> grad(0.f, 0.f, 0.f, 0.f, 0.f);
+  if (there) grad = factors.gradient<T>(a, row, a.targets == nullptr || has_target);
+  if (!grad.none) {
+    at.load(z, h);
+    if (has_target) target_logit = Vec<T>::value(Vec<T>::raw(z + y));
+  }
+  const uint32_t yv = static_cast<uint32_t>(y);
+  const bool to_target = !grad.none && has_target;
+  if (at.cols < kN) {
+    if (!there) return;
+    T v[kN];
+    const u4v d = grad.of_vector(h[0]);
+    __builtin_memcpy(v, &d, sizeof(v));
+    for (uint32_t k = at.overlap; k < kN; ++k) dz[k - at.overlap] = v[k];
+    if (to_target) dz[yv] = static_cast<T>(grad.of(target_logit, true));
+    return;
+  }
+  if constexpr (HOLD == 1) {
+    Vec<T>::store(dz, 0, 0, grad.of_vector(h[0]));
+    if (to_target) dz[yv] = static_cast<T>(grad.of(target_logit, true));   // after its vector, by the same lane
+  } else {
+    u4v* mine = turned + threadIdx.x / kWave * (kWave * HOLD);          // the wave's rows, one after the other
+    u4v* line = mine + threadIdx.x % kWave / LANES * at.vectors;
+#pragma unroll
+    for (int i = 0; i < HOLD; ++i) {
+      const uint32_t v = at.number(i);
+      if (v >= at.vectors) continue;
+      line[v] = grad.of_vector(h[i]);
+      if (to_target && yv - at.start(v) < kN) {
+        const T d = static_cast<T>(grad.of(target_logit, true));
+        __builtin_memcpy(reinterpret_cast<char*>(line + v) + (yv - at.start(v)) * sizeof(T), &d, sizeof(T));
+      }
+    }
+    store_turned<T, LANES, HOLD>(a, at, mine, first);
+  }
+}
 
 // All modes for short rows, 64 / LANES of them to a wave.  What bounds them is the number of
 // instructions: few lanes per row, each with several vectors, spare the joins and the row's own
@@ -446,12 +537,16 @@ void short_row_kernel(LogitsArgs a, Factors factors) {
   const bool there = row < a.rows;
   if (!kTurn && !Factors::kPairs && !there) return;
   const T* z = static_cast<const T*>(a.logits) + row * a.stride;
-  const int32_t y = there ? a.targets[row] : -1;
+  const int32_t y = there && (!Factors::kScores || a.targets) ? a.targets[row] : -1;
   u4v h[HOLD];
   uint32_t target = 0;
   float lp = 0.f, loss = 0.f, g = 0.f, log_sum = 0.f;
   Stat s{-INFINITY, 0.f};
   bool counts = y >= 0 && y < a.cols;
+  if constexpr (Factors::kScores) {
+    store_short_scores<T, LANES, HOLD>(a, factors, at, turned, row, first, there, y);
+    return;
+  }
   PolicyRow pr{};
   if constexpr (kPolicy) {
     if (there) pr = policy_row(a, row);
@@ -514,14 +609,7 @@ void short_row_kernel(LogitsArgs a, Factors factors) {
         __builtin_memcpy(reinterpret_cast<char*>(line + v) + (yv - at.start(v)) * sizeof(T), &d, sizeof(T));
       }
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // lanes of one wave: LDS keeps their order
-    __builtin_amdgcn_wave_barrier();
-    const uint32_t inverse = 65536 / vectors + 1;   // n / vectors = n * inverse >> 16 for n up to 256, vectors up to 128
-#pragma unroll
-    for (int i = 0; i < HOLD; ++i) {
-      const uint32_t n = i * kWave + threadIdx.x % kWave, r = n * inverse >> 16, v = n - r * vectors;
-      if (r < kRows && first + r < a.rows) Vec<T>::store(static_cast<T*>(a.dlogits) + (first + r) * a.out_stride + at.start(v), 0, 0, mine[n]);
-    }
+    store_turned<T, LANES, HOLD>(a, at, mine, first);
   }
 }
 
@@ -820,7 +908,7 @@ void gradient_kernel(LogitsArgs a, Factors factors) {
   const uint32_t head = static_cast<uint32_t>(-reinterpret_cast<uintptr_t>(z) % kLine / sizeof(T));
   const uint32_t lane = Place<LANES>::lane(), cols = static_cast<uint32_t>(a.cols);
   const uint32_t full = (cols - head) / kN, rem = cols - head - full * kN, v0 = blockIdx.x * (LANES * U);
-  const int32_t y = a.targets[row];
+  const int32_t y = !Factors::kScores || a.targets ? a.targets[row] : -1;
   const bool has_token = y >= 0 && y < a.cols;
   u4v h[U];
   auto load = [&] {
@@ -846,11 +934,17 @@ void gradient_kernel(LogitsArgs a, Factors factors) {
         g = factor;
       }
     }
-  } else {
+  } else if constexpr (!Factors::kScores) {
     g = a.grad[row];
   }
-  const float top = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
-  const RowGradient<T> grad = RowGradient<T>::of_stats(has_token ? g : 0.f, top, log_sum);
+  const auto grad = [&] {
+    if constexpr (Factors::kScores) {
+      return factors.template gradient<T>(a, row, a.targets == nullptr || has_token);
+    } else {
+      const float top = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
+      return RowGradient<T>::of_stats(has_token ? g : 0.f, top, log_sum);
+    }
+  }();
   // Columns outside of the vectors: up to kN - 1 at the end, less than a cache line at the start.
   const uint32_t yv = static_cast<uint32_t>(y), last = cols - rem + lane;
   const bool has_tail = blockIdx.x == gridDim.x - 1 && lane < rem, has_head = blockIdx.x == 0 && lane < head;
@@ -862,7 +956,7 @@ void gradient_kernel(LogitsArgs a, Factors factors) {
     if (has_head) dz[lane] = static_cast<T>(0.f);
     return;
   }
-  const uint32_t target = (yv - head) / kN - v0;   // the target's vector, and whether this lane has it
+  const uint32_t target = (yv - head) / kN - v0;   // the target's vector, and whether this lane has it (without a target, past the last)
   const bool has_target = target < LANES * U && target + v0 < full && target % LANES == lane;
   uint32_t z_target = 0, z_tail = 0, z_head = 0;
   if constexpr (!Factors::kPairs) load();
@@ -1259,6 +1353,24 @@ hipError_t launch_pair_gradient(const LogitsArgs& a, const PairArgs& p, int dtyp
     case PGC_F32: return launch_backward<float>(a, stream, PairFactors{p});
     case PGC_BF16: return launch_backward<__bf16>(a, stream, PairFactors{p});
     default: return launch_backward<_Float16>(a, stream, PairFactors{p});
+  }
+}
+
+hipError_t launch_scores_gradient(const ScoresArgs& s, int dtype, hipStream_t stream) {
+  LogitsArgs a{};
+  a.logits = s.logits;
+  a.targets = s.targets;
+  a.rows = s.rows;
+  a.cols = s.cols;
+  a.stride = s.stride;
+  a.out_stride = s.out_stride;
+  a.dlogits = s.dlogits;
+  a.stats = s.stats;
+  const ScoresFactors factors{s.grad_logprobs, s.grad_entropy, s.entropy};
+  switch (dtype) {
+    case PGC_F32: return launch_backward<float>(a, stream, factors);
+    case PGC_BF16: return launch_backward<__bf16>(a, stream, factors);
+    default: return launch_backward<_Float16>(a, stream, factors);
   }
 }
 

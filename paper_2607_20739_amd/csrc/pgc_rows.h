@@ -107,6 +107,33 @@ struct Place {
 // Grids of up to 2^31 blocks (of one dimension, HIP takes fewer threads than that needs).
 constexpr int64_t kGridX = 1 << 20, kGridYZ = 65535;
 
+// A short row as one of LANES lanes sees it: its vectors are lane, lane + LANES, ..., HOLD of them.
+// The row's last vector ends with the row and may overlap the one before it (both have the same
+// gradient; in the sums only one counts the values that both hold).
+template <class T, int LANES, int HOLD>
+struct ShortVectors {
+  static constexpr uint32_t kN = Vec<T>::kN;
+  uint32_t lane, cols, vectors, overlap;
+
+  __device__ __forceinline__ explicit ShortVectors(uint32_t cols_)
+      : lane(Place<LANES>::lane()), cols(cols_), vectors((cols_ + kN - 1) / kN), overlap(vectors * kN - cols_) {}
+  __device__ __forceinline__ uint32_t number(int i) const { return i * LANES + lane; }
+  // First column of vector v, and how many of its values others have.
+  __device__ __forceinline__ uint32_t start(uint32_t v) const { return v + 1 < vectors ? v * kN : cols - kN; }
+  __device__ __forceinline__ uint32_t skipped(uint32_t v) const { return v + 1 < vectors ? 0 : v < vectors ? overlap : kN; }
+
+  __device__ __forceinline__ void load(const T* z, u4v (&h)[HOLD]) const {
+    if (cols >= kN) {
+#pragma unroll
+      for (int i = 0; i < HOLD; ++i) h[i] = Vec<T>::template load<true>(z + start(number(i)), 0, 0);
+    } else {                // fewer values than a vector: at its end
+      T v[kN];
+      for (uint32_t k = 0; k < kN; ++k) v[k] = z[k < overlap ? 0 : k - overlap];
+      __builtin_memcpy(&h[0], v, sizeof(v));
+    }
+  }
+};
+
 // The whole vectors of a long row.  The values left over, 1 to kN of them, go to a lane each, so that
 // the vectors of a shifted row, too, end within it.
 template <class T>

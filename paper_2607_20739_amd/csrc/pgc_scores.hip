@@ -1,129 +1,646 @@
-// Scores of tokens under rows of logits and their gradient (include/pgc_ops.h), for gfx950.
+// Scores of tokens under rows of logits (include/pgc_ops.h), for gfx950: the given token's log-probability, the
+// row's entropy and its most probable tokens in one pass over the row.
+//
+// Beside the sum S of 2^t, t = z log2 e - K, runs W, that of 2^t t.  With t_M the maximum's t they give
+// ln S' = ln 2 (log2 S - t_M) and the entropy ln S' - ln 2 (W / S - t_M).  K is a whole number near the maximum so far, the
+// same for a wave, so that t takes one fused operation without losing digits, and moving from one K to another only
+// scales by a power of two.  Nine to ten instructions per logit, one of them an exponential of four times the cost: memory
+// is the bound on many rows, but not by far, and a single row is bound by its CUs.
+//
+// The top tokens cost no sorting of the row.  A lane keeps the largest of each group of its values.  The
+// `top`-th largest of 64 maxima of equally many values each is a bound that at least `top` values reach, and in a row
+// of no special order few more: one wave looks through the groups that reach it again, and ranks what reaches it
+// by value and column, which no two share.  Where too many do (equal logits, or sorted ones), that wave goes through
+// the row with a list that is cut to the best ones whenever it is full.
+//
+// As for the log-probabilities, rows of up to 64 vectors of 16 bytes belong to 1 to 16 lanes, longer ones to 1 to 16
+// waves, by the number of columns alone; so a row's bits do not depend on where it lies.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 
 #include "pgc_ops_kernels.h"
+#include "pgc_rows.h"
 
 #pragma clang fp contract(off)
 
 namespace pgc {
 namespace {
 
-constexpr int kThreads = 256;
+// ---- over a wave ------------------------------------------------------------------------------
 
-// A logit and its column: the larger comes first, of equal ones the lower column.
-struct Entry {
-  float value;
-  uint32_t column;
-  __device__ __forceinline__ bool before(const Entry& o) const { return value > o.value || (value == o.value && column < o.column); }
+// Joined over all lanes, in all of them: within rows of 16 lanes as elsewhere, then rows and halves by lane swaps, which
+// spare the way through LDS.
+template <class Join>
+__device__ __forceinline__ float wave_join(float v, Join join) {
+  v = join(v, dpp_move<kDppSwap1>(v));
+  v = join(v, dpp_move<kDppSwap2>(v));
+  v = join(v, dpp_move<kDppHalfMirror>(v));
+  v = join(v, dpp_move<kDppMirror>(v));
+  const auto rows = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = join(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
+  const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return join(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+}
+__device__ __forceinline__ float wave_sum(float v) { return wave_join(v, [](float x, float y) { return x + y; }); }
+__device__ __forceinline__ float wave_max(float v) { return wave_join(v, [](float x, float y) { return fmaxf(x, y); }); }
+
+// ---- sums -------------------------------------------------------------------------------------
+
+// The maximum of some of a row's values, the sum of e = exp(z - maximum) and that of e t.
+struct Sums {
+  float top, sum, moved;
 };
-constexpr uint32_t kNoColumn = 0xFFFFFFFFu;
 
-// Over the block's threads, in all of them.
-template <class V, class Join>
-__device__ __forceinline__ V block_join(V v, Join join) {
-  __shared__ V all[kThreads];
-  __syncthreads();
-  all[threadIdx.x] = v;
-  for (int d = kThreads / 2; d > 0; d /= 2) {
-    __syncthreads();
-    if (threadIdx.x < static_cast<uint32_t>(d)) all[threadIdx.x] = join(all[threadIdx.x], all[threadIdx.x + d]);
+// Exponents this far down give 0, and t must not be infinite beside it.
+constexpr float kFar = -200.f;
+
+// What a sum counts for once the maximum is `base`: its factor, and how far its values have moved.
+struct Shift {
+  float by, factor;
+  __device__ __forceinline__ Shift(float top, float base) : by(fmaxf((top - base) * kLog2E, kFar)), factor(exp2_fast(by)) {}
+  __device__ __forceinline__ float sum(const Sums& s) const { return s.sum * factor; }
+  __device__ __forceinline__ float moved(const Sums& s) const { return __builtin_fmaf(by, s.sum, s.moved) * factor; }
+};
+
+// A wave's sums over its part of a long row, with K (`shift`) the same in all lanes.
+struct WaveSums {
+  // Values may exceed the maximum that K was taken from by this much in t before it is taken anew: so many
+  // roundings of W / S the entropy loses.  Past the largest K would not be exact.
+  static constexpr float kAbove = 16.f, kLargest = 0x1p20f;
+  float shift = 0.f, limit = -INFINITY;   // limit: the largest value that needs no other K
+  float sum = 0.f, moved = 0.f, top = -INFINITY;   // of this lane
+
+  __device__ __forceinline__ float exponent(float v) const { return __builtin_fmaf(v, kLog2E, -shift); }
+
+  // Takes K from the wave's largest of `most`, the lanes' maxima of the values that come next; false where that is too large.
+  __device__ __forceinline__ bool take_shift(float most) {
+    const float peak = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(wave_max(most))));
+    if (peak == -INFINITY) return true;
+    if (!(fabsf(peak) < kLargest)) return false;
+    const float next = rintf(peak * kLog2E), by = limit == -INFINITY ? 0.f : fmaxf(shift - next, kFar), factor = exp2_fast(by);
+    moved = __builtin_fmaf(by, sum, moved) * factor;
+    sum *= factor;
+    shift = next;
+    limit = (next + kAbove) * kLn2;
+    return true;
   }
-  __syncthreads();
-  return all[0];
+  // Adds U vectors of each lane; returns the largest of the lane's values.
+  template <class T, int U>
+  __device__ __forceinline__ float add_at(const u4v (&h)[U]) {
+    constexpr int kN = Vec<T>::kN;
+    float most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      auto f = Vec<T>::floats(h[i]);
+#pragma unroll
+      for (int k = 0; k < kN; ++k) most = fmaxf(most, f[k]);
+#pragma unroll
+      for (int k = 0; k < kN; ++k) {
+        const float t = exponent(f[k]);
+        f[k] = exp2_fast(t);
+        moved = __builtin_fmaf(f[k], fmaxf(t, kFar), moved);
+      }
+#pragma unroll
+      for (int w = kN / 2; w >= 1; w /= 2)
+#pragma unroll
+        for (int k = 0; k < w; ++k) f[k] += f[k + w];
+      sum += f[0];
+    }
+    return most;
+  }
+  // The same with another K where that is needed; false where a value is too large.
+  template <class T, int U>
+  __device__ __forceinline__ bool add(u4v (&h)[U], float& most) {
+    while (true) {
+      const float sum_before = sum, moved_before = moved;
+#pragma unroll
+      for (int i = 0; i < U; ++i) asm("" : "+v"(h[i]));   // unpacked anew: else the values stay in registers for another time
+      most = add_at<T, U>(h);
+      if (__ballot(most > limit) == 0) break;
+      sum = sum_before;
+      moved = moved_before;
+      if (!take_shift(most)) return false;
+    }
+    top = fmaxf(top, most);
+    return true;
+  }
+  __device__ __forceinline__ bool add_value(float v) {
+    if (__ballot(v > limit) != 0 && !take_shift(v)) return false;
+    const float t = exponent(v), e = exp2_fast(t);
+    sum += e;
+    moved = __builtin_fmaf(e, fmaxf(t, kFar), moved);
+    top = fmaxf(top, v);
+    return true;
+  }
+  // Over the wave, with the maximum in K's place.
+  __device__ __forceinline__ Sums join() const {
+    const float peak = wave_max(top), s = wave_sum(sum), w = wave_sum(moved);
+    if (peak == -INFINITY) return {peak, s, w};
+    const float t = exponent(peak), factor = exp2_fast(-t);
+    return {peak, s * factor, __builtin_fmaf(-t, s, w) * factor};
+  }
+};
+
+// Joined over LANES lanes of a wave; every lane ends with the result.
+template <int LANES>
+__device__ __forceinline__ Sums join_lanes(Sums s) {
+  const float top = lane_group_max<LANES>(s.top);
+  const Shift shift(s.top, finite_top(top));
+  return {top, lane_group_sum<LANES>(shift.sum(s)), lane_group_sum<LANES>(shift.moved(s))};
 }
 
-// A block per row: the maximum, the sums, then the top tokens one by one.
-template <class T>
-__global__ __launch_bounds__(kThreads)
-void scores_kernel(ScoresArgs a) {
-  const int64_t row = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
-  if (row >= a.rows) return;
-  const int64_t y = a.targets ? a.targets[row] : 0;
-  const bool first = threadIdx.x == 0;
-  auto write = [&](float lp, float entropy, float top, float log_sum) {
-    if (!first) return;
-    if (a.targets) a.logprobs[row] = lp;
+// What becomes of a row's sums.
+struct RowScores {
+  float logprob = 0.f, entropy = 0.f, top = 0.f, log_sum = 0.f;
+  bool any = false;   // whether there are tokens to list: else these take the place of their log-probabilities
+  float instead = 0.f;
+
+  __device__ __forceinline__ RowScores() {}   // of a row that is not read
+  __device__ __forceinline__ RowScores(Sums s, float target_logit) {
+    if (s.top == -INFINITY && s.sum == 0.f) {
+      logprob = top = instead = -INFINITY;
+      return;
+    }
+    log_sum = kLn2 * log2f(s.sum);
+    any = log_sum == log_sum;
+    top = any ? s.top : log_sum;   // fmaxf leaves NaN out
+    instead = log_sum;
+    entropy = log_sum - kLn2 * (s.moved / s.sum);
+    logprob = (target_logit - top) - log_sum;
+  }
+  __device__ __forceinline__ void write(const ScoresArgs& a, int64_t row) const {
+    if (a.logprobs) a.logprobs[row] = logprob;
     if (a.entropy) a.entropy[row] = entropy;
     if (a.stats) {
       a.stats[2 * row] = top;
       a.stats[2 * row + 1] = log_sum;
     }
-  };
-  auto write_top = [&](int i, float lp, int32_t token) {
-    a.top_logprobs[row * a.top + i] = lp;
+  }
+  __device__ __forceinline__ void write_top(const ScoresArgs& a, int64_t row, int i, float value, int32_t token) const {
+    a.top_logprobs[row * a.top + i] = token >= 0 ? (value - top) - log_sum : any ? -INFINITY : instead;
     a.top_tokens[row * a.top + i] = token;
-  };
-  if (a.targets && (y < 0 || y >= a.cols)) {
-    write(0.f, 0.f, 0.f, 0.f);
-    for (int i = threadIdx.x; i < a.top; i += kThreads) write_top(i, 0.f, -1);
+  }
+};
+
+// Whether a row is read, and its target's column, or one that no value has.
+struct Target {
+  int32_t y;
+  bool counts;
+  __device__ __forceinline__ Target(const ScoresArgs& a, int64_t row) {
+    y = a.targets ? a.targets[row] : -1;
+    counts = a.targets == nullptr || (y >= 0 && y < a.cols);
+  }
+  // For the target's logit; of a row without one the first value stands in.
+  __device__ __forceinline__ uint32_t column() const { return y > 0 ? static_cast<uint32_t>(y) : 0; }
+};
+
+// ---- short rows -------------------------------------------------------------------------------
+
+template <int LANES>
+__device__ __forceinline__ uint32_t lane_group_min(uint32_t v) {
+  auto take = [&](int other) { v = std::min(v, static_cast<uint32_t>(other)); };
+  const auto bits = [&] { return static_cast<int>(v); };
+  if constexpr (LANES >= 2) take(__builtin_amdgcn_update_dpp(0, bits(), kDppSwap1, 0xF, 0xF, true));
+  if constexpr (LANES >= 4) take(__builtin_amdgcn_update_dpp(0, bits(), kDppSwap2, 0xF, 0xF, true));
+  if constexpr (LANES >= 8) take(__builtin_amdgcn_update_dpp(0, bits(), kDppHalfMirror, 0xF, 0xF, true));
+  if constexpr (LANES >= 16) take(__builtin_amdgcn_update_dpp(0, bits(), kDppMirror, 0xF, 0xF, true));
+  return v;
+}
+
+// 64 / LANES rows to a wave.  The row stays in registers; its top tokens are taken out one by one.
+template <class T, int LANES, int HOLD>
+__global__ __launch_bounds__(kBlock)
+void short_scores_kernel(ScoresArgs a) {
+  constexpr uint32_t kN = Vec<T>::kN;
+  constexpr int kValues = HOLD * kN;
+  const ShortVectors<T, LANES, HOLD> at(static_cast<uint32_t>(a.cols));
+  const int64_t row = Place<LANES>::row(static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x);
+  if (row >= a.rows) return;
+  const Target target(a, row);
+  if (!target.counts) {
+    if (at.lane == 0) RowScores().write(a, row);
+    for (int i = at.lane; i < a.top; i += LANES) RowScores().write_top(a, row, i, 0.f, -1);
     return;
   }
   const T* z = static_cast<const T*>(a.logits) + row * a.stride;
-  float top = -INFINITY, bad = 0.f;
-  for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) {
-    const float v = static_cast<float>(z[j]);
-    top = fmaxf(top, v);
-    if (!(v < INFINITY)) bad = 1.f;
+  u4v h[HOLD];
+  const uint32_t target_raw = Vec<T>::raw(z + target.column());
+  at.load(z, h);
+  float f[kValues];
+  float most = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < HOLD; ++i) {
+    const auto v = Vec<T>::floats(h[i]);
+    const uint32_t skip = (i + 1) * LANES >= at.vectors ? at.skipped(at.number(i)) : 0;
+#pragma unroll
+    for (uint32_t k = 0; k < kN; ++k) {
+      f[i * kN + k] = k < skip ? -INFINITY : v[k];
+      most = fmaxf(most, f[i * kN + k]);
+    }
   }
-  top = block_join(top, [](float x, float y) { return fmaxf(x, y); });
-  bad = block_join(bad, [](float x, float y) { return fmaxf(x, y); });
-  if (bad != 0.f || top == -INFINITY) {
-    if (bad != 0.f) write(NAN, NAN, NAN, NAN);
-    else write(-INFINITY, 0.f, -INFINITY, 0.f);
-    for (int i = threadIdx.x; i < a.top; i += kThreads) write_top(i, bad != 0.f ? NAN : -INFINITY, -1);
+  Sums s{lane_group_max<LANES>(most), 0.f, 0.f};
+  const float base = finite_top(s.top);
+#pragma unroll
+  for (int k = 0; k < kValues; ++k) {
+    const float t = (f[k] - base) * kLog2E, e = exp2_fast(t);
+    s.sum += e;
+    s.moved = __builtin_fmaf(e, fmaxf(t, kFar), s.moved);
+  }
+  s.sum = lane_group_sum<LANES>(s.sum);
+  s.moved = lane_group_sum<LANES>(s.moved);
+  const RowScores scores(s, Vec<T>::value(target_raw));
+  if (at.lane == 0) scores.write(a, row);
+  for (int i = 0; i < a.top; ++i) {
+    float best = most;
+    if (i > 0) {
+      best = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < kValues; ++k) best = fmaxf(best, f[k]);
+    }
+    best = lane_group_max<LANES>(best);
+    const bool there = scores.any && best > -INFINITY;
+    uint32_t mine = kValues;       // the first place of it in this lane
+#pragma unroll
+    for (int k = kValues - 1; k >= 0; --k) mine = f[k] == best ? k : mine;
+    const uint32_t column = mine < kValues ? at.start(at.number(mine / kN)) + mine % kN : 0xFFFFFFFFu;
+    const uint32_t first = lane_group_min<LANES>(column);
+    if (column != first) mine = kValues;
+#pragma unroll
+    for (int k = 0; k < kValues; ++k) f[k] = mine == static_cast<uint32_t>(k) ? -INFINITY : f[k];
+    if (at.lane == 0) scores.write_top(a, row, i, best, there ? static_cast<int32_t>(first) : -1);
+  }
+}
+
+// ---- long rows --------------------------------------------------------------------------------
+
+// A value and its column as one number: the larger value is the larger number, of equal ones the lower column.
+// No value's is 0.
+__device__ __forceinline__ uint32_t ordered(float v) {
+  const uint32_t bits = __float_as_uint(v + 0.f);   // -0 as 0
+  return bits ^ (bits >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu)); }
+__device__ __forceinline__ uint64_t key_of(float v, uint32_t column) {
+  return static_cast<uint64_t>(ordered(v)) << 32 | (0xFFFFFFFFu - column);
+}
+__device__ __forceinline__ float value_of(uint64_t key) { return unordered(static_cast<uint32_t>(key >> 32)); }
+__device__ __forceinline__ int32_t column_of(uint64_t key) { return static_cast<int32_t>(0xFFFFFFFFu - static_cast<uint32_t>(key)); }
+
+// A number that at least `top` of the wave's 64 lanes' values reach, near the largest such (its upper 16 bits are
+// searched); -inf where fewer lanes hold more.
+__device__ __forceinline__ float reached_by(float v, int top) {
+  const uint32_t o = ordered(v) >> 16;
+  uint32_t bound = 0;
+#pragma unroll
+  for (int b = 15; b >= 0; --b) {
+    const uint32_t next = bound | 1u << b;
+    if (__popcll(__ballot(o >= next)) >= top) bound = next;
+  }
+  return bound <= 0x7F ? -INFINITY : unordered(bound << 16);
+}
+
+__device__ __forceinline__ void wave_sync() {   // lanes of one wave: LDS keeps their order
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// What a row's waves share.
+template <int WAVES>
+struct RowShared {
+  static constexpr uint32_t kSlots = WAVES <= 4 ? 6 : 16, kThreads = WAVES * kWave;
+  static constexpr uint32_t kRoom = 512, kGroups = std::min(512u, kSlots * kThreads);
+  Sums parts[WAVES];
+  float lane_most[kWave];                 // the largest of the values of WAVES lanes each
+  alignas(16) float most[kSlots][kThreads];   // the largest of a thread's turn; the last slot's of all turns from there on
+  uint64_t list[kRoom];                   // candidates for the top tokens
+  uint32_t groups[kGroups];               // turns and threads whose values may hold some
+};
+
+// A long row as its WAVES waves see it.  In turn n the row's thread `tid` has the vectors n kTurn + (tid / 64) 64 U + tid % 64 + 64 i,
+// i = 0 .. U - 1.
+template <class T, int WAVES, int U>
+struct LongRow {
+  static constexpr uint32_t kN = Vec<T>::kN, kTurn = WAVES * kWave * U;
+  using Shared = RowShared<WAVES>;
+  const T* z;
+  uint32_t cols, full, rem, tid, turns;
+
+  __device__ __forceinline__ LongRow(const T* z_, uint32_t cols_, uint32_t tid_)
+      : z(z_), cols(cols_), full(long_row_vectors<T>(cols_)), rem(cols_ - full * kN), tid(tid_), turns((full + kTurn - 1) / kTurn) {}
+  __device__ __forceinline__ static uint32_t slot(uint32_t turn) { return std::min(turn, Shared::kSlots - 1); }
+  __device__ __forceinline__ static uint32_t vector(uint32_t turn, uint32_t thread, uint32_t i) {
+    return turn * kTurn + thread / kWave * (kWave * U) + i * kWave + thread % kWave;
+  }
+  // The values behind the vectors go to the row's first lanes.
+  __device__ __forceinline__ uint32_t tail_column() const { return full * kN + (tid < rem ? tid : rem - 1); }
+  __device__ __forceinline__ float tail() const {
+    const float v = Vec<T>::value(Vec<T>::raw(z + tail_column()));
+    return tid < rem ? v : -INFINITY;
+  }
+
+  // Passes the vectors of this wave's part to each(turn, vectors), until that returns false.
+  template <class Each>
+  __device__ __forceinline__ bool each_turn(Each each) const {
+    uint32_t turn = 0, v0 = __builtin_amdgcn_readfirstlane(tid / kWave) * (kWave * U);
+    if (v0 >= full) return true;
+    VectorRun<T> run(z, full, v0, kWave * U);
+    uint32_t before = run.before();
+    u4v next[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) next[i] = run.load(i);
+    for (bool more = true; more; ++turn) {
+      u4v h[U];
+      uint32_t carry = before << 16;
+#pragma unroll
+      for (int i = 0; i < U; ++i) h[i] = run.values(next[i], carry);
+      const VectorRun<T> now = run;
+      v0 += kTurn;
+      more = v0 < full;
+      if (more) {      // the next turn's vectors are on their way while these are added
+        run = VectorRun<T>(z, full, v0, kWave * U);
+        before = run.before();
+#pragma unroll
+        for (int i = 0; i < U; ++i) next[i] = run.load(i);
+      }
+      if (now.whole < U) {
+#pragma unroll
+        for (uint32_t i = 0; i < U; ++i)
+          if (!(i < now.whole || (i == now.whole && now.lane < now.part))) h[i] = Vec<T>::none();
+      }
+      if (!each(turn, h)) return false;
+    }
+    return true;
+  }
+  // The sums of this wave's part, in all its lanes; and the largest of this lane's values.
+  __device__ __forceinline__ Sums sums(Shared& shared, float& most) const {
+    const float tail_value = tail();
+    WaveSums s;
+    float last = -INFINITY;
+    const bool done = each_turn([&](uint32_t turn, u4v (&h)[U]) {
+      if (turn == 0) {   // the first K, by the first vectors
+        const auto f = Vec<T>::floats(h[0]);
+        float first = f[0];
+#pragma unroll
+        for (uint32_t k = 1; k < kN; ++k) first = fmaxf(first, f[k]);
+        if (!s.take_shift(first)) return false;
+      }
+      float here;
+      if (!s.template add<T, U>(h, here)) return false;
+      last = turn < Shared::kSlots ? here : fmaxf(last, here);
+      shared.most[slot(turn)][tid] = last;
+      return true;
+    });
+    if (!done || (tid < kWave && !s.add_value(tail_value))) return sums_of_large(shared, most, tail_value);
+    most = s.top;
+    return s.join();
+  }
+  // The same of values past 2^20, where a K near the maximum is no 32-bit number: the differences to the maximum
+  // themselves, in a second pass.
+  __device__ __forceinline__ Sums sums_of_large(Shared& shared, float& most, float tail_value) const {
+    float top = -INFINITY, last = -INFINITY;
+    each_turn([&](uint32_t turn, u4v (&h)[U]) {
+      float here = -INFINITY;
+      for (uint32_t i = 0; i < U; ++i) {
+        const auto f = Vec<T>::floats(h[i]);
+        for (uint32_t k = 0; k < kN; ++k) here = fmaxf(here, f[k]);
+      }
+      last = turn < Shared::kSlots ? here : fmaxf(last, here);
+      shared.most[slot(turn)][tid] = last;
+      top = fmaxf(top, here);
+      return true;
+    });
+    if (tid < kWave) top = fmaxf(top, tail_value);
+    most = top;
+    const float peak = wave_max(top);
+    float sum = 0.f, moved = 0.f;
+    auto add = [&](float v) {
+      const float t = (v - peak) * kLog2E, e = exp2_fast(t);
+      sum += e;
+      moved = __builtin_fmaf(e, fmaxf(t, kFar), moved);
+    };
+    each_turn([&](uint32_t, u4v (&h)[U]) {
+      for (uint32_t i = 0; i < U; ++i) {
+        const auto f = Vec<T>::floats(h[i]);
+        for (uint32_t k = 0; k < kN; ++k) add(f[k]);
+      }
+      return true;
+    });
+    if (tid < kWave) add(tail_value);
+    return {peak, wave_sum(sum), wave_sum(moved)};
+  }
+
+  // ---- the top tokens, by the row's first wave
+
+  // Passes the vectors of the groups' turns to look(there, vector's values, its first column), one to a lane.
+  template <class Look>
+  __device__ __forceinline__ void look_at(const Shared& shared, uint32_t n, Look look) const {
+    for (uint32_t j = 0; j < n * U; j += kWave) {
+      const uint32_t at = std::min(j + tid, n * U - 1), group = shared.groups[at / U];
+      const uint32_t v = vector(group / Shared::kThreads, group % Shared::kThreads, at % U);
+      const bool there = j + tid < n * U && v < full;
+      look(there, Vec<T>::floats(Vec<T>::template load<true>(z, std::min(v, full - 1), 0)), v * kN);
+    }
+  }
+  // Appends a candidate for each lane where `there`; returns how many there are then (those past the room are lost).
+  __device__ __forceinline__ static uint32_t append(Shared& shared, uint32_t n, bool there, uint64_t key) {
+    const uint64_t lanes = __ballot(there);
+    const uint32_t at = n + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(lanes >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(lanes), 0));
+    if (there && at < Shared::kRoom) shared.list[at] = key;
+    return n + __popcll(lanes);
+  }
+  // Sorts n candidates downwards.
+  __device__ __forceinline__ void sort(Shared& shared, uint32_t n) const {
+    uint32_t size = 2;
+    while (size < n) size *= 2;
+    for (uint32_t i = n + tid; i < size; i += kWave) shared.list[i] = 0;
+    wave_sync();
+    for (uint32_t run = 2; run <= size; run *= 2)
+      for (uint32_t step = run / 2; step > 0; step /= 2) {
+        for (uint32_t i = tid; i < size / 2; i += kWave) {
+          const uint32_t low = i / step * 2 * step + i % step, high = low + step;
+          const uint64_t a = shared.list[low], b = shared.list[high];
+          if ((a < b) == ((low & run) == 0)) {
+            shared.list[low] = b;
+            shared.list[high] = a;
+          }
+        }
+        wave_sync();
+      }
+  }
+
+  // What reaches `bound`, as candidates; more than the room where there are too many.
+  __device__ __forceinline__ uint32_t collect(Shared& shared, float bound) const {
+    uint32_t groups = 0;
+    auto add_group = [&](bool there, uint32_t group) {
+      const uint64_t lanes = __ballot(there);
+      if (lanes == 0) return;
+      const uint32_t at = groups + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(lanes >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(lanes), 0));
+      if (there && at < Shared::kGroups) shared.groups[at] = group;
+      groups += __popcll(lanes);
+    };
+    if constexpr (WAVES >= 4) {   // four threads' maxima to a lane
+      constexpr uint32_t kEach = 4, kStep = kEach * kWave;
+      typedef float f4v __attribute__((ext_vector_type(4)));
+      for (uint32_t j = 0; j < turns * (Shared::kThreads / kStep); ++j) {
+        const uint32_t turn = j / (Shared::kThreads / kStep), thread = j % (Shared::kThreads / kStep) * kStep + kEach * tid;
+        // (Threads without vectors in the last turn have written nothing.)
+        const bool there = vector(turn, thread & ~(kWave - 1), 0) < full;
+        const f4v m = *reinterpret_cast<const f4v*>(&shared.most[slot(turn)][thread]);
+        if (__ballot(there && fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) >= bound) == 0) continue;
+#pragma unroll
+        for (uint32_t k = 0; k < kEach; ++k) add_group(there && m[k] >= bound, turn * Shared::kThreads + thread + k);
+      }
+    } else {
+      for (uint32_t turn = 0; turn < turns; ++turn)
+        for (uint32_t thread = 0; thread < Shared::kThreads; thread += kWave) {
+          if (vector(turn, thread, 0) >= full) break;
+          add_group(shared.most[slot(turn)][thread + tid] >= bound, turn * Shared::kThreads + thread + tid);
+        }
+    }
+    if (groups > Shared::kGroups) return Shared::kRoom + 1;
+    wave_sync();
+    uint32_t n = 0;
+    look_at(shared, groups, [&](bool there, typename Vec<T>::Floats f, uint32_t first) {
+      uint32_t found = 0;    // few lanes have more than one
+#pragma unroll
+      for (uint32_t k = 0; k < kN; ++k) found |= f[k] >= bound && f[k] > -INFINITY ? 1u << k : 0;
+      if (!there) found = 0;
+      while (__ballot(found != 0) != 0) {
+        const uint32_t at = found == 0 ? 0 : __builtin_ctz(found);
+        float v = f[0];
+#pragma unroll
+        for (uint32_t k = 1; k < kN; ++k) v = at == k ? f[k] : v;
+        n = append(shared, n, found != 0, key_of(v, first + at));
+        found &= found - 1;
+      }
+    });
+    const float last = tail();
+    n = append(shared, n, last >= bound && last > -INFINITY, key_of(last, tail_column()));
+    return n;
+  }
+
+  // The same, sorted, where the candidates have no room: the list is cut to the best `top` whenever it might not take
+  // one more of each lane.
+  __device__ __forceinline__ uint32_t collect_in_turns(Shared& shared, uint32_t top) const {
+    uint64_t floor = 0;
+    uint32_t n = 0;
+    auto look = [&](bool there, float v, uint32_t column) {
+      there = there && v > -INFINITY && key_of(v, column) > floor;
+      if (__ballot(there) == 0) return;
+      n = append(shared, n, there, key_of(v, column));
+      wave_sync();
+      if (n <= Shared::kRoom - kWave) return;
+      sort(shared, n);
+      n = std::min(n, top);
+      floor = shared.list[n - 1];
+      wave_sync();
+    };
+    for (uint32_t turn = 0; turn < turns; ++turn)
+      for (uint32_t thread = 0; thread < Shared::kThreads; thread += kWave) {
+        const uint32_t first = vector(turn, thread + tid, 0);
+        // (The lowest column of the turn's values with the largest of them.)
+        if (__ballot(first < full && key_of(shared.most[slot(turn)][thread + tid], first * kN) > floor) == 0) continue;
+        shared.groups[tid] = turn * Shared::kThreads + thread + tid;
+        wave_sync();
+        look_at(shared, kWave, [&](bool there, typename Vec<T>::Floats f, uint32_t first_column) {
+          for (uint32_t k = 0; k < kN; ++k) look(there, f[k], first_column + k);
+        });
+        wave_sync();
+      }
+    look(tid < rem, tail(), tail_column());
+    wave_sync();
+    sort(shared, n);
+    return n;
+  }
+
+  // put(i, key) for i = 0 .. top - 1; key 0 where there are no more.
+  template <class Put>
+  __device__ __forceinline__ void top(Shared& shared, uint32_t top, Put put) const {
+    uint32_t n = collect(shared, reached_by(shared.lane_most[tid], top));
+    wave_sync();
+    if (n <= kWave) {
+      const uint64_t mine = tid < n ? shared.list[tid] : 0;
+      const int low = static_cast<int>(mine), high = static_cast<int>(mine >> 32);
+      uint32_t rank = 0;
+      for (uint32_t j = 0; j < n; ++j) {
+        const uint32_t l = __builtin_amdgcn_readlane(low, j), h = __builtin_amdgcn_readlane(high, j);
+        rank += (static_cast<uint64_t>(h) << 32 | l) > mine;
+      }
+      if (tid >= n) rank = tid;
+      if (rank < top) put(rank, mine);
+      return;
+    }
+    if (n <= Shared::kRoom) sort(shared, n);
+    else n = collect_in_turns(shared, top);
+    if (tid < top) put(tid, tid < n ? shared.list[tid] : 0);
+  }
+};
+static_assert(PGC_MAX_TOP <= kWave, "a lane for each of the top tokens");
+
+template <class T, int WAVES, int U>
+__global__ __launch_bounds__(Place<WAVES * kWave>::kThreads, WAVES > 1 ? 8 : 1)   // eight waves to a SIMD
+void long_scores_kernel(ScoresArgs a) {
+  constexpr int LANES = WAVES * kWave;
+  using Row = LongRow<T, WAVES, U>;
+  __shared__ typename Row::Shared all[Place<LANES>::kRows];
+  auto& shared = all[LANES == kWave ? __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) : 0];
+  const int64_t row = Place<LANES>::row(static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x);
+  if (row >= a.rows) return;
+  const uint32_t tid = Place<LANES>::lane();
+  const Target target(a, row);
+  if (!target.counts) {
+    if (tid == 0) RowScores().write(a, row);
+    if (static_cast<int>(tid) < a.top) RowScores().write_top(a, row, tid, 0.f, -1);
     return;
   }
-  float sum = 0.f, weighted = 0.f;
-  for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) {
-    const float d = static_cast<float>(z[j]) - top, e = expf(d);
-    sum += e;
-    if (e > 0.f) weighted += e * d;
+  const Row at(static_cast<const T*>(a.logits) + row * a.stride, static_cast<uint32_t>(a.cols), tid);
+  const uint32_t target_raw = Vec<T>::raw(at.z + target.column());
+  float most;
+  Sums s = at.sums(shared, most);
+  most = lane_group_max<WAVES>(most);
+  if (tid % WAVES == 0) shared.lane_most[tid / WAVES] = most;
+  if constexpr (WAVES > 1) {
+    if (tid % kWave == 0) shared.parts[tid / kWave] = s;
+    __syncthreads();
+    if (tid >= kWave) return;
+    s = join_lanes<WAVES>(shared.parts[tid % WAVES]);
+  } else {
+    wave_sync();
   }
-  sum = block_join(sum, [](float x, float y) { return x + y; });
-  weighted = block_join(weighted, [](float x, float y) { return x + y; });
-  const float log_sum = logf(sum);
-  write(a.targets ? (static_cast<float>(z[y]) - top) - log_sum : 0.f, log_sum - weighted / sum, top, log_sum);
-  Entry last{INFINITY, 0};
-  for (int i = 0; i < a.top; ++i) {
-    Entry best{-INFINITY, kNoColumn};
-    for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) {
-      const Entry e{static_cast<float>(z[j]), static_cast<uint32_t>(j)};
-      if (last.before(e) && e.before(best) && e.value > -INFINITY) best = e;
-    }
-    last = best = block_join(best, [](const Entry& x, const Entry& y) { return x.before(y) ? x : y; });
-    if (first) write_top(i, (best.value - top) - log_sum, best.column == kNoColumn ? -1 : static_cast<int32_t>(best.column));
+  const RowScores scores(s, Vec<T>::value(target_raw));
+  if (tid == 0) scores.write(a, row);
+  if (a.top == 0) return;
+  if (!scores.any) {
+    if (static_cast<int>(tid) < a.top) scores.write_top(a, row, tid, 0.f, -1);
+    return;
   }
+  at.top(shared, a.top, [&](uint32_t i, uint64_t key) { scores.write_top(a, row, i, value_of(key), key == 0 ? -1 : column_of(key)); });
+}
+
+// One block per kRows rows.
+template <int LANES, class Kernel>
+hipError_t launch_rows(Kernel kernel, const ScoresArgs& a, hipStream_t stream) {
+  const int64_t blocks = Place<LANES>::blocks(a.rows), x = std::min(blocks, kGridX);
+  const dim3 grid(static_cast<uint32_t>(x), static_cast<uint32_t>((blocks + x - 1) / x));
+  kernel<<<grid, Place<LANES>::kThreads, 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 template <class T>
-__global__ __launch_bounds__(kThreads)
-void scores_gradient_kernel(ScoresArgs a) {
-  const int64_t row = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
-  if (row >= a.rows) return;
-  const int64_t y = a.targets ? a.targets[row] : -1;
-  const T* z = static_cast<const T*>(a.logits) + row * a.stride;
-  T* dz = static_cast<T*>(a.dlogits) + row * a.out_stride;
-  const bool counts = a.targets == nullptr || (y >= 0 && y < a.cols);
-  const float g = a.grad_logprobs && counts ? a.grad_logprobs[row] : 0.f, e = a.grad_entropy && counts ? a.grad_entropy[row] : 0.f;
-  const float top = a.stats[2 * row], log_sum = a.stats[2 * row + 1];
-  const bool none = (g == 0.f && e == 0.f) || (top == -INFINITY && log_sum == 0.f);
-  const float rest = e == 0.f ? 0.f : a.entropy[row] - log_sum;
-  for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) {
-    float v = 0.f;
-    if (!none) {
-      const float d = static_cast<float>(z[j]) - top, p = expf(d - log_sum);
-      v = p * (-g - e * (fmaxf(d, -1e4f) + rest));
-      if (j == y) v += g;
-    }
-    dz[j] = static_cast<T>(v);
-  }
-}
-
-dim3 grid_of(int64_t rows) {
-  const int64_t x = std::min<int64_t>(rows, 1 << 20);
-  return dim3(static_cast<uint32_t>(x), static_cast<uint32_t>((rows + x - 1) / x));
+hipError_t launch_typed(const ScoresArgs& a, hipStream_t stream) {
+  const int64_t vectors = (a.cols + Vec<T>::kN - 1) / Vec<T>::kN, full = a.cols / Vec<T>::kN;
+  if (vectors <= 1) return launch_rows<1>(short_scores_kernel<T, 1, 1>, a, stream);
+  if (vectors <= 2) return launch_rows<1>(short_scores_kernel<T, 1, 2>, a, stream);
+  if (vectors <= 4) return launch_rows<1>(short_scores_kernel<T, 1, 4>, a, stream);
+  if (vectors <= 8) return launch_rows<2>(short_scores_kernel<T, 2, 4>, a, stream);
+  if (vectors <= 16) return launch_rows<4>(short_scores_kernel<T, 4, 4>, a, stream);
+  if (vectors <= 32) return launch_rows<8>(short_scores_kernel<T, 8, 4>, a, stream);
+  if (vectors <= 64) return launch_rows<16>(short_scores_kernel<T, 16, 4>, a, stream);
+  if (full <= 512) return launch_rows<64>(long_scores_kernel<T, 1, 2>, a, stream);
+  if (full <= 1536) return launch_rows<128>(long_scores_kernel<T, 2, 2>, a, stream);
+  if (full <= 2048) return launch_rows<256>(long_scores_kernel<T, 4, 2>, a, stream);
+  return launch_rows<512>(long_scores_kernel<T, 8, 2>, a, stream);
 }
 
 }  // namespace
@@ -131,19 +648,11 @@ dim3 grid_of(int64_t rows) {
 size_t scores_workspace_bytes(int64_t, int64_t, int64_t, int) { return 0; }
 
 hipError_t launch_scores(const ScoresArgs& a, int dtype, void*, hipStream_t stream) {
-  const dim3 grid = grid_of(a.rows);
-  if (dtype == PGC_F32) scores_kernel<float><<<grid, kThreads, 0, stream>>>(a);
-  else if (dtype == PGC_BF16) scores_kernel<__bf16><<<grid, kThreads, 0, stream>>>(a);
-  else scores_kernel<_Float16><<<grid, kThreads, 0, stream>>>(a);
-  return hipGetLastError();
-}
-
-hipError_t launch_scores_gradient(const ScoresArgs& a, int dtype, hipStream_t stream) {
-  const dim3 grid = grid_of(a.rows);
-  if (dtype == PGC_F32) scores_gradient_kernel<float><<<grid, kThreads, 0, stream>>>(a);
-  else if (dtype == PGC_BF16) scores_gradient_kernel<__bf16><<<grid, kThreads, 0, stream>>>(a);
-  else scores_gradient_kernel<_Float16><<<grid, kThreads, 0, stream>>>(a);
-  return hipGetLastError();
+  switch (dtype) {
+    case PGC_F32: return launch_typed<float>(a, stream);
+    case PGC_BF16: return launch_typed<__bf16>(a, stream);
+    default: return launch_typed<_Float16>(a, stream);
+  }
 }
 
 }  // namespace pgc
