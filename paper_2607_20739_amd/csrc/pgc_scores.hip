@@ -195,11 +195,26 @@ struct Target {
   __device__ __forceinline__ uint32_t column() const { return y > 0 ? static_cast<uint32_t>(y) : 0; }
 };
 
+// ---- values in order ----------------------------------------------------------------------------
+
+// A value and its column as one number: the larger value is the larger number, of equal ones the lower column.
+// No value's is 0.
+__device__ __forceinline__ uint32_t ordered(float v) {
+  const uint32_t bits = __float_as_uint(v + 0.f);   // -0 as 0
+  return bits ^ (bits >> 31 ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu)); }
+__device__ __forceinline__ uint64_t key_of(float v, uint32_t column) {
+  return static_cast<uint64_t>(ordered(v)) << 32 | (0xFFFFFFFFu - column);
+}
+__device__ __forceinline__ float value_of(uint64_t key) { return unordered(static_cast<uint32_t>(key >> 32)); }
+__device__ __forceinline__ int32_t column_of(uint64_t key) { return static_cast<int32_t>(0xFFFFFFFFu - static_cast<uint32_t>(key)); }
+
 // ---- short rows -------------------------------------------------------------------------------
 
-template <int LANES>
-__device__ __forceinline__ uint32_t lane_group_min(uint32_t v) {
-  auto take = [&](int other) { v = std::min(v, static_cast<uint32_t>(other)); };
+template <int LANES, class Join>
+__device__ __forceinline__ uint32_t lane_group_join(uint32_t v, Join join) {
+  auto take = [&](int other) { v = join(v, static_cast<uint32_t>(other)); };
   const auto bits = [&] { return static_cast<int>(v); };
   if constexpr (LANES >= 2) take(__builtin_amdgcn_update_dpp(0, bits(), kDppSwap1, 0xF, 0xF, true));
   if constexpr (LANES >= 4) take(__builtin_amdgcn_update_dpp(0, bits(), kDppSwap2, 0xF, 0xF, true));
@@ -208,7 +223,18 @@ __device__ __forceinline__ uint32_t lane_group_min(uint32_t v) {
   return v;
 }
 
-// 64 / LANES rows to a wave.  The row stays in registers; its top tokens are taken out one by one.
+// Value and column of a short row of 16-bit values as one 32-bit number (0: none), in the order of key_of: such
+// values' floats have 13 zeros at their end, and there are at most 512 columns.
+constexpr uint32_t kColumnBits = 0x1FFF;
+__device__ __forceinline__ uint32_t short_key(float v, uint32_t column) {
+  return v > -INFINITY ? (ordered(v) & ~kColumnBits) | (kColumnBits - column) : 0;
+}
+__device__ __forceinline__ float short_value(uint32_t key) { return unordered(key >> 31 ? key & ~kColumnBits : key | kColumnBits); }
+
+// 64 / LANES rows to a wave.  The row stays in registers; its top tokens are taken out one by one, 16-bit values as
+// numbers that no two share: fewer instructions for each, but they have to be made (400,000 rows of 500 bf16: 30 top tokens
+// 506 us and 816 by value and column, 8 212 and 257, one 128 and 85).
+constexpr int kTopByKeys = 4;
 template <class T, int LANES, int HOLD>
 __global__ __launch_bounds__(kBlock)
 void short_scores_kernel(ScoresArgs a) {
@@ -251,41 +277,43 @@ void short_scores_kernel(ScoresArgs a) {
   s.moved = lane_group_sum<LANES>(s.moved);
   const RowScores scores(s, Vec<T>::value(target_raw));
   if (at.lane == 0) scores.write(a, row);
-  for (int i = 0; i < a.top; ++i) {
-    float best = most;
-    if (i > 0) {
-      best = -INFINITY;
+  if (sizeof(T) == 2 && a.top >= kTopByKeys) {
+    uint32_t key[kValues];
 #pragma unroll
-      for (int k = 0; k < kValues; ++k) best = fmaxf(best, f[k]);
+    for (int k = 0; k < kValues; ++k) key[k] = scores.any ? short_key(f[k], at.start(at.number(k / kN)) + k % kN) : 0;
+    for (int i = 0; i < a.top; ++i) {
+      uint32_t best = 0;
+#pragma unroll
+      for (int k = 0; k < kValues; ++k) best = std::max(best, key[k]);
+      best = lane_group_join<LANES>(best, [](uint32_t x, uint32_t y) { return std::max(x, y); });
+#pragma unroll
+      for (int k = 0; k < kValues; ++k) key[k] = key[k] == best ? 0 : key[k];
+      if (at.lane == 0) scores.write_top(a, row, i, short_value(best), best == 0 ? -1 : static_cast<int32_t>(kColumnBits - (best & kColumnBits)));
     }
-    best = lane_group_max<LANES>(best);
-    const bool there = scores.any && best > -INFINITY;
-    uint32_t mine = kValues;       // the first place of it in this lane
+  } else {
+    for (int i = 0; i < a.top; ++i) {
+      float best = most;
+      if (i > 0) {
+        best = -INFINITY;
 #pragma unroll
-    for (int k = kValues - 1; k >= 0; --k) mine = f[k] == best ? k : mine;
-    const uint32_t column = mine < kValues ? at.start(at.number(mine / kN)) + mine % kN : 0xFFFFFFFFu;
-    const uint32_t first = lane_group_min<LANES>(column);
-    if (column != first) mine = kValues;
+        for (int k = 0; k < kValues; ++k) best = fmaxf(best, f[k]);
+      }
+      best = lane_group_max<LANES>(best);
+      const bool there = scores.any && best > -INFINITY;
+      uint32_t mine = kValues;       // the first place of it in this lane
 #pragma unroll
-    for (int k = 0; k < kValues; ++k) f[k] = mine == static_cast<uint32_t>(k) ? -INFINITY : f[k];
-    if (at.lane == 0) scores.write_top(a, row, i, best, there ? static_cast<int32_t>(first) : -1);
+      for (int k = kValues - 1; k >= 0; --k) mine = f[k] == best ? k : mine;
+      const uint32_t column = mine < kValues ? at.start(at.number(mine / kN)) + mine % kN : 0xFFFFFFFFu;
+      const uint32_t first = lane_group_join<LANES>(column, [](uint32_t x, uint32_t y) { return std::min(x, y); });
+      if (column != first) mine = kValues;
+#pragma unroll
+      for (int k = 0; k < kValues; ++k) f[k] = mine == static_cast<uint32_t>(k) ? -INFINITY : f[k];
+      if (at.lane == 0) scores.write_top(a, row, i, best, there ? static_cast<int32_t>(first) : -1);
+    }
   }
 }
 
-// ---- long rows --------------------------------------------------------------------------------
-
-// A value and its column as one number: the larger value is the larger number, of equal ones the lower column.
-// No value's is 0.
-__device__ __forceinline__ uint32_t ordered(float v) {
-  const uint32_t bits = __float_as_uint(v + 0.f);   // -0 as 0
-  return bits ^ (bits >> 31 ? 0xFFFFFFFFu : 0x80000000u);
-}
-__device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float(o ^ (o >> 31 ? 0x80000000u : 0xFFFFFFFFu)); }
-__device__ __forceinline__ uint64_t key_of(float v, uint32_t column) {
-  return static_cast<uint64_t>(ordered(v)) << 32 | (0xFFFFFFFFu - column);
-}
-__device__ __forceinline__ float value_of(uint64_t key) { return unordered(static_cast<uint32_t>(key >> 32)); }
-__device__ __forceinline__ int32_t column_of(uint64_t key) { return static_cast<int32_t>(0xFFFFFFFFu - static_cast<uint32_t>(key)); }
+// ---- many candidates ----------------------------------------------------------------------------
 
 // A number that at least `top` of the wave's 64 lanes' values reach, near the largest such (its upper 16 bits are
 // searched); -inf where fewer lanes hold more.
@@ -305,16 +333,208 @@ __device__ __forceinline__ void wave_sync() {   // lanes of one wave: LDS keeps 
   __builtin_amdgcn_wave_barrier();
 }
 
+// Candidates for a row's top tokens, in LDS; kept by one wave.
+struct Candidates {
+  static constexpr uint32_t kRoom = 512;
+  uint64_t key[kRoom];
+
+  // Appends one for each lane where `there`; returns how many there are then (those past the room are lost).
+  __device__ __forceinline__ uint32_t append(uint32_t n, bool there, uint64_t k) {
+    const uint64_t lanes = __ballot(there);
+    const uint32_t at = n + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(lanes >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(lanes), 0));
+    if (there && at < kRoom) key[at] = k;
+    return n + __popcll(lanes);
+  }
+  // Of a vector per lane, from column `first` on, the values that reach `bound`.
+  template <uint32_t N, class Floats>
+  __device__ __forceinline__ uint32_t append_vector(uint32_t n, bool there, Floats f, uint32_t first, float bound) {
+    uint32_t found = 0;    // few lanes have more than one
+#pragma unroll
+    for (uint32_t k = 0; k < N; ++k) found |= f[k] >= bound && f[k] > -INFINITY ? 1u << k : 0;
+    if (!there) found = 0;
+    while (__ballot(found != 0) != 0) {
+      const uint32_t at = found == 0 ? 0 : __builtin_ctz(found);
+      float v = f[0];
+#pragma unroll
+      for (uint32_t k = 1; k < N; ++k) v = at == k ? f[k] : v;
+      n = append(n, found != 0, key_of(v, first + at));
+      found &= found - 1;
+    }
+    return n;
+  }
+  __device__ __forceinline__ uint32_t append_value(uint32_t n, float v, uint32_t column, float bound) {
+    return append(n, v >= bound && v > -INFINITY, key_of(v, column));
+  }
+
+  // Sorts n of them downwards.
+  __device__ __forceinline__ void sort(uint32_t n) {
+    const uint32_t lane = threadIdx.x % kWave;
+    uint32_t size = 2;
+    while (size < n) size *= 2;
+    for (uint32_t i = n + lane; i < size; i += kWave) key[i] = 0;
+    wave_sync();
+    for (uint32_t run = 2; run <= size; run *= 2)
+      for (uint32_t step = run / 2; step > 0; step /= 2) {
+        for (uint32_t i = lane; i < size / 2; i += kWave) {
+          const uint32_t low = i / step * 2 * step + i % step, high = low + step;
+          const uint64_t a = key[low], b = key[high];
+          if ((a < b) == ((low & run) == 0)) {
+            key[low] = b;
+            key[high] = a;
+          }
+        }
+        wave_sync();
+      }
+  }
+
+  // The best of n, `there` many at most: put(i, key) for i = 0 .. top - 1; key 0 where there are no more.
+  template <class Put>
+  __device__ __forceinline__ void put_best(uint32_t n, uint32_t top, Put put) {
+    const uint32_t lane = threadIdx.x % kWave;
+    wave_sync();
+    if (n <= kWave) {   // ranked
+      const uint64_t mine = lane < n ? key[lane] : 0;
+      const int low = static_cast<int>(mine), high = static_cast<int>(mine >> 32);
+      uint32_t rank = 0;
+      for (uint32_t j = 0; j < n; ++j) {
+        const uint32_t l = __builtin_amdgcn_readlane(low, j), h = __builtin_amdgcn_readlane(high, j);
+        rank += (static_cast<uint64_t>(h) << 32 | l) > mine;
+      }
+      if (lane >= n) rank = lane;
+      if (rank < top) put(rank, mine);
+      return;
+    }
+    sort(n);
+    if (lane < top) put(lane, lane < n ? key[lane] : 0);
+  }
+};
+static_assert(PGC_MAX_TOP <= kWave, "a lane for each of the top tokens");
+
+// The best of more candidates than there is room for: the list is cut to the best `top` whenever it might not take
+// one more of each lane.
+struct CutList {
+  Candidates& list;
+  uint32_t top, n = 0;
+  uint64_t floor = 0;     // what no longer counts
+
+  __device__ __forceinline__ void add(bool there, float v, uint32_t column) {
+    there = there && v > -INFINITY && key_of(v, column) > floor;
+    if (__ballot(there) == 0) return;
+    n = list.append(n, there, key_of(v, column));
+    if (n <= Candidates::kRoom - kWave) return;
+    wave_sync();
+    list.sort(n);
+    n = std::min(n, top);
+    floor = list.key[n - 1];
+    wave_sync();
+  }
+};
+
+// ---- rows of a wave ---------------------------------------------------------------------------
+
+// Rows of up to 64 HOLD vectors, which stay in the registers of a wave.
+template <class T, int HOLD>
+__global__ __launch_bounds__(kBlock)
+void wave_scores_kernel(ScoresArgs a) {
+  constexpr uint32_t kN = Vec<T>::kN;
+  __shared__ Candidates lists[kBlock / kWave];
+  const int64_t row = Place<kWave>::row(static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x);
+  if (row >= a.rows) return;
+  const uint32_t lane = threadIdx.x % kWave, cols = static_cast<uint32_t>(a.cols);
+  const Target target(a, row);
+  if (!target.counts) {
+    if (lane == 0) RowScores().write(a, row);
+    if (static_cast<int>(lane) < a.top) RowScores().write_top(a, row, lane, 0.f, -1);
+    return;
+  }
+  const T* z = static_cast<const T*>(a.logits) + row * a.stride;
+  const uint32_t full = long_row_vectors<T>(cols), rem = cols - full * kN, tail_column = full * kN + (lane < rem ? lane : rem - 1);
+  const VectorRun<T> run(z, full, 0, full);
+  const uint32_t before = run.before(), tail_raw = Vec<T>::raw(z + tail_column), target_raw = Vec<T>::raw(z + target.column());
+  u4v h[HOLD];
+#pragma unroll
+  for (int i = 0; i < HOLD; ++i) h[i] = run.load(i);
+  uint32_t carry = before << 16;
+  const float tail = lane < rem ? Vec<T>::value(tail_raw) : -INFINITY;
+  float most = tail;
+#pragma unroll
+  for (int i = 0; i < HOLD; ++i) {
+    h[i] = run.values(h[i], carry);
+    if (!(i < static_cast<int>(run.whole) || (i == static_cast<int>(run.whole) && lane < run.part))) h[i] = Vec<T>::none();
+    const auto f = Vec<T>::floats(h[i]);
+#pragma unroll
+    for (uint32_t k = 0; k < kN; ++k) most = fmaxf(most, f[k]);
+  }
+  WaveSums w;
+  Sums s;
+  if (w.take_shift(most)) {
+    w.template add_at<T, HOLD>(h);
+    w.add_value(tail);
+    w.top = most;
+    s = w.join();
+  } else {   // too large for it: the differences to the maximum themselves
+    const float peak = wave_max(most);
+    s = {peak, 0.f, 0.f};
+    auto add = [&](float v) {
+      const float t = (v - peak) * kLog2E, e = exp2_fast(t);
+      s.sum += e;
+      s.moved = __builtin_fmaf(e, fmaxf(t, kFar), s.moved);
+    };
+#pragma unroll
+    for (int i = 0; i < HOLD; ++i) {
+      u4v again = h[i];
+      asm("" : "+v"(again));   // unpacked anew: else the values stay in registers for it
+      const auto f = Vec<T>::floats(again);
+#pragma unroll
+      for (uint32_t k = 0; k < kN; ++k) add(f[k]);
+    }
+    add(tail);
+    s.sum = wave_sum(s.sum);
+    s.moved = wave_sum(s.moved);
+  }
+  const RowScores scores(s, Vec<T>::value(target_raw));
+  if (lane == 0) scores.write(a, row);
+  if (a.top == 0) return;
+  if (!scores.any) {
+    if (static_cast<int>(lane) < a.top) scores.write_top(a, row, lane, 0.f, -1);
+    return;
+  }
+  Candidates& list = lists[__builtin_amdgcn_readfirstlane(threadIdx.x / kWave)];
+  const uint32_t top = static_cast<uint32_t>(a.top);
+  const float bound = reached_by(most, a.top);
+  uint32_t n = 0;
+#pragma unroll
+  for (int i = 0; i < HOLD; ++i) {
+    u4v again = h[i];
+    asm("" : "+v"(again));
+    n = list.template append_vector<kN>(n, true, Vec<T>::floats(again), (i * kWave + lane) * kN, bound);
+  }
+  n = list.append_value(n, tail, tail_column, bound);
+  if (n > Candidates::kRoom) {
+    CutList cut{list, top};
+    for (uint32_t v0 = 0; v0 < full; v0 += kWave)
+      for (uint32_t k = 0; k < kN; ++k) {
+        const uint32_t column = std::min(v0 + lane, full - 1) * kN + k;
+        cut.add(v0 + lane < full, Vec<T>::value(Vec<T>::raw(z + column)), column);
+      }
+    cut.add(lane < rem, tail, tail_column);
+    n = cut.n;
+  }
+  list.put_best(n, top, [&](uint32_t i, uint64_t key) { scores.write_top(a, row, i, value_of(key), key == 0 ? -1 : column_of(key)); });
+}
+
+// ---- long rows --------------------------------------------------------------------------------
+
 // What a row's waves share.
 template <int WAVES>
 struct RowShared {
   static constexpr uint32_t kSlots = WAVES <= 4 ? 6 : 16, kThreads = WAVES * kWave;
-  static constexpr uint32_t kRoom = 512, kGroups = std::min(512u, kSlots * kThreads);
+  static constexpr uint32_t kGroups = 512;
   Sums parts[WAVES];
   float lane_most[kWave];                 // the largest of the values of WAVES lanes each
   alignas(16) float most[kSlots][kThreads];   // the largest of a thread's turn; the last slot's of all turns from there on
-  uint64_t list[kRoom];                   // candidates for the top tokens
-  uint32_t groups[kGroups];               // turns and threads whose values may hold some
+  Candidates list;
+  uint32_t groups[kGroups];               // turns and threads whose values may hold candidates
 };
 
 // A long row as its WAVES waves see it.  In turn n the row's thread `tid` has the vectors n kTurn + (tid / 64) 64 U + tid % 64 + 64 i,
@@ -442,33 +662,6 @@ struct LongRow {
       look(there, Vec<T>::floats(Vec<T>::template load<true>(z, std::min(v, full - 1), 0)), v * kN);
     }
   }
-  // Appends a candidate for each lane where `there`; returns how many there are then (those past the room are lost).
-  __device__ __forceinline__ static uint32_t append(Shared& shared, uint32_t n, bool there, uint64_t key) {
-    const uint64_t lanes = __ballot(there);
-    const uint32_t at = n + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(lanes >> 32), __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(lanes), 0));
-    if (there && at < Shared::kRoom) shared.list[at] = key;
-    return n + __popcll(lanes);
-  }
-  // Sorts n candidates downwards.
-  __device__ __forceinline__ void sort(Shared& shared, uint32_t n) const {
-    uint32_t size = 2;
-    while (size < n) size *= 2;
-    for (uint32_t i = n + tid; i < size; i += kWave) shared.list[i] = 0;
-    wave_sync();
-    for (uint32_t run = 2; run <= size; run *= 2)
-      for (uint32_t step = run / 2; step > 0; step /= 2) {
-        for (uint32_t i = tid; i < size / 2; i += kWave) {
-          const uint32_t low = i / step * 2 * step + i % step, high = low + step;
-          const uint64_t a = shared.list[low], b = shared.list[high];
-          if ((a < b) == ((low & run) == 0)) {
-            shared.list[low] = b;
-            shared.list[high] = a;
-          }
-        }
-        wave_sync();
-      }
-  }
-
   // What reaches `bound`, as candidates; more than the room where there are too many.
   __device__ __forceinline__ uint32_t collect(Shared& shared, float bound) const {
     uint32_t groups = 0;
@@ -498,96 +691,50 @@ struct LongRow {
           add_group(shared.most[slot(turn)][thread + tid] >= bound, turn * Shared::kThreads + thread + tid);
         }
     }
-    if (groups > Shared::kGroups) return Shared::kRoom + 1;
+    if (groups > Shared::kGroups) return Candidates::kRoom + 1;
     wave_sync();
     uint32_t n = 0;
     look_at(shared, groups, [&](bool there, typename Vec<T>::Floats f, uint32_t first) {
-      uint32_t found = 0;    // few lanes have more than one
-#pragma unroll
-      for (uint32_t k = 0; k < kN; ++k) found |= f[k] >= bound && f[k] > -INFINITY ? 1u << k : 0;
-      if (!there) found = 0;
-      while (__ballot(found != 0) != 0) {
-        const uint32_t at = found == 0 ? 0 : __builtin_ctz(found);
-        float v = f[0];
-#pragma unroll
-        for (uint32_t k = 1; k < kN; ++k) v = at == k ? f[k] : v;
-        n = append(shared, n, found != 0, key_of(v, first + at));
-        found &= found - 1;
-      }
+      n = shared.list.template append_vector<kN>(n, there, f, first, bound);
     });
-    const float last = tail();
-    n = append(shared, n, last >= bound && last > -INFINITY, key_of(last, tail_column()));
-    return n;
+    return shared.list.append_value(n, tail(), tail_column(), bound);
   }
 
-  // The same, sorted, where the candidates have no room: the list is cut to the best `top` whenever it might not take
-  // one more of each lane.
+  // The same where the candidates have no room.
   __device__ __forceinline__ uint32_t collect_in_turns(Shared& shared, uint32_t top) const {
-    uint64_t floor = 0;
-    uint32_t n = 0;
-    auto look = [&](bool there, float v, uint32_t column) {
-      there = there && v > -INFINITY && key_of(v, column) > floor;
-      if (__ballot(there) == 0) return;
-      n = append(shared, n, there, key_of(v, column));
-      wave_sync();
-      if (n <= Shared::kRoom - kWave) return;
-      sort(shared, n);
-      n = std::min(n, top);
-      floor = shared.list[n - 1];
-      wave_sync();
-    };
+    CutList cut{shared.list, top};
     for (uint32_t turn = 0; turn < turns; ++turn)
       for (uint32_t thread = 0; thread < Shared::kThreads; thread += kWave) {
         const uint32_t first = vector(turn, thread + tid, 0);
         // (The lowest column of the turn's values with the largest of them.)
-        if (__ballot(first < full && key_of(shared.most[slot(turn)][thread + tid], first * kN) > floor) == 0) continue;
-        shared.groups[tid] = turn * Shared::kThreads + thread + tid;
-        wave_sync();
-        look_at(shared, kWave, [&](bool there, typename Vec<T>::Floats f, uint32_t first_column) {
-          for (uint32_t k = 0; k < kN; ++k) look(there, f[k], first_column + k);
-        });
-        wave_sync();
+        if (__ballot(first < full && key_of(shared.most[slot(turn)][thread + tid], first * kN) > cut.floor) == 0) continue;
+        for (uint32_t i = 0; i < U; ++i)
+          for (uint32_t k = 0; k < kN; ++k) {
+            const uint32_t column = std::min(first + i * kWave, full - 1) * kN + k;
+            cut.add(first + i * kWave < full, Vec<T>::value(Vec<T>::raw(z + column)), column);
+          }
       }
-    look(tid < rem, tail(), tail_column());
-    wave_sync();
-    sort(shared, n);
-    return n;
+    cut.add(tid < rem, tail(), tail_column());
+    return cut.n;
   }
 
   // put(i, key) for i = 0 .. top - 1; key 0 where there are no more.
   template <class Put>
   __device__ __forceinline__ void top(Shared& shared, uint32_t top, Put put) const {
     uint32_t n = collect(shared, reached_by(shared.lane_most[tid], top));
-    wave_sync();
-    if (n <= kWave) {
-      const uint64_t mine = tid < n ? shared.list[tid] : 0;
-      const int low = static_cast<int>(mine), high = static_cast<int>(mine >> 32);
-      uint32_t rank = 0;
-      for (uint32_t j = 0; j < n; ++j) {
-        const uint32_t l = __builtin_amdgcn_readlane(low, j), h = __builtin_amdgcn_readlane(high, j);
-        rank += (static_cast<uint64_t>(h) << 32 | l) > mine;
-      }
-      if (tid >= n) rank = tid;
-      if (rank < top) put(rank, mine);
-      return;
-    }
-    if (n <= Shared::kRoom) sort(shared, n);
-    else n = collect_in_turns(shared, top);
-    if (tid < top) put(tid, tid < n ? shared.list[tid] : 0);
+    if (n > Candidates::kRoom) n = collect_in_turns(shared, top);
+    shared.list.put_best(n, top, put);
   }
 };
-static_assert(PGC_MAX_TOP <= kWave, "a lane for each of the top tokens");
 
 template <class T, int WAVES, int U>
-__global__ __launch_bounds__(Place<WAVES * kWave>::kThreads, WAVES > 1 ? 8 : 1)   // eight waves to a SIMD
+__global__ __launch_bounds__(WAVES * kWave)
 void long_scores_kernel(ScoresArgs a) {
-  constexpr int LANES = WAVES * kWave;
   using Row = LongRow<T, WAVES, U>;
-  __shared__ typename Row::Shared all[Place<LANES>::kRows];
-  auto& shared = all[LANES == kWave ? __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) : 0];
-  const int64_t row = Place<LANES>::row(static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x);
+  __shared__ typename Row::Shared shared;
+  const int64_t row = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
   if (row >= a.rows) return;
-  const uint32_t tid = Place<LANES>::lane();
+  const uint32_t tid = threadIdx.x;
   const Target target(a, row);
   if (!target.counts) {
     if (tid == 0) RowScores().write(a, row);
@@ -600,14 +747,10 @@ void long_scores_kernel(ScoresArgs a) {
   Sums s = at.sums(shared, most);
   most = lane_group_max<WAVES>(most);
   if (tid % WAVES == 0) shared.lane_most[tid / WAVES] = most;
-  if constexpr (WAVES > 1) {
-    if (tid % kWave == 0) shared.parts[tid / kWave] = s;
-    __syncthreads();
-    if (tid >= kWave) return;
-    s = join_lanes<WAVES>(shared.parts[tid % WAVES]);
-  } else {
-    wave_sync();
-  }
+  if (tid % kWave == 0) shared.parts[tid / kWave] = s;
+  __syncthreads();
+  if (tid >= kWave) return;
+  s = join_lanes<WAVES>(shared.parts[tid % WAVES]);
   const RowScores scores(s, Vec<T>::value(target_raw));
   if (tid == 0) scores.write(a, row);
   if (a.top == 0) return;
@@ -637,7 +780,12 @@ hipError_t launch_typed(const ScoresArgs& a, hipStream_t stream) {
   if (vectors <= 16) return launch_rows<4>(short_scores_kernel<T, 4, 4>, a, stream);
   if (vectors <= 32) return launch_rows<8>(short_scores_kernel<T, 8, 4>, a, stream);
   if (vectors <= 64) return launch_rows<16>(short_scores_kernel<T, 16, 4>, a, stream);
-  if (full <= 512) return launch_rows<64>(long_scores_kernel<T, 1, 2>, a, stream);
+  if (full <= 64) return launch_rows<64>(wave_scores_kernel<T, 1>, a, stream);
+  if (full <= 128) return launch_rows<64>(wave_scores_kernel<T, 2>, a, stream);
+  if (full <= 192) return launch_rows<64>(wave_scores_kernel<T, 3>, a, stream);
+  if (full <= 256) return launch_rows<64>(wave_scores_kernel<T, 4>, a, stream);
+  if (full <= 384) return launch_rows<64>(wave_scores_kernel<T, 6>, a, stream);
+  if (full <= 512) return launch_rows<64>(wave_scores_kernel<T, 8>, a, stream);
   if (full <= 1536) return launch_rows<128>(long_scores_kernel<T, 2, 2>, a, stream);
   if (full <= 2048) return launch_rows<256>(long_scores_kernel<T, 4, 2>, a, stream);
   return launch_rows<512>(long_scores_kernel<T, 8, 2>, a, stream);
