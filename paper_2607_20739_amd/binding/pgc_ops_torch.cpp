@@ -46,8 +46,8 @@ const at::Tensor& tensor(const char* name, PyObject* o) {
   TORCH_CHECK_VALUE(THPVariable_Check(o), name, " must be a tensor");
   const at::Tensor& t = THPVariable_Unpack(o);
   TORCH_CHECK_VALUE(!t.is_neg(), name, " must not be a view that negates its values on reading (resolve_neg() writes them out)");
-  // Otherwise the result would have no tangent, which counts as 0.
-  TORCH_CHECK_NOT_IMPLEMENTED(!t._fw_grad(0).defined() || !c10::AutogradState::get_tls_state().get_fw_grad_mode(),
+  // Otherwise the result would have no tangent, which counts as 0.  (A tensor that autograd knows nothing of has none.)
+  TORCH_CHECK_NOT_IMPLEMENTED(t.unsafeGetTensorImpl()->autograd_meta() == nullptr || !t._fw_grad(0).defined() || !c10::AutogradState::get_tls_state().get_fw_grad_mode(),
                               "forward-mode derivatives of the operators are not implemented, and ", name, " carries a tangent");
   return t;
 }
@@ -443,12 +443,23 @@ void of_type(const char* name, const at::Tensor& t, at::ScalarType type) {
   TORCH_CHECK_VALUE(t.scalar_type() == type, name, " must be ", type, " tensors");
 }
 
-// The call changes the tensor: autograd notices a saved one by its version.
-void written(const at::Tensor& t) {
-  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
-}
+// Tensors that a call changes: autograd notices a saved one by its version.
+class Changed {
+ public:
+  explicit Changed(int64_t most) { impls_.reserve(static_cast<size_t>(most)); }
+  void add(const at::Tensor& t) {
+    if (!t.is_inference()) impls_.push_back(t.unsafeGetTensorImpl());
+  }
+  void bump() const {
+    for (c10::TensorImpl* impl : impls_) impl->bump_version();
+  }
+
+ private:
+  std::vector<c10::TensorImpl*> impls_;
+};
 void no_gradient(const char* name, const at::Tensor& t) {
-  TORCH_CHECK_VALUE(!t.requires_grad() || !at::GradMode::is_enabled(), name, " must not ask for a gradient (detach() them)");
+  TORCH_CHECK_VALUE(t.unsafeGetTensorImpl()->autograd_meta() == nullptr || !t.requires_grad() || !at::GradMode::is_enabled(), name,
+                    " must not ask for a gradient (detach() them)");
 }
 
 // One value on the GPU; null for None.
@@ -516,6 +527,7 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
   }
   std::optional<at::Device> device;
   std::vector<pgc_adamw_tensor> tensors(count);
+  Changed changed(5 * count);
   for (int64_t i = 0; i < count; ++i) {
     const at::Tensor& p = dense("params", params[i]);
     if (!device) device = p.device();
@@ -527,6 +539,9 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
     of_type("variances", v, scales ? at::kByte : at::kFloat);
     no_gradient("moments", m);
     no_gradient("variances", v);
+    changed.add(p);
+    changed.add(m);
+    changed.add(v);
     pgc_adamw_tensor& t = tensors[i];
     t.param = p.data_ptr();
     t.grad = g.data_ptr();
@@ -541,11 +556,13 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
       TORCH_CHECK_VALUE(s.device() == *device && s.scalar_type() == at::kFloat && s.sizes() == at::IntArrayRef({blocks, 2}) && s.is_contiguous(),
                         "scales must be contiguous float32 tensors of shape [blocks of 256 values, 2]");
       no_gradient("scales", s);
+      changed.add(s);
       t.scales = static_cast<float*>(s.data_ptr());
     }
     if (copies) {
       const at::Tensor& c = beside("copies", (*copies)[i], p);
       no_gradient("copies", c);
+      changed.add(c);
       t.copy = c.data_ptr();
       t.copy_dtype = floating("copies", c);
     }
@@ -566,13 +583,7 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Py_RETURN_NONE;
   }
   launch(*device, [&](void* stream) { return pgc_adamw(tensors.data(), count, &k, stream); });
-  for (int64_t i = 0; i < count; ++i) {
-    written(params[i]);
-    written(moments[i]);
-    written(variances[i]);
-    if (scales) written((*scales)[i]);
-    if (copies) written((*copies)[i]);
-  }
+  changed.bump();
   Py_RETURN_NONE;
   END_HANDLE_TH_ERRORS
 }
@@ -587,6 +598,7 @@ PyObject* adamw_state_values(PyObject*, PyObject* const* a, Py_ssize_t n) {
   for (const List* l : {&variances, &scales, &ms, &vs}) l->expect_size(count);
   if (count == 0) Py_RETURN_NONE;
   std::vector<pgc_adamw_state> tensors(count);
+  Changed changed(2 * count);
   const at::Device device = dense("moments", moments[0]).device();
   for (int64_t i = 0; i < count; ++i) {
     const at::Tensor &m = dense("moments", moments[i]), &v = beside("variances", variances[i], m), &s = scales[i];
@@ -600,13 +612,12 @@ PyObject* adamw_state_values(PyObject*, PyObject* const* a, Py_ssize_t n) {
                       "out must be float32 or bfloat16 tensors");
     no_gradient("out", mv);
     no_gradient("out", vv);
+    changed.add(mv);
+    changed.add(vv);
     tensors[i] = {m.data_ptr(), v.data_ptr(), static_cast<float*>(s.data_ptr()), mv.data_ptr(), vv.data_ptr(), m.numel(), dtype_of(mv)};
   }
   launch(device, [&](void* stream) { return pgc_adamw_state_values(tensors.data(), count, stream); });
-  for (int64_t i = 0; i < count; ++i) {
-    written(ms[i]);
-    written(vs[i]);
-  }
+  changed.bump();
   Py_RETURN_NONE;
   END_HANDLE_TH_ERRORS
 }

@@ -240,19 +240,18 @@ class Ranges {
   std::vector<size_t> kinds_{0};
 };
 
-// Deals tensors out to launches of at most `most`, each with the first block of its own: calls
-// put(args, slot, index) for a tensor with values, launch(args, blocks) for each full or last one.
+// Deals tensors out to launches of at most Args::kMost: calls put(args, slot, index, first block) for a tensor with
+// values, launch(args, blocks) for each full or last launch.
 template <class Args, class Count, class Put, class Launch>
-int deal(Args& args, int64_t n, int most, int64_t chunk, Count count, Put put, Launch launch) {
+int deal(Args& args, int64_t n, int64_t chunk, Count count, Put put, Launch launch) {
   int64_t blocks = 0;
   args.tensors = 0;
   args.chunk = static_cast<int32_t>(chunk);
   for (int64_t i = 0; i < n; ++i) {
     if (count(i) == 0) continue;
-    put(args, args.tensors, i);
-    args.first[args.tensors++] = static_cast<int32_t>(blocks);
+    put(args, args.tensors++, i, static_cast<int32_t>(blocks));
     blocks += (count(i) + chunk - 1) / chunk;
-    if (args.tensors < most) continue;
+    if (args.tensors < Args::kMost) continue;
     CHECK(launch(args, blocks));
     args.tensors = 0;
     blocks = 0;
@@ -320,18 +319,31 @@ int adamw(const pgc_adamw_tensor* tensors, int64_t n, const pgc_adamw_args* a, h
   k.step = a->step;
   k.rate = static_cast<float>(a->lr / -std::expm1(a->step * k.log_beta1));
   k.spread = static_cast<float>(1.0 / std::sqrt(-std::expm1(a->step * k.log_beta2)));
+  // The root of a number below 2^-126 may be taken for 0: at most 1.1e-19, times spread. Beside this eps that is within
+  // the roundings; a step on the device can be any.
+  const bool exact = k.eps < 0x1p-30f || !(k.spread <= 1024.f) || (a->step_at && a->beta2 > 0.999999);
   k.lr_at = a->lr_at;
   k.step_at = a->step_at;
   k.factor = a->factor;
-  return deal(k, n, pgc::kMostTensors, pgc::adamw_chunk(values), [&](int64_t i) { return tensors[i].count; },
-              [&](pgc::AdamwArgs& args, int at, int64_t i) {
+  return deal(k, n, pgc::adamw_chunk(values, a->state_bits), [&](int64_t i) { return tensors[i].count; },
+              [&](pgc::AdamwArgs& args, int at, int64_t i, int32_t first) {
                 const pgc_adamw_tensor& t = tensors[i];
-                args.tensor[at] = {t.param, t.grad, t.copy, t.m, t.v, t.scales, t.count,
-                                   static_cast<float>(a->lr_at ? t.weight_decay : t.weight_decay * a->lr),
-                                   static_cast<int8_t>(t.param_dtype), static_cast<int8_t>(t.grad_dtype), static_cast<int8_t>(t.copy_dtype)};
+                pgc::AdamwTensor& to = args.tensor[at];
+                to.param = t.param;
+                to.grad = t.grad;
+                to.copy = t.copy;
+                to.m = t.m;
+                to.v = t.v;
+                to.scales = t.scales;
+                to.count = t.count;
+                to.param_dtype = t.param_dtype;
+                to.grad_dtype = t.grad_dtype;
+                to.copy_dtype = t.copy_dtype;
+                to.decay = static_cast<float>(a->lr_at ? t.weight_decay : t.weight_decay * a->lr);
+                to.first = first;
               },
               [&](const pgc::AdamwArgs& args, int64_t blocks) {
-                return launched(pgc::launch_adamw(args, blocks, a->state_bits, stream), "AdamW kernel");
+                return launched(pgc::launch_adamw(args, blocks, a->state_bits, exact, stream), "AdamW kernel");
               });
 }
 
@@ -362,16 +374,18 @@ int state_values(const pgc_adamw_state* tensors, int64_t n, hipStream_t stream) 
   each("v_values", true, [](Tensor t) { return t.v_values; }, [](Tensor t) -> size_t { return t.count * value_bytes(t.dtype); });
   CHECK(ranges.check());
   pgc::StateArgs k{};
-  return deal(k, n, pgc::kMostTensors, pgc::adamw_chunk(values), [&](int64_t i) { return tensors[i].count; },
-              [&](pgc::StateArgs& args, int at, int64_t i) {
+  return deal(k, n, pgc::state_chunk(values), [&](int64_t i) { return tensors[i].count; },
+              [&](pgc::StateArgs& args, int at, int64_t i, int32_t first) {
                 const pgc_adamw_state& t = tensors[i];
-                args.m[at] = t.m;
-                args.v[at] = t.v;
-                args.scales[at] = t.scales;
-                args.m_values[at] = t.m_values;
-                args.v_values[at] = t.v_values;
-                args.count[at] = t.count;
-                args.dtype[at] = static_cast<int8_t>(t.dtype);
+                pgc::StateTensor& to = args.tensor[at];
+                to.m = t.m;
+                to.v = t.v;
+                to.scales = t.scales;
+                to.m_values = t.m_values;
+                to.v_values = t.v_values;
+                to.count = t.count;
+                to.dtype = t.dtype;
+                to.first = first;
               },
               [&](const pgc::StateArgs& args, int64_t blocks) {
                 return launched(pgc::launch_state_values(args, blocks, stream), "state kernel");
@@ -418,11 +432,11 @@ int grad_norm(const pgc_values* tensors, int64_t n, double max_norm, double scal
   CHECK(ranges.check());
   double* sums = static_cast<double*>(workspace);
   pgc::NormArgs k{};
-  CHECK(deal(k, n, pgc::kMostValues, chunk, [&](int64_t i) { return tensors[i].count; },
-             [&](pgc::NormArgs& args, int at, int64_t i) {
+  CHECK(deal(k, n, chunk, [&](int64_t i) { return tensors[i].count; },
+             [&](pgc::NormArgs& args, int at, int64_t i, int32_t first) {
                args.data[at] = tensors[i].data;
-               args.count[at] = tensors[i].count;
-               args.dtype[at] = static_cast<int8_t>(tensors[i].dtype);
+               args.count[at] = tensors[i].count | static_cast<int64_t>(tensors[i].dtype) << 56;
+               args.first[at] = first;
              },
              [&](pgc::NormArgs& args, int64_t blocks_now) {
                args.sums = sums;

@@ -92,15 +92,13 @@ hipError_t launch_scores(const ScoresArgs& a, int dtype, void* workspace, hipStr
 size_t scores_workspace_bytes(int64_t rows, int64_t cols, int64_t top, int dtype);
 hipError_t launch_scores_gradient(const ScoresArgs& a, int dtype, hipStream_t stream);
 
-// Many tensors go to a kernel by value, as many at a time as its arguments hold.
-constexpr int kMostTensors = 48, kMostValues = 64;
-
+// Many tensors go to a kernel by value, as many at a time as 4 KiB of arguments hold.
 struct NormArgs {
-  const void* data[kMostValues];
-  int64_t count[kMostValues];
-  int32_t first[kMostValues];   // the tensor's first block
-  int8_t dtype[kMostValues];
-  int32_t tensors, chunk;       // chunk: values of a block
+  static constexpr int kMost = 192;
+  const void* data[kMost];
+  int64_t count[kMost];         // the values, and from bit 56 on their dtype
+  int32_t first[kMost];         // the tensor's first block
+  int32_t tensors, chunk;       // chunk: values of a block, a multiple of 2,048
   double* sums;                 // a block's each
 };
 struct NormEnd {
@@ -121,14 +119,16 @@ struct AdamwTensor {
   void* m;
   void* v;
   float* scales;           // of 8-bit states
-  int64_t count;
+  int64_t count : 48;
+  int64_t param_dtype : 4, grad_dtype : 4, copy_dtype : 4;
   float decay;             // weight_decay; times lr where that is on the host
-  int8_t param_dtype, grad_dtype, copy_dtype;
+  int32_t first;           // the tensor's first block
 };
+static_assert(sizeof(AdamwTensor) == 64);
 struct AdamwArgs {
-  AdamwTensor tensor[kMostTensors];
-  int32_t first[kMostTensors];   // the tensor's first block
-  int32_t tensors, chunk;        // chunk: values of a block, a multiple of 4,096
+  static constexpr int kMost = 61;
+  AdamwTensor tensor[kMost];
+  int32_t tensors, chunk;        // chunk: values of a block, a multiple of 2,048
   float beta1, rest1, beta2, rest2, eps;   // rest = 1 - beta
   float rate;                    // lr / (1 - beta1^step)
   float spread;                  // 1 / sqrt(1 - beta2^step)
@@ -139,20 +139,28 @@ struct AdamwArgs {
   const int64_t* step_at;
   const float* factor;
 };
-int32_t adamw_chunk(int64_t values);
-hipError_t launch_adamw(const AdamwArgs& a, int64_t blocks, int state_bits, hipStream_t stream);
+int32_t adamw_chunk(int64_t values, int state_bits);
+// exact: whether roots and quotients have to be.
+hipError_t launch_adamw(const AdamwArgs& a, int64_t blocks, int state_bits, bool exact, hipStream_t stream);
 
-struct StateArgs {
-  const void* m[kMostTensors];
-  const void* v[kMostTensors];
-  const float* scales[kMostTensors];
-  void* m_values[kMostTensors];
-  void* v_values[kMostTensors];
-  int64_t count[kMostTensors];
-  int32_t first[kMostTensors];
-  int8_t dtype[kMostTensors];
-  int32_t tensors, chunk;
+struct StateTensor {
+  const void* m;
+  const void* v;
+  const float* scales;
+  void* m_values;
+  void* v_values;
+  int64_t count : 48;
+  int64_t dtype : 8;
+  int32_t first;           // the tensor's first block
 };
+struct StateArgs {
+  static constexpr int kMost = 64;
+  StateTensor tensor[kMost];
+  int32_t tensors, chunk;  // chunk: values of a block, a multiple of 2,048
+};
+int32_t state_chunk(int64_t values);
 hipError_t launch_state_values(const StateArgs& a, int64_t blocks, hipStream_t stream);
+
+static_assert(sizeof(NormArgs) <= 4096 && sizeof(AdamwArgs) <= 4096 && sizeof(StateArgs) <= 4096);
 
 }  // namespace pgc
