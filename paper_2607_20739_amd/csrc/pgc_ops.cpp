@@ -656,7 +656,7 @@ int pgc_token_scores_workspace_bytes(const pgc_logits* logits, int64_t top, size
   if (!known(logits->dtype)) return fail(PGC_EINVAL, "unknown dtype %d", logits->dtype);
   CHECK(check_extents(logits->rows, logits->cols));
   if (top < 0 || top > PGC_MAX_TOP) return fail(PGC_EINVAL, "top must lie in [0, %d]", PGC_MAX_TOP);
-  *bytes = align_up(pgc::scores_workspace_bytes(logits->rows, logits->cols, top, logits->dtype));
+  *bytes = align_up(pgc::scores_workspace_bytes(logits->rows, logits->cols, logits->dtype));
   return PGC_OK;
 }
 

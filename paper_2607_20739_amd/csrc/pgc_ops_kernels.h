@@ -89,7 +89,7 @@ struct ScoresArgs {
   void* dlogits;
 };
 hipError_t launch_scores(const ScoresArgs& a, int dtype, void* workspace, hipStream_t stream);
-size_t scores_workspace_bytes(int64_t rows, int64_t cols, int64_t top, int dtype);
+size_t scores_workspace_bytes(int64_t rows, int64_t cols, int dtype);
 hipError_t launch_scores_gradient(const ScoresArgs& a, int dtype, hipStream_t stream);
 
 // Many tensors go to a kernel by value, as many at a time as 4 KiB of arguments hold.

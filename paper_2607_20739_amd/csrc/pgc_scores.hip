@@ -133,14 +133,25 @@ struct WaveSums {
     top = fmaxf(top, v);
     return true;
   }
-  // Over the wave, with the maximum in K's place.
-  __device__ __forceinline__ Sums join() const {
-    const float peak = wave_max(top), s = wave_sum(sum), w = wave_sum(moved);
-    if (peak == -INFINITY) return {peak, s, w};
-    const float t = exponent(peak), factor = exp2_fast(-t);
-    return {peak, s * factor, __builtin_fmaf(-t, s, w) * factor};
+  // This lane's, with the wave's maximum in K's place.
+  __device__ __forceinline__ Sums by_maximum() const {
+    const float peak = wave_max(top);
+    if (peak == -INFINITY) return {peak, sum, moved};
+    // Far below K, which the row's values have reached elsewhere, nothing is left of the sums, nor counts.
+    const float t = exponent(peak), factor = t < -100.f ? 0.f : exp2_fast(-t);
+    return {peak, sum * factor, __builtin_fmaf(-t, sum, moved) * factor};
   }
 };
+
+// Sums of values that follow each other.
+__device__ __forceinline__ Sums both(Sums a, Sums b) {
+  const float top = fmaxf(a.top, b.top), base = finite_top(top);
+  const Shift x(a.top, base), y(b.top, base);
+  return {top, x.sum(a) + y.sum(b), x.moved(a) + y.moved(b)};
+}
+
+// Over a wave whose lanes have the same maximum.
+__device__ __forceinline__ Sums add_lanes(Sums s) { return {s.top, wave_sum(s.sum), wave_sum(s.moved)}; }
 
 // Joined over LANES lanes of a wave; every lane ends with the result.
 template <int LANES>
@@ -471,7 +482,7 @@ void wave_scores_kernel(ScoresArgs a) {
     w.template add_at<T, HOLD>(h);
     w.add_value(tail);
     w.top = most;
-    s = w.join();
+    s = add_lanes(w.by_maximum());
   } else {   // too large for it: the differences to the maximum themselves
     const float peak = wave_max(most);
     s = {peak, 0.f, 0.f};
@@ -525,12 +536,18 @@ void wave_scores_kernel(ScoresArgs a) {
 
 // ---- long rows --------------------------------------------------------------------------------
 
+// Rows of more than seven turns are added up in up to kParts parts of at least kPartTurns turns (to end a part costs a wave a
+// twentieth of four turns); the longest rows' waves, and how many vectors a lane of theirs takes at once; turns under way
+// in a part that has a block to itself.
+constexpr uint32_t kParts = 4, kPartTurns = 4;
+constexpr int kLongWaves = 8, kLongVectors = 2, kPartAhead = 4;
+
 // What a row's waves share.
 template <int WAVES>
 struct RowShared {
   static constexpr uint32_t kSlots = WAVES <= 4 ? 6 : 16, kThreads = WAVES * kWave;
   static constexpr uint32_t kGroups = 512;
-  Sums parts[WAVES];
+  Sums parts[kParts][WAVES];
   float lane_most[kWave];                 // the largest of the values of WAVES lanes each
   alignas(16) float most[kSlots][kThreads];   // the largest of a thread's turn; the last slot's of all turns from there on
   Candidates list;
@@ -538,116 +555,169 @@ struct RowShared {
 };
 
 // A long row as its WAVES waves see it.  In turn n the row's thread `tid` has the vectors n kTurn + (tid / 64) 64 U + tid % 64 + 64 i,
-// i = 0 .. U - 1.
+// i = 0 .. U - 1.  Turns are dealt out to parts, whose sums are added lane by lane, so that few rows can have a block for
+// each part.
 template <class T, int WAVES, int U>
 struct LongRow {
   static constexpr uint32_t kN = Vec<T>::kN, kTurn = WAVES * kWave * U;
   using Shared = RowShared<WAVES>;
   const T* z;
-  uint32_t cols, full, rem, tid, turns;
+  uint32_t cols, full, rem, tid;
+  uint32_t begin, end;      // the block's turns
 
   __device__ __forceinline__ LongRow(const T* z_, uint32_t cols_, uint32_t tid_)
-      : z(z_), cols(cols_), full(long_row_vectors<T>(cols_)), rem(cols_ - full * kN), tid(tid_), turns((full + kTurn - 1) / kTurn) {}
-  __device__ __forceinline__ static uint32_t slot(uint32_t turn) { return std::min(turn, Shared::kSlots - 1); }
+      : z(z_), cols(cols_), full(long_row_vectors<T>(cols_)), rem(cols_ - full * kN), tid(tid_), begin(0), end((full + kTurn - 1) / kTurn) {}
+  __device__ __forceinline__ uint32_t slot(uint32_t turn) const { return std::min(turn - begin, Shared::kSlots - 1); }
   __device__ __forceinline__ static uint32_t vector(uint32_t turn, uint32_t thread, uint32_t i) {
     return turn * kTurn + thread / kWave * (kWave * U) + i * kWave + thread % kWave;
   }
-  // The values behind the vectors go to the row's first lanes.
+  // The values behind the vectors go to the first lanes of who has the last turn.
+  __device__ __forceinline__ bool has_tail() const { return tid < kWave && begin < end && static_cast<uint64_t>(end) * kTurn >= full; }
   __device__ __forceinline__ uint32_t tail_column() const { return full * kN + (tid < rem ? tid : rem - 1); }
   __device__ __forceinline__ float tail() const {
     const float v = Vec<T>::value(Vec<T>::raw(z + tail_column()));
-    return tid < rem ? v : -INFINITY;
+    return has_tail() && tid < rem ? v : -INFINITY;
   }
 
-  // Passes the vectors of this wave's part to each(turn, vectors), until that returns false.
-  template <class Each>
-  __device__ __forceinline__ bool each_turn(Each each) const {
-    uint32_t turn = 0, v0 = __builtin_amdgcn_readfirstlane(tid / kWave) * (kWave * U);
-    if (v0 >= full) return true;
-    VectorRun<T> run(z, full, v0, kWave * U);
-    uint32_t before = run.before();
-    u4v next[U];
+  __device__ __forceinline__ VectorRun<T> run(uint32_t v0) const { return VectorRun<T>(z, full, v0, kWave * U); }
+  // Passes the vectors of this wave in turns `from` to `to` to each(turn, vectors); those of AHEAD further turns are on
+  // their way meanwhile.
+  template <int AHEAD, class Each>
+  __device__ __forceinline__ void each_turn(uint32_t from_turn, uint32_t to, Each each) const {
+    const uint32_t wave0 = __builtin_amdgcn_readfirstlane(tid / kWave) * (kWave * U);
+    u4v next[AHEAD][U];
+    uint32_t before[AHEAD];
+    auto load = [&](uint32_t turn, int a) {
+      const VectorRun<T> from = run(turn * kTurn + wave0);
+      before[a] = from.before();
 #pragma unroll
-    for (int i = 0; i < U; ++i) next[i] = run.load(i);
-    for (bool more = true; more; ++turn) {
-      u4v h[U];
-      uint32_t carry = before << 16;
+      for (int i = 0; i < U; ++i) next[a][i] = from.load(i);
+    };
+    auto has = [&](uint32_t turn) { return turn < to && turn * kTurn + wave0 < full; };
 #pragma unroll
-      for (int i = 0; i < U; ++i) h[i] = run.values(next[i], carry);
-      const VectorRun<T> now = run;
-      v0 += kTurn;
-      more = v0 < full;
-      if (more) {      // the next turn's vectors are on their way while these are added
-        run = VectorRun<T>(z, full, v0, kWave * U);
-        before = run.before();
+    for (int a = 0; a < AHEAD; ++a)
+      if (has(from_turn + a)) load(from_turn + a, a);
+    for (uint32_t turn0 = from_turn; has(turn0); turn0 += AHEAD) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) next[i] = run.load(i);
+      for (int a = 0; a < AHEAD; ++a) {
+        const uint32_t turn = turn0 + a;
+        if (!has(turn)) break;
+        const VectorRun<T> now = run(turn * kTurn + wave0);
+        u4v h[U];
+        uint32_t carry = before[a] << 16;
+#pragma unroll
+        for (int i = 0; i < U; ++i) h[i] = now.values(next[a][i], carry);
+        if (has(turn + AHEAD)) load(turn + AHEAD, a);
+        if (now.whole < U) {
+#pragma unroll
+          for (uint32_t i = 0; i < U; ++i)
+            if (!(i < now.whole || (i == now.whole && now.lane < now.part))) h[i] = Vec<T>::none();
+        }
+        each(turn, h);
       }
-      if (now.whole < U) {
-#pragma unroll
-        for (uint32_t i = 0; i < U; ++i)
-          if (!(i < now.whole || (i == now.whole && now.lane < now.part))) h[i] = Vec<T>::none();
-      }
-      if (!each(turn, h)) return false;
     }
-    return true;
   }
-  // The sums of this wave's part, in all its lanes; and the largest of this lane's values.
-  __device__ __forceinline__ Sums sums(Shared& shared, float& most) const {
+  // The largest of a turn's values of this lane, for its slot.
+  __device__ __forceinline__ void keep(Shared& shared, uint32_t turn, float most) const {
+    float& to = shared.most[slot(turn)][tid];
+    to = turn - begin < Shared::kSlots ? most : fmaxf(to, most);
+  }
+  // This wave's sums, by parts of so many turns, to shared.parts; and the largest of this lane's values.
+  template <int AHEAD>
+  __device__ __forceinline__ float sums(Shared& shared, uint32_t part_turns) const {
     const float tail_value = tail();
-    WaveSums s;
-    float last = -INFINITY;
-    const bool done = each_turn([&](uint32_t turn, u4v (&h)[U]) {
-      if (turn == 0) {   // the first K, by the first vectors
-        const auto f = Vec<T>::floats(h[0]);
-        float first = f[0];
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    if (tid % kWave < kParts) shared.parts[tid % kWave][wave] = Sums{-INFINITY, 0.f, 0.f};   // of parts without a vector
+    uint32_t part = 0, next = begin + part_turns, large = 0;
+    float most = -INFINITY;
+    // Each part starts from the K of the wave's first vectors in the row, whoever has them.
+    WaveSums start;
+    bool start_fine = true;
+    auto begin_with = [&](u4v first) {
+      const auto f = Vec<T>::floats(first);
+      float peak = f[0];
 #pragma unroll
-        for (uint32_t k = 1; k < kN; ++k) first = fmaxf(first, f[k]);
-        if (!s.take_shift(first)) return false;
+      for (uint32_t k = 1; k < kN; ++k) peak = fmaxf(peak, f[k]);
+      start_fine = start.take_shift(peak);
+    };
+    if (begin > 0 && begin < end) {   // (of a row in parts: its first turn is a whole one)
+      const VectorRun<T> from = run(wave * (kWave * U));
+      uint32_t carry = from.before() << 16;
+      begin_with(from.values(from.load(0), carry));
+    }
+    WaveSums s = start;
+    bool fine = start_fine;
+    auto finish = [&] {
+      if (fine) {
+        const Sums sums = add_lanes(s.by_maximum());
+        if (tid % kWave == 0) shared.parts[part][wave] = sums;
+      } else {
+        large |= 1u << part;
       }
+    };
+    each_turn<AHEAD>(begin, end, [&](uint32_t turn, u4v (&h)[U]) {
+      if (turn == 0) {
+        begin_with(h[0]);
+        s = start;
+        fine = start_fine;
+      }
+      if (turn == next) {
+        finish();
+        s = start;
+        fine = start_fine;
+        ++part;
+        next += part_turns;
+      }
+      if (!fine) return;
       float here;
-      if (!s.template add<T, U>(h, here)) return false;
-      last = turn < Shared::kSlots ? here : fmaxf(last, here);
-      shared.most[slot(turn)][tid] = last;
-      return true;
+      fine = s.template add<T, U>(h, here);
+      if (!fine) return;
+      most = fmaxf(most, here);
+      keep(shared, turn, here);
     });
-    if (!done || (tid < kWave && !s.add_value(tail_value))) return sums_of_large(shared, most, tail_value);
-    most = s.top;
-    return s.join();
+    if (fine && has_tail()) {
+      most = fmaxf(most, tail_value);
+      fine = s.add_value(tail_value);
+    }
+    finish();
+    while (large != 0) {
+      const uint32_t p = __builtin_ctz(large);
+      large &= large - 1;
+      const Sums sums = sums_of_large(shared, begin + p * part_turns, std::min(begin + (p + 1) * part_turns, end), most, tail_value);
+      if (tid % kWave == 0) shared.parts[p][wave] = sums;
+    }
+    return most;
   }
-  // The same of values past 2^20, where a K near the maximum is no 32-bit number: the differences to the maximum
+  // Those of a part with values past 2^20, where a K near the maximum is no 32-bit number: the differences to the maximum
   // themselves, in a second pass.
-  __device__ __forceinline__ Sums sums_of_large(Shared& shared, float& most, float tail_value) const {
-    float top = -INFINITY, last = -INFINITY;
-    each_turn([&](uint32_t turn, u4v (&h)[U]) {
+  __device__ __forceinline__ Sums sums_of_large(Shared& shared, uint32_t from, uint32_t to, float& most, float tail_value) const {
+    float top = -INFINITY;
+    each_turn<1>(from, to, [&](uint32_t turn, u4v (&h)[U]) {
       float here = -INFINITY;
       for (uint32_t i = 0; i < U; ++i) {
         const auto f = Vec<T>::floats(h[i]);
         for (uint32_t k = 0; k < kN; ++k) here = fmaxf(here, f[k]);
       }
-      last = turn < Shared::kSlots ? here : fmaxf(last, here);
-      shared.most[slot(turn)][tid] = last;
+      keep(shared, turn, here);
       top = fmaxf(top, here);
-      return true;
     });
-    if (tid < kWave) top = fmaxf(top, tail_value);
-    most = top;
-    const float peak = wave_max(top);
-    float sum = 0.f, moved = 0.f;
+    const bool with_tail = to == end && has_tail();
+    if (with_tail) top = fmaxf(top, tail_value);
+    most = fmaxf(most, top);
+    Sums s{wave_max(top), 0.f, 0.f};
     auto add = [&](float v) {
-      const float t = (v - peak) * kLog2E, e = exp2_fast(t);
-      sum += e;
-      moved = __builtin_fmaf(e, fmaxf(t, kFar), moved);
+      const float t = (v - finite_top(s.top)) * kLog2E, e = exp2_fast(t);
+      s.sum += e;
+      s.moved = __builtin_fmaf(e, fmaxf(t, kFar), s.moved);
     };
-    each_turn([&](uint32_t, u4v (&h)[U]) {
+    each_turn<1>(from, to, [&](uint32_t, u4v (&h)[U]) {
       for (uint32_t i = 0; i < U; ++i) {
         const auto f = Vec<T>::floats(h[i]);
         for (uint32_t k = 0; k < kN; ++k) add(f[k]);
       }
-      return true;
     });
-    if (tid < kWave) add(tail_value);
-    return {peak, wave_sum(sum), wave_sum(moved)};
+    if (with_tail) add(tail_value);
+    return add_lanes(s);
   }
 
   // ---- the top tokens, by the row's first wave
@@ -675,17 +745,29 @@ struct LongRow {
     if constexpr (WAVES >= 4) {   // four threads' maxima to a lane
       constexpr uint32_t kEach = 4, kStep = kEach * kWave;
       typedef float f4v __attribute__((ext_vector_type(4)));
-      for (uint32_t j = 0; j < turns * (Shared::kThreads / kStep); ++j) {
-        const uint32_t turn = j / (Shared::kThreads / kStep), thread = j % (Shared::kThreads / kStep) * kStep + kEach * tid;
-        // (Threads without vectors in the last turn have written nothing.)
-        const bool there = vector(turn, thread & ~(kWave - 1), 0) < full;
-        const f4v m = *reinterpret_cast<const f4v*>(&shared.most[slot(turn)][thread]);
-        if (__ballot(there && fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) >= bound) == 0) continue;
+      constexpr uint32_t kSteps = Shared::kThreads / kStep, kReads = 4;
+      const uint32_t steps = (end - begin) * kSteps;
+      auto turn_of = [&](uint32_t j) { return begin + j / kSteps; };
+      auto thread_of = [&](uint32_t j) { return j % kSteps * kStep + kEach * tid; };
+      for (uint32_t j0 = 0; j0 < steps; j0 += kReads) {
+        f4v m[kReads];
 #pragma unroll
-        for (uint32_t k = 0; k < kEach; ++k) add_group(there && m[k] >= bound, turn * Shared::kThreads + thread + k);
+        for (uint32_t r = 0; r < kReads; ++r) {
+          const uint32_t j = std::min(j0 + r, steps - 1);
+          m[r] = *reinterpret_cast<const f4v*>(&shared.most[slot(turn_of(j))][thread_of(j)]);
+        }
+#pragma unroll
+        for (uint32_t r = 0; r < kReads; ++r) {
+          const uint32_t j = j0 + r, turn = turn_of(j), thread = thread_of(j);
+          // (Threads without vectors in the last turn have written nothing.)
+          const bool there = j < steps && vector(turn, thread & ~(kWave - 1), 0) < full;
+          if (__ballot(there && fmaxf(fmaxf(m[r][0], m[r][1]), fmaxf(m[r][2], m[r][3])) >= bound) == 0) continue;
+#pragma unroll
+          for (uint32_t k = 0; k < kEach; ++k) add_group(there && m[r][k] >= bound, turn * Shared::kThreads + thread + k);
+        }
       }
     } else {
-      for (uint32_t turn = 0; turn < turns; ++turn)
+      for (uint32_t turn = begin; turn < end; ++turn)
         for (uint32_t thread = 0; thread < Shared::kThreads; thread += kWave) {
           if (vector(turn, thread, 0) >= full) break;
           add_group(shared.most[slot(turn)][thread + tid] >= bound, turn * Shared::kThreads + thread + tid);
@@ -703,7 +785,7 @@ struct LongRow {
   // The same where the candidates have no room.
   __device__ __forceinline__ uint32_t collect_in_turns(Shared& shared, uint32_t top) const {
     CutList cut{shared.list, top};
-    for (uint32_t turn = 0; turn < turns; ++turn)
+    for (uint32_t turn = begin; turn < end; ++turn)
       for (uint32_t thread = 0; thread < Shared::kThreads; thread += kWave) {
         const uint32_t first = vector(turn, thread + tid, 0);
         // (The lowest column of the turn's values with the largest of them.)
@@ -714,22 +796,32 @@ struct LongRow {
             cut.add(first + i * kWave < full, Vec<T>::value(Vec<T>::raw(z + column)), column);
           }
       }
-    cut.add(tid < rem, tail(), tail_column());
+    cut.add(true, tail(), tail_column());
     return cut.n;
   }
 
-  // put(i, key) for i = 0 .. top - 1; key 0 where there are no more.
-  template <class Put>
-  __device__ __forceinline__ void top(Shared& shared, uint32_t top, Put put) const {
-    uint32_t n = collect(shared, reached_by(shared.lane_most[tid], top));
-    if (n > Candidates::kRoom) n = collect_in_turns(shared, top);
-    shared.list.put_best(n, top, put);
+  // The list ends with n candidates, the `top` best among them.
+  __device__ __forceinline__ uint32_t candidates(Shared& shared, uint32_t top) const {
+    const uint32_t n = collect(shared, reached_by(shared.lane_most[tid], top));
+    return n <= Candidates::kRoom ? n : collect_in_turns(shared, top);
   }
 };
 
-template <class T, int WAVES, int U>
+// Whether a row of so many vectors is added up in parts.
+template <int WAVES, int U>
+__host__ __device__ constexpr bool in_parts(int64_t full) { return full > 7 * WAVES * kWave * U; }
+
+// What a part of a row leaves for the row's end: its sums and candidates for the top tokens.
+struct PartResult {
+  Sums sums;
+  int32_t keys;
+  uint64_t key[kWave];
+};
+
+// A block for each row, or (kSplit) for each part of one.
+template <class T, int WAVES, int U, bool kSplit>
 __global__ __launch_bounds__(WAVES * kWave)
-void long_scores_kernel(ScoresArgs a) {
+void long_scores_kernel(ScoresArgs a, PartResult* results) {
   using Row = LongRow<T, WAVES, U>;
   __shared__ typename Row::Shared shared;
   const int64_t row = static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
@@ -737,20 +829,45 @@ void long_scores_kernel(ScoresArgs a) {
   const uint32_t tid = threadIdx.x;
   const Target target(a, row);
   if (!target.counts) {
+    if (kSplit) return;
     if (tid == 0) RowScores().write(a, row);
     if (static_cast<int>(tid) < a.top) RowScores().write_top(a, row, tid, 0.f, -1);
     return;
   }
-  const Row at(static_cast<const T*>(a.logits) + row * a.stride, static_cast<uint32_t>(a.cols), tid);
-  const uint32_t target_raw = Vec<T>::raw(at.z + target.column());
-  float most;
-  Sums s = at.sums(shared, most);
-  most = lane_group_max<WAVES>(most);
+  Row at(static_cast<const T*>(a.logits) + row * a.stride, static_cast<uint32_t>(a.cols), tid);
+  const uint32_t target_raw = kSplit ? 0 : Vec<T>::raw(at.z + target.column());
+  const uint32_t turns = at.end, part_turns = in_parts<WAVES, U>(at.full) ? std::max((turns + kParts - 1) / kParts, kPartTurns) : turns;
+  if constexpr (kSplit) {
+    at.begin = std::min(blockIdx.z * part_turns, turns);
+    at.end = std::min(at.begin + part_turns, turns);
+  }
+  const float most = lane_group_max<WAVES>(at.template sums<kSplit ? kPartAhead : 1>(shared, part_turns));
   if (tid % WAVES == 0) shared.lane_most[tid / WAVES] = most;
-  if (tid % kWave == 0) shared.parts[tid / kWave] = s;
   __syncthreads();
   if (tid >= kWave) return;
-  s = join_lanes<WAVES>(shared.parts[tid % WAVES]);
+  Sums s = join_lanes<WAVES>(shared.parts[0][tid % WAVES]);
+  if constexpr (kSplit) {
+    PartResult& result = results[row * kParts + blockIdx.z];
+    uint32_t n = 0;
+    if (a.top > 0) {
+      n = at.candidates(shared, a.top);
+      wave_sync();
+      if (n > kWave) {
+        shared.list.sort(n);
+        n = a.top;
+      }
+      if (tid < n) result.key[tid] = shared.list.key[tid];
+    }
+    if (tid == 0) {
+      result.sums = s;
+      result.keys = static_cast<int32_t>(n);
+    }
+    return;
+  }
+  if (in_parts<WAVES, U>(at.full)) {
+#pragma unroll
+    for (uint32_t p = 1; p < kParts; ++p) s = both(s, join_lanes<WAVES>(shared.parts[p][tid % WAVES]));
+  }
   const RowScores scores(s, Vec<T>::value(target_raw));
   if (tid == 0) scores.write(a, row);
   if (a.top == 0) return;
@@ -758,7 +875,50 @@ void long_scores_kernel(ScoresArgs a) {
     if (static_cast<int>(tid) < a.top) scores.write_top(a, row, tid, 0.f, -1);
     return;
   }
-  at.top(shared, a.top, [&](uint32_t i, uint64_t key) { scores.write_top(a, row, i, value_of(key), key == 0 ? -1 : column_of(key)); });
+  shared.list.put_best(at.candidates(shared, a.top), a.top, [&](uint32_t i, uint64_t key) {
+    scores.write_top(a, row, i, value_of(key), key == 0 ? -1 : column_of(key));
+  });
+}
+
+// The end of rows that had a block for each part.
+template <class T>
+__global__ __launch_bounds__(kParts * kWave)
+void parts_end_kernel(ScoresArgs a, const PartResult* results) {
+  __shared__ uint64_t keys[kParts * kWave];
+  const int64_t row = blockIdx.x;
+  const uint32_t tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const Target target(a, row);
+  if (!target.counts) {
+    if (tid == 0) RowScores().write(a, row);
+    if (static_cast<int>(tid) < a.top) RowScores().write_top(a, row, tid, 0.f, -1);
+    return;
+  }
+  const PartResult* parts = results + row * kParts;
+  const uint32_t target_raw = Vec<T>::raw(static_cast<const T*>(a.logits) + row * a.stride + target.column());
+  const uint64_t raw_key = parts[wave].key[lane];   // of the first `keys` lanes
+  // Each wave has a part's candidates; they lie after each other.
+  Sums s;
+  uint32_t all = 0, ahead = 0, own = 0;
+#pragma unroll
+  for (uint32_t p = 0; p < kParts; ++p) {
+    s = p == 0 ? parts[p].sums : both(s, parts[p].sums);
+    const uint32_t n = parts[p].keys;
+    ahead += p < wave ? n : 0;
+    own = p == wave ? n : own;
+    all += n;
+  }
+  const bool has_key = lane < own;
+  const uint64_t key = has_key ? raw_key : 0;
+  if (has_key) keys[ahead + lane] = key;
+  __syncthreads();
+  const RowScores scores(s, Vec<T>::value(target_raw));
+  if (tid == 0) scores.write(a, row);
+  const uint32_t top = a.top, there = scores.any ? all : 0;
+  if (tid < top && tid >= there) scores.write_top(a, row, tid, 0.f, -1);
+  if (!has_key || !scores.any) return;
+  uint32_t rank = 0;
+  for (uint32_t j = 0; j < all; ++j) rank += keys[j] > key;
+  if (rank < top) scores.write_top(a, row, rank, value_of(key), column_of(key));
 }
 
 // One block per kRows rows.
@@ -770,8 +930,32 @@ hipError_t launch_rows(Kernel kernel, const ScoresArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Few rows that are added up in parts have a block for each.
+constexpr int64_t kFewRows = 64;
 template <class T>
-hipError_t launch_typed(const ScoresArgs& a, hipStream_t stream) {
+bool splits(int64_t rows, int64_t cols) {
+  return rows > 0 && rows <= kFewRows && cols > 0 && in_parts<kLongWaves, kLongVectors>((cols - 1) / Vec<T>::kN);
+}
+
+template <class T>
+hipError_t launch_split(const ScoresArgs& a, PartResult* results, hipStream_t stream) {
+  const dim3 grid(static_cast<uint32_t>(a.rows), 1, kParts);
+  long_scores_kernel<T, kLongWaves, kLongVectors, true><<<grid, kLongWaves * kWave, 0, stream>>>(a, results);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  parts_end_kernel<T><<<static_cast<uint32_t>(a.rows), kParts * kWave, 0, stream>>>(a, results);
+  return hipGetLastError();
+}
+
+template <class T, int WAVES, int U>
+hipError_t launch_long(const ScoresArgs& a, hipStream_t stream) {
+  const int64_t x = std::min(a.rows, kGridX);
+  const dim3 grid(static_cast<uint32_t>(x), static_cast<uint32_t>((a.rows + x - 1) / x));
+  long_scores_kernel<T, WAVES, U, false><<<grid, WAVES * kWave, 0, stream>>>(a, nullptr);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t launch_typed(const ScoresArgs& a, void* workspace, hipStream_t stream) {
   const int64_t vectors = (a.cols + Vec<T>::kN - 1) / Vec<T>::kN, full = a.cols / Vec<T>::kN;
   if (vectors <= 1) return launch_rows<1>(short_scores_kernel<T, 1, 1>, a, stream);
   if (vectors <= 2) return launch_rows<1>(short_scores_kernel<T, 1, 2>, a, stream);
@@ -786,20 +970,24 @@ hipError_t launch_typed(const ScoresArgs& a, hipStream_t stream) {
   if (full <= 256) return launch_rows<64>(wave_scores_kernel<T, 4>, a, stream);
   if (full <= 384) return launch_rows<64>(wave_scores_kernel<T, 6>, a, stream);
   if (full <= 512) return launch_rows<64>(wave_scores_kernel<T, 8>, a, stream);
-  if (full <= 1536) return launch_rows<128>(long_scores_kernel<T, 2, 2>, a, stream);
-  if (full <= 2048) return launch_rows<256>(long_scores_kernel<T, 4, 2>, a, stream);
-  return launch_rows<512>(long_scores_kernel<T, 8, 2>, a, stream);
+  if (full <= 1536) return launch_long<T, 2, 2>(a, stream);
+  if (full <= 2048) return launch_long<T, 4, 2>(a, stream);
+  if (splits<T>(a.rows, a.cols)) return launch_split<T>(a, static_cast<PartResult*>(workspace), stream);
+  return launch_long<T, kLongWaves, kLongVectors>(a, stream);
 }
 
 }  // namespace
 
-size_t scores_workspace_bytes(int64_t, int64_t, int64_t, int) { return 0; }
+size_t scores_workspace_bytes(int64_t rows, int64_t cols, int dtype) {
+  const bool split = dtype == PGC_F32 ? splits<float>(rows, cols) : splits<__bf16>(rows, cols);
+  return split ? static_cast<size_t>(rows) * kParts * sizeof(PartResult) : 0;
+}
 
-hipError_t launch_scores(const ScoresArgs& a, int dtype, void*, hipStream_t stream) {
+hipError_t launch_scores(const ScoresArgs& a, int dtype, void* workspace, hipStream_t stream) {
   switch (dtype) {
-    case PGC_F32: return launch_typed<float>(a, stream);
-    case PGC_BF16: return launch_typed<__bf16>(a, stream);
-    default: return launch_typed<_Float16>(a, stream);
+    case PGC_F32: return launch_typed<float>(a, workspace, stream);
+    case PGC_BF16: return launch_typed<__bf16>(a, workspace, stream);
+    default: return launch_typed<_Float16>(a, workspace, stream);
   }
 }
 

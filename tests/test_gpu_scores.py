@@ -251,6 +251,39 @@ def test_special_rows(dtype, cols):
     assert not ops.token_scores_backward(z.cuda(), None, stats, zero, None, zero).any()
 
 
+def _spiked_rows(cols):
+    """Values that the sums' reference points do not fit: the maximum far above or below the rest, at the front, in the
+    middle, at the end; slopes over the whole row; parts of nothing but -inf."""
+    rng = np.random.default_rng(cols)
+    base, at = rng.normal(size=cols), np.arange(cols)
+    rows = [base.copy() for _ in range(9)]
+    rows[0][:8] += 300.0
+    rows[1][-1] += 300.0
+    rows[2][cols // 2] += 50.0
+    rows[3][:cols // 2] -= 400.0
+    rows[4][cols // 2:] -= 400.0
+    rows[5] = at / cols * 200.0 - 100.0
+    rows[6] = -at / cols * 200.0
+    rows[7][:cols - cols // 3] = -INF
+    rows[8] = np.where(at % 64 < 8, -INF, base + (at // 4096) * 13.0)
+    return torch.from_numpy(np.stack(rows).astype(np.float32))
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("cols", [9, 64, 513, 1000, 4100, 9001, 20000, 33000, 70001, 131073, 262147])
+def test_maxima_far_from_the_rest(dtype, cols):
+    _say("spikes", dtype, cols)
+    for shift in (0, 1):
+        z = _spiked_rows(cols).to(DTYPES[dtype])
+        y = torch.from_numpy(np.random.default_rng(cols).integers(0, cols, len(z)).astype(np.int32))
+        _check(z, y, 11, dtype, shift, shift)
+        more = 70    # more rows than have blocks for their parts
+        many = ops.token_scores(torch.cat([z, z[:1].expand(more, cols)]).cuda(), None, 11)
+        few = ops.token_scores(z.cuda(), None, 11)
+        for a, b in zip(many[1:], few[1:]):
+            assert torch.equal(a[:len(z)], b)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("cols", [10, 64, 1000, 9001, 131071])
 def test_logits_of_large_magnitude(dtype, cols):
