@@ -1,18 +1,22 @@
 #!/usr/bin/env python3
 """Trains a small language-model head by pipelined gradient coding with the operators of
-paper_2607_20739_amd.ops: dropout, token log-probabilities, the preference loss, the policy loss.
+paper_2607_20739_amd.ops: dropout, token log-probabilities, the preference loss, the policy loss, the scores of
+tokens, the norm of gradients, the AdamW step.
 
   python examples/coded_preference.py                       PGC-FR, 4 workers, one straggler a step
   python examples/coded_preference.py --scheme CR --n 6 --c 3 --steps 60
+  python examples/coded_preference.py --optimizer adamw8 --entropy 0.01      8-bit states, an entropy bonus
 
 n workers hold c partitions of preference pairs each (Sec. III).  At step t >= 1 a worker evaluates the
 one in slot (t - 1) mod c, keeps the latest gradient of each, and sends their coded sum; the master
 ignores the stragglers, decodes and updates (Sec. IV-A, V-B).  A second phase goes on with the
-policy loss on the preferred answers, scored by the first phase's model.
+policy loss on the preferred answers, scored by the first phase's model, with a bonus for the entropy where that
+is asked for.  The update is plain descent, or an AdamW step on the decoded gradient, whose norm is bounded.
 
 A partition's gradient must be the same whichever worker evaluates it.  Hence dropout draws its mask
 from the step and the token's number in the data set, and every loss is a fixed-order sum over its own
-rows.  With FR the decoded gradient then is the same for every set of stragglers, to the last bit.
+rows.  With FR the decoded gradient then is the same for every set of stragglers, to the last bit, and so is
+every update from it.
 
 The model is features -> hidden (ReLU, dropout, residual) -> vocabulary, in bf16 products by torch.
 The data is synthetic: a fixed random teacher writes the preferred answers, chance the others.
@@ -133,10 +137,32 @@ class Coded:
         P.pgc_destroy(self.ctx)
 
 
+class Update:
+    """The step from a decoded gradient: "sgd", or "adamw" and "adamw8" with states in 32 bits and 8."""
+
+    def __init__(self, head, how, max_norm=1.0):
+        n = head.width * head.width
+        self.parts = [slice(0, n), slice(n, None)]
+        self.how, self.max_norm, self.step = how, max_norm, 0
+        if how != "sgd":
+            self.states = ops.adamw_states([head.w[part] for part in self.parts], 8 if how == "adamw8" else 32)
+
+    def __call__(self, w, ghat, rate):
+        self.step += 1
+        if self.how == "sgd":
+            w -= rate * ghat
+            return
+        moments, variances, scales = self.states
+        _, factor = ops.grad_norm([ghat], self.max_norm)
+        ops.adamw([w[part] for part in self.parts], [ghat[part] for part in self.parts], moments, variances, self.step, 0.1 * rate,
+                  weight_decay=0.01, scales=scales, factor=factor)
+
+
 def train(scheme="FR", n=4, c=2, steps=40, policy_steps=20, pairs=6, longest=12, width=64, vocab=1000, lr=0.2, policy_lr=0.1, p=0.1,
-          mask_seed=3, device="cuda", each_worker=False):
+          mask_seed=3, device="cuda", each_worker=False, optimizer="sgd", entropy=0.0):
     """Both phases; returns {"preference": losses, "accuracy": of the pairs, "policy": losses, "w": parameters,
-    "words": each worker's word of each step, where each evaluates its own}."""
+    "words": each worker's word of each step, where each evaluates its own; "entropy": the model's mean over the tokens,
+    "first": the share of preferred answers' tokens that the model has first, both at the end}."""
     g = torch.Generator(device=device)
     g.manual_seed(1)
     teacher = torch.randn(width, vocab, generator=g, device=device)
@@ -145,6 +171,7 @@ def train(scheme="FR", n=4, c=2, steps=40, policy_steps=20, pairs=6, longest=12,
     # The reference model's scores are fixed: the model before the first step.
     reference = [ops.token_logprobs(head.logits(head.w, part.x), part.targets)[0] for part in data]
     out = {"preference": [], "policy": [], "words": []}
+    update = Update(head, optimizer)
 
     def run(count, first, loss_of, rate, name):
         coded = Coded(scheme, n, c, head.w.numel(), device, each_worker)
@@ -158,7 +185,7 @@ def train(scheme="FR", n=4, c=2, steps=40, policy_steps=20, pairs=6, longest=12,
                     value, grad = head.gradient(data[k], loss_of(k), drop)
                     values.append(value)
                     return grad
-                head.w -= rate * coded.step(evaluate, mask)
+                update(head.w, coded.step(evaluate, mask), rate)
                 out[name].append(float(torch.stack(values).mean()))
                 if each_worker:
                     out["words"].append([coded.word(j) for j in range(n)])
@@ -187,10 +214,17 @@ def train(scheme="FR", n=4, c=2, steps=40, policy_steps=20, pairs=6, longest=12,
         def loss(z):
             value, _, dz = ops.policy_loss(z, part.targets, old[k], advantages, ref_logprobs=reference[k], clip_high=0.28,
                                            kl=0.01, scale=1.0 / len(part.x))
+            if entropy:
+                _, h, _, _, stats = ops.token_scores(z, part.targets)
+                dz += ops.token_scores_backward(z, part.targets, stats, h, grad_entropy=torch.full_like(h, -entropy / len(part.x)))
             return value.mean(), dz
         return loss
 
     run(policy_steps, steps, policy_of, policy_lr, "policy")
+    scores = [ops.token_scores(head.logits(head.w, part.x), part.targets, 1) for part in data]
+    told = torch.cat([(part.targets >= 0) & part.preferred for part in data])
+    out["entropy"] = float(torch.cat([s[1] for s in scores])[told].mean())
+    out["first"] = float((torch.cat([s[3][:, 0] for s in scores]) == torch.cat([part.targets for part in data]))[told].float().mean())
     out["w"] = head.w
     return out
 
@@ -204,11 +238,15 @@ def main():
     ap.add_argument("--policy-steps", type=int, default=20)
     ap.add_argument("--vocab", type=int, default=1000)
     ap.add_argument("--each-worker", action="store_true", help="every worker evaluates its own copy of a partition")
+    ap.add_argument("--optimizer", choices=["sgd", "adamw", "adamw8"], default="sgd")
+    ap.add_argument("--entropy", type=float, default=0.0, help="weight of the entropy bonus in the policy phase")
     args = ap.parse_args()
-    out = train(args.scheme, args.n, args.c, args.steps, args.policy_steps, vocab=args.vocab, each_worker=args.each_worker)
+    out = train(args.scheme, args.n, args.c, args.steps, args.policy_steps, vocab=args.vocab, each_worker=args.each_worker,
+                optimizer=args.optimizer, entropy=args.entropy)
     print(json.dumps({"scheme": args.scheme, "n": args.n, "c": args.c, "preference_first": out["preference"][0],
                       "preference_last": out["preference"][-1], "pairs_ranked_right": out["accuracy"],
-                      "policy_first": out["policy"][0], "policy_last": out["policy"][-1]}))
+                      "policy_first": out["policy"][0], "policy_last": out["policy"][-1], "entropy": out["entropy"],
+                      "preferred_first": out["first"]}))
 
 
 if __name__ == "__main__":

@@ -549,7 +549,7 @@ struct RowShared {
   static constexpr uint32_t kGroups = 512;
   Sums parts[kParts][WAVES];
   float lane_most[kWave];                 // the largest of the values of WAVES lanes each
-  alignas(16) float most[kSlots][kThreads];   // the largest of a thread's turn; the last slot's of all turns from there on
+  alignas(16) float most[kSlots][kThreads];   // the largest of a thread's turn, or of a few that follow each other
   Candidates list;
   uint32_t groups[kGroups];               // turns and threads whose values may hold candidates
 };
@@ -564,10 +564,17 @@ struct LongRow {
   const T* z;
   uint32_t cols, full, rem, tid;
   uint32_t begin, end;      // the block's turns
+  uint32_t slot_shift = 0;  // 2^slot_shift of them share a slot of their maxima
 
   __device__ __forceinline__ LongRow(const T* z_, uint32_t cols_, uint32_t tid_)
       : z(z_), cols(cols_), full(long_row_vectors<T>(cols_)), rem(cols_ - full * kN), tid(tid_), begin(0), end((full + kTurn - 1) / kTurn) {}
-  __device__ __forceinline__ uint32_t slot(uint32_t turn) const { return std::min(turn - begin, Shared::kSlots - 1); }
+  __device__ __forceinline__ uint32_t slot(uint32_t turn) const { return (turn - begin) >> slot_shift; }
+  // Once the block's turns are known.
+  __device__ __forceinline__ void share_slots(Shared& shared) {
+    while ((end - begin + (1u << slot_shift) - 1) >> slot_shift > Shared::kSlots) ++slot_shift;
+    if (slot_shift > 0)
+      for (uint32_t i = 0; i < Shared::kSlots; ++i) shared.most[i][tid] = -INFINITY;
+  }
   __device__ __forceinline__ static uint32_t vector(uint32_t turn, uint32_t thread, uint32_t i) {
     return turn * kTurn + thread / kWave * (kWave * U) + i * kWave + thread % kWave;
   }
@@ -620,7 +627,7 @@ struct LongRow {
   // The largest of a turn's values of this lane, for its slot.
   __device__ __forceinline__ void keep(Shared& shared, uint32_t turn, float most) const {
     float& to = shared.most[slot(turn)][tid];
-    to = turn - begin < Shared::kSlots ? most : fmaxf(to, most);
+    to = slot_shift == 0 ? most : fmaxf(to, most);
   }
   // This wave's sums, by parts of so many turns, to shared.parts; and the largest of this lane's values.
   template <int AHEAD>
@@ -841,6 +848,7 @@ void long_scores_kernel(ScoresArgs a, PartResult* results) {
     at.begin = std::min(blockIdx.z * part_turns, turns);
     at.end = std::min(at.begin + part_turns, turns);
   }
+  at.share_slots(shared);
   const float most = lane_group_max<WAVES>(at.template sums<kSplit ? kPartAhead : 1>(shared, part_turns));
   if (tid % WAVES == 0) shared.lane_most[tid / WAVES] = most;
   __syncthreads();

@@ -284,6 +284,28 @@ def test_maxima_far_from_the_rest(dtype, cols):
             assert torch.equal(a[:len(z)], b)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("cols", [7, 300, 1000, 4100, 20000, 70001, 140003, 300001])
+def test_values_past_what_whole_numbers_reach(dtype, cols):
+    """Logits past 2^20 in the whole row, in one stretch of it, or at its ends: there the sums take another way."""
+    _say("large values", dtype, cols)
+    rng = np.random.default_rng(cols)
+    base = rng.normal(size=cols)
+    rows = [base * 3.0 + 5e6, base * 2.0, base * 2.0, base * 2.0, base * 1e7, base - 4e8, base * 2.0, -np.abs(base) * 1e30]
+    rows[1][cols // 2:cols // 2 + cols // 8 + 1] += 3e6
+    rows[2][:1] = 1e9
+    rows[3][-1:] = 2e6
+    rows[6][cols // 3:cols // 2] -= 5e7
+    z = torch.from_numpy(np.stack(rows).astype(np.float32)).to(DTYPES[dtype])
+    y = torch.from_numpy(rng.integers(0, cols, len(z)).astype(np.int32))
+    for shift in (0, 1):
+        _check(z, y, 9, dtype, shift, shift)
+    many = ops.token_scores(torch.cat([z, z[1:2].expand(70, cols)]).cuda(), None, 9)
+    few = ops.token_scores(z.cuda(), None, 9)
+    for a, b in zip(many[1:], few[1:]):
+        assert torch.equal(a[:len(z)], b)
+
+
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("cols", [10, 64, 1000, 9001, 131071])
 def test_logits_of_large_magnitude(dtype, cols):
