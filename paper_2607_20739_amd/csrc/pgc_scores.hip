@@ -545,7 +545,7 @@ constexpr int kLongWaves = 8, kLongVectors = 2, kPartAhead = 4;
 // What a row's waves share.
 template <int WAVES>
 struct RowShared {
-  static constexpr uint32_t kSlots = WAVES <= 4 ? 6 : 16, kThreads = WAVES * kWave;
+  static constexpr uint32_t kSlots = 2 * WAVES <= 6 ? 6 : 2 * WAVES, kThreads = WAVES * kWave;
   static constexpr uint32_t kGroups = 512;
   Sums parts[kParts][WAVES];
   float lane_most[kWave];                 // the largest of the values of WAVES lanes each
@@ -938,7 +938,9 @@ hipError_t launch_rows(Kernel kernel, const ScoresArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// Few rows that are added up in parts have a block for each.
+// Few rows that are added up in parts have a block for each, and a second launch: with 20 top tokens 1 x 131,072 bf16 13.0 us (one
+// launch 20.3), 64 15.5 (22.1), 1 x 131,072 fp32 15.6 (40.3), 1 x 65,536 bf16 12.4 (13.4).  100 x 131,072 22.3 and 25.1, but
+// 200 30 and 26.
 constexpr int64_t kFewRows = 64;
 template <class T>
 bool splits(int64_t rows, int64_t cols) {
@@ -972,14 +974,19 @@ hipError_t launch_typed(const ScoresArgs& a, void* workspace, hipStream_t stream
   if (vectors <= 16) return launch_rows<4>(short_scores_kernel<T, 4, 4>, a, stream);
   if (vectors <= 32) return launch_rows<8>(short_scores_kernel<T, 8, 4>, a, stream);
   if (vectors <= 64) return launch_rows<16>(short_scores_kernel<T, 16, 4>, a, stream);
+  // 200,000 rows of 1,000 bf16 152 us from a wave's registers, 228 by turns.
   if (full <= 64) return launch_rows<64>(wave_scores_kernel<T, 1>, a, stream);
   if (full <= 128) return launch_rows<64>(wave_scores_kernel<T, 2>, a, stream);
   if (full <= 192) return launch_rows<64>(wave_scores_kernel<T, 3>, a, stream);
   if (full <= 256) return launch_rows<64>(wave_scores_kernel<T, 4>, a, stream);
   if (full <= 384) return launch_rows<64>(wave_scores_kernel<T, 6>, a, stream);
   if (full <= 512) return launch_rows<64>(wave_scores_kernel<T, 8>, a, stream);
+  // More waves share what a row costs besides its values, but each adds to it, and leaves the chip fewer rows at once: in rows of
+  // 9,000 bf16 columns (1,125 vectors) 60,000 take 216 us on 2 waves, 242 on 4, 416 on 8; 30,000 of 20,001 228, 215 and 299;
+  // 12,000 of 50,021 fp16 239, 221 and 222, but 48 of them 24, 16 and 11; 16 of 20,000 12.1, 8.4 and 7.3.  On 8,192 of 131,072
+  // bf16 8 waves with 2 vectors per lane in turn take 338 us, with 4 445, 4 waves 378, 16 waves 425 with 2 and 474 with 4.
   if (full <= 1536) return launch_long<T, 2, 2>(a, stream);
-  if (full <= 2048) return launch_long<T, 4, 2>(a, stream);
+  if (full <= 4096) return launch_long<T, 4, 2>(a, stream);
   if (splits<T>(a.rows, a.cols)) return launch_split<T>(a, static_cast<PartResult*>(workspace), stream);
   return launch_long<T, kLongWaves, kLongVectors>(a, stream);
 }
