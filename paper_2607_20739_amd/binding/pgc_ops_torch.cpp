@@ -17,6 +17,7 @@
 #include <c10/core/DeviceGuard.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/forward_grad.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 
@@ -42,12 +43,13 @@ int dtype_of(const at::Tensor& t) {
   }
 }
 
-const at::Tensor& tensor(const char* name, PyObject* o) {
+// Of many tensors the caller asks once whether any can carry a tangent, which of views takes a lock.
+const at::Tensor& tensor(const char* name, PyObject* o, bool tangents = true) {
   TORCH_CHECK_VALUE(THPVariable_Check(o), name, " must be a tensor");
   const at::Tensor& t = THPVariable_Unpack(o);
   TORCH_CHECK_VALUE(!t.is_neg(), name, " must not be a view that negates its values on reading (resolve_neg() writes them out)");
-  // Otherwise the result would have no tangent, which counts as 0.  (A tensor that autograd knows nothing of has none.)
-  TORCH_CHECK_NOT_IMPLEMENTED(t.unsafeGetTensorImpl()->autograd_meta() == nullptr || !t._fw_grad(0).defined() || !c10::AutogradState::get_tls_state().get_fw_grad_mode(),
+  // Otherwise the result would have no tangent, which counts as 0.
+  TORCH_CHECK_NOT_IMPLEMENTED(!tangents || !t._fw_grad(0).defined() || !c10::AutogradState::get_tls_state().get_fw_grad_mode(),
                               "forward-mode derivatives of the operators are not implemented, and ", name, " carries a tangent");
   return t;
 }
@@ -405,19 +407,20 @@ PyObject* token_scores_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // A list of tensors: a Python sequence and its items, which it keeps alive.
 class List {
  public:
-  List(const char* name, PyObject* o) : name_(name) {
+  List(const char* name, PyObject* o) : name_(name), tangents_(torch::autograd::ForwardADLevel::try_get_by_idx(0) != nullptr) {
     TORCH_CHECK_VALUE(!THPVariable_Check(o) && PySequence_Check(o), name, " must be a list of tensors");
     items_ = THPObjectPtr(PySequence_Fast(o, "a list of tensors"));
     if (!items_) throw python_error();
   }
   int64_t size() const { return PySequence_Fast_GET_SIZE(items_.get()); }
   PyObject* item(int64_t i) const { return PySequence_Fast_GET_ITEM(items_.get(), i); }
-  const at::Tensor& operator[](int64_t i) const { return tensor(name_, item(i)); }
+  const at::Tensor& operator[](int64_t i) const { return tensor(name_, item(i), tangents_); }
   const char* name() const { return name_; }
   void expect_size(int64_t n) const { TORCH_CHECK_VALUE(size() == n, name_, " must have as many tensors as the first list: ", n); }
 
  private:
   const char* name_;
+  bool tangents_;
   mutable THPObjectPtr items_;
 };
 
@@ -458,8 +461,7 @@ class Changed {
   std::vector<c10::TensorImpl*> impls_;
 };
 void no_gradient(const char* name, const at::Tensor& t) {
-  TORCH_CHECK_VALUE(t.unsafeGetTensorImpl()->autograd_meta() == nullptr || !t.requires_grad() || !at::GradMode::is_enabled(), name,
-                    " must not ask for a gradient (detach() them)");
+  TORCH_CHECK_VALUE(!t.requires_grad() || !at::GradMode::is_enabled(), name, " must not ask for a gradient (detach() them)");
 }
 
 // One value on the GPU; null for None.
@@ -532,7 +534,7 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& p = dense("params", params[i]);
     if (!device) device = p.device();
     TORCH_CHECK_VALUE(p.device() == *device, "params must be on one GPU");
-    TORCH_CHECK_VALUE(p.is_leaf() || !p.requires_grad() || !at::GradMode::is_enabled(),
+    TORCH_CHECK_VALUE(!p.requires_grad() || !at::GradMode::is_enabled() || p.is_leaf(),
                       "params that were computed cannot be changed where a gradient is asked for (detach() them)");
     const at::Tensor &g = beside("grads", grads[i], p), &m = beside("moments", moments[i], p), &v = beside("variances", variances[i], p);
     of_type("moments", m, scales ? at::kByte : at::kFloat);
