@@ -18,7 +18,8 @@
  *     is checked before any work is enqueued.
  *   - All pointers are device pointers unless stated; `hip_stream` is a hipStream_t
  *     (NULL = the null stream) of the current device.  Work is enqueued and not
- *     synchronised.  Nothing is allocated; the calls can be captured into a graph.
+ *     synchronised.  Nothing is allocated on the device; the calls can be captured into
+ *     a graph, which replays them with the arguments that they were captured with.
  *   - Matrices are row-major; a stride is the number of values between the starts of
  *     two rows, at least the number of columns.  Data is aligned to its own type;
  *     nothing else is asked of addresses, strides and sizes.

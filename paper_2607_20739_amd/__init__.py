@@ -6,7 +6,9 @@ lets torch own the workspace memory and the stream.  There is no fallback:
 if the library is missing, every call raises.
 
 The submodule `ops` binds include/pgc_ops.h: dropout, token log-probabilities,
-the preference loss and the policy loss, to compute a partition's gradient with.
+the preference loss, the policy loss and the scores of tokens, to compute a
+partition's gradient with; the norm of gradients and the AdamW step, to update
+with the decoded one.
 """
 
 from ._lib import *  # noqa: F401,F403  (the C entry points, same names)

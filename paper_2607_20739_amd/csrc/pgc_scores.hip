@@ -18,6 +18,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "pgc_ops_kernels.h"
 #include "pgc_rows.h"
@@ -41,6 +42,17 @@ __device__ __forceinline__ float wave_join(float v, Join join) {
   v = join(__uint_as_float(rows[0]), __uint_as_float(rows[1]));
   const auto halves = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return join(__uint_as_float(halves[0]), __uint_as_float(halves[1]));
+}
+__device__ __forceinline__ uint32_t wave_max_bits(uint32_t v) {
+  auto moved = [&](auto ctrl) { return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), decltype(ctrl)::value, 0xF, 0xF, true)); };
+  v = std::max(v, moved(std::integral_constant<int, kDppSwap1>()));
+  v = std::max(v, moved(std::integral_constant<int, kDppSwap2>()));
+  v = std::max(v, moved(std::integral_constant<int, kDppHalfMirror>()));
+  v = std::max(v, moved(std::integral_constant<int, kDppMirror>()));
+  const auto rows = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = std::max<uint32_t>(rows[0], rows[1]);
+  const auto halves = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return __builtin_amdgcn_readfirstlane(std::max<uint32_t>(halves[0], halves[1]));
 }
 __device__ __forceinline__ float wave_sum(float v) { return wave_join(v, [](float x, float y) { return x + y; }); }
 __device__ __forceinline__ float wave_max(float v) { return wave_join(v, [](float x, float y) { return fmaxf(x, y); }); }
@@ -377,7 +389,7 @@ struct Candidates {
     return append(n, v >= bound && v > -INFINITY, key_of(v, column));
   }
 
-  // Sorts n of them downwards.
+  // Sorts n of them downwards, in LDS.
   __device__ __forceinline__ void sort(uint32_t n) {
     const uint32_t lane = threadIdx.x % kWave;
     uint32_t size = 2;
@@ -398,7 +410,38 @@ struct Candidates {
       }
   }
 
-  // The best of n, `there` many at most: put(i, key) for i = 0 .. top - 1; key 0 where there are no more.
+  // The best `top` of n, in order, to the front; returns how many there are.  Few are taken one by one, from registers: 200,000
+  // rows of 1,000 equal bf16 logits take 502 us with 8 top tokens so, 1,214 by sorting; of 64 by chance 1,625 and 953.
+  __device__ __forceinline__ uint32_t take_best(uint32_t n, uint32_t top) {
+    constexpr uint32_t kEach = kRoom / kWave, kMostByOne = 24;
+    const uint32_t lane = threadIdx.x % kWave;
+    if (top > kMostByOne) {
+      wave_sync();
+      sort(n);
+      return std::min(n, top);
+    }
+    uint64_t mine[kEach];
+    wave_sync();
+#pragma unroll
+    for (uint32_t i = 0; i < kEach; ++i) mine[i] = i * kWave + lane < n ? key[i * kWave + lane] : 0;
+    wave_sync();
+    for (uint32_t r = 0; r < top; ++r) {
+      uint64_t best = 0;
+#pragma unroll
+      for (uint32_t i = 0; i < kEach; ++i) best = std::max(best, mine[i]);
+      const uint32_t high = wave_max_bits(static_cast<uint32_t>(best >> 32));
+      const uint32_t low = wave_max_bits(best >> 32 == high ? static_cast<uint32_t>(best) : 0);
+      best = static_cast<uint64_t>(high) << 32 | low;
+      if (best == 0) return r;
+#pragma unroll
+      for (uint32_t i = 0; i < kEach; ++i) mine[i] = mine[i] == best ? 0 : mine[i];
+      if (lane == 0) key[r] = best;
+    }
+    wave_sync();
+    return top;
+  }
+
+  // The best of n: put(i, key) for i = 0 .. top - 1; key 0 where there are no more.
   template <class Put>
   __device__ __forceinline__ void put_best(uint32_t n, uint32_t top, Put put) {
     const uint32_t lane = threadIdx.x % kWave;
@@ -415,8 +458,9 @@ struct Candidates {
       if (rank < top) put(rank, mine);
       return;
     }
-    sort(n);
-    if (lane < top) put(lane, lane < n ? key[lane] : 0);
+    const uint32_t there = take_best(n, top);
+    wave_sync();
+    if (lane < top) put(lane, lane < there ? key[lane] : 0);
   }
 };
 static_assert(PGC_MAX_TOP <= kWave, "a lane for each of the top tokens");
@@ -426,16 +470,29 @@ static_assert(PGC_MAX_TOP <= kWave, "a lane for each of the top tokens");
 struct CutList {
   Candidates& list;
   uint32_t top, n = 0;
-  uint64_t floor = 0;     // what no longer counts
+  uint64_t floor;         // up to which candidates no longer count
 
+  // `bound`: a number that at least `top` values reach.
+  __device__ __forceinline__ CutList(Candidates& list_, uint32_t top_, float bound)
+      : list(list_), top(top_), floor((static_cast<uint64_t>(ordered(bound)) << 32) - 1) {}
+  // A vector of each lane, from column `first` on.
+  template <uint32_t N, class Floats>
+  __device__ __forceinline__ void add_vector(bool there, Floats f, uint32_t first) {
+#pragma unroll 1
+    for (uint32_t k = 0; k < N; ++k) {
+      float v = f[0];
+#pragma unroll
+      for (uint32_t j = 1; j < N; ++j) v = k == j ? f[j] : v;
+      add(there, v, first + k);
+    }
+  }
   __device__ __forceinline__ void add(bool there, float v, uint32_t column) {
     there = there && v > -INFINITY && key_of(v, column) > floor;
     if (__ballot(there) == 0) return;
     n = list.append(n, there, key_of(v, column));
     if (n <= Candidates::kRoom - kWave) return;
+    n = list.take_best(n, top);
     wave_sync();
-    list.sort(n);
-    n = std::min(n, top);
     floor = list.key[n - 1];
     wave_sync();
   }
@@ -522,12 +579,11 @@ void wave_scores_kernel(ScoresArgs a) {
   }
   n = list.append_value(n, tail, tail_column, bound);
   if (n > Candidates::kRoom) {
-    CutList cut{list, top};
-    for (uint32_t v0 = 0; v0 < full; v0 += kWave)
-      for (uint32_t k = 0; k < kN; ++k) {
-        const uint32_t column = std::min(v0 + lane, full - 1) * kN + k;
-        cut.add(v0 + lane < full, Vec<T>::value(Vec<T>::raw(z + column)), column);
-      }
+    CutList cut(list, top, bound);
+    for (uint32_t v0 = 0; v0 < full; v0 += kWave) {
+      const uint32_t v = std::min(v0 + lane, full - 1);
+      cut.template add_vector<kN>(v0 + lane < full, Vec<T>::floats(Vec<T>::template load<true>(z, v, 0)), v * kN);
+    }
     cut.add(lane < rem, tail, tail_column);
     n = cut.n;
   }
@@ -790,18 +846,18 @@ struct LongRow {
   }
 
   // The same where the candidates have no room.
-  __device__ __forceinline__ uint32_t collect_in_turns(Shared& shared, uint32_t top) const {
-    CutList cut{shared.list, top};
+  __device__ __forceinline__ uint32_t collect_in_turns(Shared& shared, uint32_t top, float bound) const {
+    CutList cut(shared.list, top, bound);
     for (uint32_t turn = begin; turn < end; ++turn)
       for (uint32_t thread = 0; thread < Shared::kThreads; thread += kWave) {
         const uint32_t first = vector(turn, thread + tid, 0);
         // (The lowest column of the turn's values with the largest of them.)
         if (__ballot(first < full && key_of(shared.most[slot(turn)][thread + tid], first * kN) > cut.floor) == 0) continue;
-        for (uint32_t i = 0; i < U; ++i)
-          for (uint32_t k = 0; k < kN; ++k) {
-            const uint32_t column = std::min(first + i * kWave, full - 1) * kN + k;
-            cut.add(first + i * kWave < full, Vec<T>::value(Vec<T>::raw(z + column)), column);
-          }
+#pragma unroll 1
+        for (uint32_t i = 0; i < U; ++i) {
+          const uint32_t v = std::min(first + i * kWave, full - 1);
+          cut.template add_vector<kN>(first + i * kWave < full, Vec<T>::floats(Vec<T>::template load<true>(z, v, 0)), v * kN);
+        }
       }
     cut.add(true, tail(), tail_column());
     return cut.n;
@@ -809,8 +865,9 @@ struct LongRow {
 
   // The list ends with n candidates, the `top` best among them.
   __device__ __forceinline__ uint32_t candidates(Shared& shared, uint32_t top) const {
-    const uint32_t n = collect(shared, reached_by(shared.lane_most[tid], top));
-    return n <= Candidates::kRoom ? n : collect_in_turns(shared, top);
+    const float bound = reached_by(shared.lane_most[tid], top);
+    const uint32_t n = collect(shared, bound);
+    return n <= Candidates::kRoom ? n : collect_in_turns(shared, top, bound);
   }
 };
 
@@ -859,11 +916,8 @@ void long_scores_kernel(ScoresArgs a, PartResult* results) {
     uint32_t n = 0;
     if (a.top > 0) {
       n = at.candidates(shared, a.top);
+      if (n > kWave) n = shared.list.take_best(n, a.top);
       wave_sync();
-      if (n > kWave) {
-        shared.list.sort(n);
-        n = a.top;
-      }
       if (tid < n) result.key[tid] = shared.list.key[tid];
     }
     if (tid == 0) {
