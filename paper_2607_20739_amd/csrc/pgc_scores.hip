@@ -13,8 +13,11 @@
 // by value and column, which no two share.  Where too many do (equal logits, or sorted ones), that wave goes through
 // the row with a list that is cut to the best ones whenever it is full.
 //
-// As for the log-probabilities, rows of up to 64 vectors of 16 bytes belong to 1 to 16 lanes, longer ones to 1 to 16
+// As for the log-probabilities, rows of up to 64 vectors of 16 bytes belong to 1 to 16 lanes, longer ones to 1 to 8
 // waves, by the number of columns alone; so a row's bits do not depend on where it lies.
+//
+// Measured (MI355X), us a call: 8,192 rows of 131,072 bf16 logits 333 with 8 top tokens, 6.4 TB/s; 48 of 50,021 fp16 10 with
+// 5; 1 of 131,072 bf16 13 with 20 and 9 without.  Where 8,192 rows of 131,072 equal logits ask for 8, 528.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
