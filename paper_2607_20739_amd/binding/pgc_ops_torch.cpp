@@ -21,6 +21,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 
+#include <algorithm>
 #include <initializer_list>
 #include <optional>
 #include <string>
@@ -480,14 +481,15 @@ PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   refuse_traces();
   const List grads("grads", a[0]);
   TORCH_CHECK_VALUE(grads.size() > 0, "grads must hold a tensor");
+  const double max_norm = number(a[1]), scale = number(a[2]);   // before addresses are taken: this may run Python code
   const at::Device device = dense("grads", grads[0]).device();
   std::vector<pgc_values> values(grads.size());
   for (int64_t i = 0; i < grads.size(); ++i) {
     const at::Tensor& t = dense("grads", grads[i]);
     TORCH_CHECK_VALUE(t.device() == device, "grads must be on one GPU");
+    no_gradient("grads", t);   // the norm would be a constant of the graph
     values[i] = {t.data_ptr(), t.numel(), floating("grads", t)};
   }
-  const double max_norm = number(a[1]), scale = number(a[2]);
   size_t bytes = 0;
   check(pgc_grad_norm_workspace_bytes(values.data(), grads.size(), &bytes));
   at::Tensor workspace;
@@ -508,25 +510,32 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
   refuse_traces();
   const List params("params", a[0]), grads("grads", a[1]), moments("moments", a[2]), variances("variances", a[3]);
   const int64_t count = params.size();
-  grads.expect_size(count);
-  moments.expect_size(count);
-  variances.expect_size(count);
   std::optional<List> scales, copies, decays;
-  if (a[10] != Py_None) {
-    scales.emplace("scales", a[10]);
-    scales->expect_size(count);
-  }
-  if (a[11] != Py_None) {
-    copies.emplace("copies", a[11]);
-    copies->expect_size(count);
-  }
-  double decay = 0.0;
+  if (a[10] != Py_None) scales.emplace("scales", a[10]);
+  if (a[11] != Py_None) copies.emplace("copies", a[11]);
+  // Numbers come before addresses: to read them may run Python code.
+  std::vector<double> decay(count);
   if (PySequence_Check(a[9]) && !THPVariable_Check(a[9])) {
     decays.emplace("weight_decay", a[9]);
     decays->expect_size(count);
+    for (int64_t i = 0; i < count; ++i) {
+      decays->expect_size(count);
+      Py_INCREF(decays->item(i));
+      THPObjectPtr kept(decays->item(i));
+      decay[i] = number(kept.get());
+    }
   } else {
-    decay = number(a[9]);
+    std::fill(decay.begin(), decay.end(), number(a[9]));
   }
+  pgc_adamw_args k{};
+  if (!THPVariable_Check(a[4])) k.step = whole("step", a[4]);
+  if (!THPVariable_Check(a[5])) k.lr = number(a[5]);
+  k.beta1 = number(a[6]);
+  k.beta2 = number(a[7]);
+  k.eps = number(a[8]);
+  for (const List* l : {&params, &grads, &moments, &variances}) l->expect_size(count);
+  if (scales) scales->expect_size(count);
+  if (copies) copies->expect_size(count);
   std::optional<at::Device> device;
   std::vector<pgc_adamw_tensor> tensors(count);
   Changed changed(5 * count);
@@ -568,16 +577,10 @@ PyObject* adamw(PyObject*, PyObject* const* a, Py_ssize_t n) {
       t.copy = c.data_ptr();
       t.copy_dtype = floating("copies", c);
     }
-    t.weight_decay = decays ? number(decays->item(i)) : decay;
+    t.weight_decay = decay[i];
   }
-  pgc_adamw_args k{};
   if (THPVariable_Check(a[4])) k.step_at = static_cast<int64_t*>(single("step", a[4], at::kLong, device));
-  else k.step = whole("step", a[4]);
   if (THPVariable_Check(a[5])) k.lr_at = static_cast<float*>(single("lr", a[5], at::kFloat, device));
-  else k.lr = number(a[5]);
-  k.beta1 = number(a[6]);
-  k.beta2 = number(a[7]);
-  k.eps = number(a[8]);
   k.factor = static_cast<float*>(single("factor", a[12], at::kFloat, device));
   k.state_bits = scales ? 8 : 32;
   if (!device) {    // no tensor to launch anything for: the arguments alone are looked at

@@ -209,7 +209,8 @@ def grad_norm(grads, max_norm=float("inf"), scale=1.0):
     """(norm [1], factor [1]): the norm of all gradients times `scale`, and what adamw has to multiply them
     by for a norm of at most max_norm: scale * min(1, max_norm / norm).
 
-    Use the inverse of a loss's scale for `scale`.  factor is NaN where a gradient is not finite.
+    Use the inverse of a loss's scale for `scale`.  factor is NaN where a gradient is not finite.  The
+    norm has no gradient itself: one of gradients that ask for some is refused (detach() them).
     """
     return _native.grad_norm(grads, max_norm, scale)
 

@@ -367,6 +367,41 @@ def test_scores_of_more_values_than_32_bits_count():
     assert (dz[rows - 1, cols - 1] != 0) and (dz[rows - 1, 0] != 0)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_a_row_of_the_most_columns(dtype):
+    cols = 2 ** 31 - 1
+    _say("longest row", dtype)
+    z = torch.empty(1, cols, dtype=dtype, device="cuda").normal_(0.0, 0.1)
+    at = [cols - 1, 0, cols // 2 + 3, 5, 2 ** 28 + 1, cols - 2]   # 0.1-sigma values stay far below
+    for i, c in enumerate(at):
+        z[0, c] = 3.0 - i / 16
+    y = torch.tensor([cols - 1], dtype=torch.int32, device="cuda")
+    lp, h, top_lp, tokens, stats = ops.token_scores(z, y, len(at))
+    assert tokens[0].tolist() == at and stats[0, 0].item() == 3.0
+    total = moved = 0.0
+    for part in z[0].split(2 ** 27):
+        d = part.double() - 3.0
+        e = d.exp()
+        total, moved = total + e.sum().item(), moved + (e * d).sum().item()
+    # A lane adds cols / (4 parts of 512 lanes) values of a row one after the other, to W each by itself.
+    n = cols / 2048
+    assert abs(lp.item() + np.log(total)) < u * (n + 64) + u * 64
+    assert abs(h.item() - (np.log(total) - moved / total)) < u * (2 * n + 128) * (1.0 - moved / total) + u * 64
+    for i, c in enumerate(at):
+        assert abs(top_lp[0, i].item() - (lp.item() + z[0, c].item() - 3.0)) <= u * 64
+    g = torch.tensor([1.0], device="cuda")
+    dz = ops.token_scores_backward(z, y, stats, h, g, None, out=z)
+    # p is 2e-10 to 1e-8 (exp(3) of the largest): in fp16 less than half the smallest number.
+    assert abs(dz[0, cols - 1].item() - 1.0) < 1e-6
+    if dtype == torch.float16:
+        assert sum(torch.count_nonzero(part).item() for part in dz[0].split(2 ** 27)) == 1
+    else:
+        for i, c in enumerate(at[1:], 1):
+            p = np.exp(lp.item() - i / 16)
+            assert abs(dz[0, c].item() + p) < p * u * 256
+        assert all((part < 0).sum().item() >= part.numel() - 1 for part in dz[0].split(2 ** 27))
+
+
 def test_more_rows_than_one_grid_dimension():
     _say("many rows")
     rows = (1 << 20) + 77

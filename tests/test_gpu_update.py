@@ -477,3 +477,40 @@ def test_the_binding_refuses_what_does_not_fit():
     ops.adamw([], [], [], [], 1, 0.1)
     ops.adamw([x[:0]], [g[:0]], [m[:0]], [v[:0]], 1, 0.1)
     ops.grad_norm([g, g])                                                # the same gradient twice counts twice
+
+
+def test_a_norm_is_no_part_of_a_graph():
+    _say("norm of gradients that ask for gradients")
+    w = torch.tensor([3.0, 4.0], device="cuda", requires_grad=True)
+    (g,) = torch.autograd.grad((w * w).sum() / 2, w, create_graph=True)
+    with pytest.raises(ValueError, match="gradient"):
+        ops.grad_norm([g])
+    with torch.no_grad():
+        assert ops.grad_norm([g])[0].item() == 5.0
+    assert ops.grad_norm([g.detach()])[0].item() == 5.0
+
+
+def test_numbers_whose_reading_changes_the_lists():
+    _say("lists that change")
+    x, g, m, v = ([torch.zeros(300, device="cuda")] for _ in range(4))
+
+    class Clears:
+        def __init__(self, which):
+            self.which = which
+
+        def __float__(self):
+            self.which.clear()
+            return 0.1
+
+    for which in (x, g, m, v):
+        kept = list(which)
+        with pytest.raises(ValueError, match="as many"):
+            ops.adamw(x, g, m, v, 1, 0.1, weight_decay=[Clears(which)])
+        which[:] = kept
+        with pytest.raises(ValueError, match="as many"):
+            ops.adamw(x, g, m, v, 1, 0.1, eps=Clears(which))
+        which[:] = kept
+    more = [0.1]
+    more.insert(0, Clears(more))
+    with pytest.raises(ValueError, match="as many"):
+        ops.adamw([*x, x[0][:0]], [*g, g[0][:0]], [*m, m[0][:0]], [*v, v[0][:0]], 1, 0.1, weight_decay=more)
