@@ -511,3 +511,42 @@ def test_scores_refuse_what_does_not_fit():
         assert h.shape == (0,) and top_lp.shape == tokens.shape == (0, 3) and st.shape == (0, 2)
         assert (lp is None) == (targets is None)
         assert ops.token_scores_backward(z[:0], targets, st, h, lp, h).shape == (0, 40)
+
+
+def test_calls_on_several_streams_at_once():
+    _say("calls at once")
+    z = [torch.randn(rows, 131072, device="cuda").to(torch.bfloat16) for rows in (1, 3, 40)]
+    want = [ops.token_scores(x, None, 20)[1:] for x in z]
+    streams = [torch.cuda.Stream() for _ in z]
+    torch.cuda.synchronize()
+    got = [[] for _ in z]
+    for _ in range(8):   # rows in parts have a workspace, and each call its own
+        for x, s, results in zip(z, streams, got):
+            with torch.cuda.stream(s):
+                results.append(ops.token_scores(x, None, 20)[1:])
+    torch.cuda.synchronize()
+    for w, results in zip(want, got):
+        assert all(torch.equal(a, b) for r in results for a, b in zip(r, w))
+
+
+def test_two_graphs_of_one_pool_replayed_in_turn():
+    _say("two graphs")
+    z = [torch.randn(2, 131072, device="cuda") for _ in range(2)]
+    for x in z:
+        ops.token_scores(x, None, 9)
+    torch.cuda.synchronize()
+    pool = torch.cuda.graph_pool_handle()
+    graphs, results = [], []
+    for x in z:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, pool=pool):
+            results.append(ops.token_scores(x, None, 9)[1:])
+        graphs.append(graph)
+    for turn in range(4):
+        for x in z:
+            x.normal_()
+        for graph in graphs:   # one after the other, as graphs of one pool may be
+            graph.replay()
+        torch.cuda.synchronize()
+        for x, r in zip(z, results):
+            assert all(torch.equal(a, b) for a, b in zip(r, ops.token_scores(x, None, 9)[1:]))
